@@ -158,6 +158,132 @@ const char* dc_flow_last_error(const dc_flow_state* s);
 /* Release the state and its device memory.  NULL is a no-op. */
 void dc_flow_free(dc_flow_state* s);
 
+/* ------------------------------------------------ attention operators
+ *
+ * What a streaming transformer's attention needs around its Linear layers,
+ * over tensors of the caller's: per-head norms with the position rotation, a
+ * carry of keys and values held in 4 bits, and the attention over that carry.
+ * A flow decoder made by dc_flow_init_opt runs the same kernels.
+ *
+ * Entries.  A call works on `batch` entries (streams) of `n` tokens each.
+ * Token i of entry e stands at position pos[e] + i.  With `lens`, entry e has
+ * only its first lens[e] tokens (0 .. n); rows behind them are neither read
+ * nor written.  These arrays are read on the device, so a captured call takes
+ * their values at each replay.  Values out of range are taken as the nearest
+ * that is in range; an entry with a negative position has no tokens.
+ *
+ * The carry keeps, per entry and key head, the first `sinks` tokens of a turn
+ * (the prompt) in slots of their own and the tokens after them in a ring of
+ * `ring` slots: position p >= sinks lies in ring slot (p - sinks) mod ring.  An
+ * entry may keep fewer first tokens (`sinks` of dc_span); it has to use the
+ * same number in every call of the turn.  The memory is the caller's
+ * (dc_carry4_bytes), needs no initial value, and holds no position or length:
+ * a call reads and writes exactly what its spans say, and a slot that no call
+ * has written is read only if a span names its position.
+ *
+ * Elements are OCP Microscaling E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) with one scale for 32 consecutive dimensions: 2^e, e the least
+ * integer in [-126, 126] for which 6 * 2^e is at least the group's largest
+ * magnitude; ties to the even code.  4.25 bits a value.  A group with a NaN
+ * or an infinity is held as NaN.
+ *
+ * Every call is launched on hip_stream, a stream of the current device, and
+ * returns without waiting; nothing is allocated, so calls can be captured.
+ * The device pointers have to be the current device's.  Errors: DC_EINVAL
+ * (nothing is launched), DC_ERANGE (a size past the kernels' limits),
+ * DC_EDEVICE; dc_carry4_last_error() explains the last one of the calling
+ * thread. */
+
+#define DC_CARRY4_ABI_VERSION 1
+
+typedef struct dc_carry4 {
+    int32_t abi_version;      /* DC_CARRY4_ABI_VERSION                                          */
+    int32_t batch, heads;     /* entries, key / value heads                                     */
+    int32_t head_dim;         /* 64 or 128                                                      */
+    int32_t sinks, ring;      /* slots of first tokens (>= 0), ring slots (>= 1); sum <= 2^24   */
+    void* data;               /* device, dc_carry4_bytes() bytes, 256-byte aligned              */
+} dc_carry4;
+
+typedef struct dc_span {
+    const int64_t* pos;       /* device [batch]: position of each entry's first token of the call */
+    const int32_t* lens;      /* device [batch]: tokens of each entry, or NULL: n each          */
+    const int32_t* sinks;     /* device [batch]: first tokens kept, or NULL: the carry's sinks  */
+    int32_t batch, n;         /* entries, tokens of a call                                      */
+} dc_span;
+
+/* Rows of heads: head h of token i of entry e at data + e stride_b + i
+ * stride_t + h stride_h, in elements; a row's head_dim elements are
+ * consecutive.  Rows aligned to 16 bytes are read and written in 16-byte
+ * words, others element by element. */
+typedef struct dc_head_rows {
+    void* data;
+    int64_t stride_b, stride_t, stride_h;
+    int32_t heads;
+} dc_head_rows;
+
+/* Per-head RMS norm and rotation: y = x / sqrt(mean(x^2) + eps) * gain; then
+ * pair j of the first 2 n_freqs dimensions turns by position * freqs[j]:
+ * (a, b) -> (a cos - b sin, b cos + a sin), a = y[j], b = y[j + n_freqs], or
+ * y[2 j], y[2 j + 1] interleaved.  Dimensions past 2 n_freqs are only
+ * normalised.  The angle is taken in 64 bits. */
+typedef struct dc_qk_norm {
+    const float* q_gain;      /* device [head_dim], or NULL: ones                               */
+    const float* k_gain;
+    const float* freqs;       /* device [n_freqs], radians a position                           */
+    int32_t n_freqs;          /* a multiple of 8, 2 n_freqs <= head_dim; 0: no rotation         */
+    int32_t interleaved;
+    float eps;                /* >= 0                                                           */
+} dc_qk_norm;
+
+/* q_out, k_out = norm and rotation of q, k (head_dim 64 or 128, dtype DC_F32
+ * or DC_BF16; sums in fp32, one rounding).  An output may be its input (the
+ * same rows); otherwise rows may not overlap. */
+dc_status dc_qk_norm_rope(const dc_qk_norm* norm, const dc_span* span, int32_t head_dim, int32_t dtype,
+                          const dc_head_rows* q, const dc_head_rows* k, const dc_head_rows* q_out,
+                          const dc_head_rows* k_out, void* hip_stream);
+
+/* Device bytes of the carry (0 for a carry that the calls refuse; data may be NULL). */
+int64_t dc_carry4_bytes(const dc_carry4* c);
+
+/* Store the span's keys and values.  With norm, q and k are normalised and
+ * rotated in the same pass: q_out receives the queries, and the keys are
+ * stored from their unrounded values; q and q_out are NULL without norm.  A
+ * call may hold more tokens than the ring: of tokens that share a slot the
+ * last one is stored. */
+dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_span* span, int32_t dtype,
+                           const dc_head_rows* q, const dc_head_rows* k, const dc_head_rows* v,
+                           const dc_head_rows* q_out, void* hip_stream);
+
+/* out = softmax(scale q k^T) v of the span's queries over the carry, which has
+ * to hold the call's own tokens already (dc_carry4_append with the same span).
+ * q->heads is a multiple of the carry's heads; query head h reads key head
+ * h / (q->heads / heads).  A query at position p sees the first tokens and
+ *   causal:  of both those up to p, and of the others the positions > p - window
+ *            (window >= 1);
+ *   else:    the positions in [pos - window, pos + len) of its entry, the same
+ *            for all its queries (window >= 0),
+ * as far as the ring still holds them after the call's last token: size it for
+ * window + n tokens (causal: one less).  A call that begins among the first
+ * tokens needs as many slots less as it stores there, so windows and calls of
+ * up to ring + sinks are taken; longer ones are refused (DC_ERANGE).
+ * workspace: dc_carry4_workspace() device bytes, 16-byte aligned (NULL where
+ * that is 0), not shared with a call that may run at the same time.  Sums and
+ * statistics in fp32; with DC_BF16 the probabilities are rounded to bf16 for
+ * the product with the values, with DC_F32 they are not.  Results do not depend
+ * on the other entries' data. */
+int64_t dc_carry4_workspace(const dc_carry4* c, int32_t q_heads, int32_t n, int32_t window);
+dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtype, const dc_head_rows* q,
+                           const dc_head_rows* out, int32_t window, int32_t causal, float scale, void* workspace,
+                           int64_t workspace_bytes, void* hip_stream);
+
+/* The values that the carry holds for the span's tokens (for audits): k, v in
+ * dtype (exact in both). */
+dc_status dc_carry4_read(const dc_carry4* c, const dc_span* span, int32_t dtype, const dc_head_rows* k,
+                         const dc_head_rows* v, void* hip_stream);
+
+/* Text of the calling thread's last error of these calls. */
+const char* dc_carry4_last_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1591,3 +1591,5 @@ hipError_t launch_carry_gather(const CarryRef& c, int b, int branch, int kv, int
 }
 
 }  // namespace dcf
+
+#include "carry4_kernels.h"

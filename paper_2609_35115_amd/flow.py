@@ -44,6 +44,29 @@ class DcFlowKernelStat(ctypes.Structure):
     ]
 
 
+class DcCarry4(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("sinks", ctypes.c_int32), ("ring", ctypes.c_int32), ("data", _P),
+    ]
+
+
+class DcSpan(ctypes.Structure):
+    _fields_ = [("pos", _P), ("lens", _P), ("sinks", _P), ("batch", ctypes.c_int32), ("n", ctypes.c_int32)]
+
+
+class DcHeadRows(ctypes.Structure):
+    _fields_ = [("data", _P), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class DcQkNorm(ctypes.Structure):
+    _fields_ = [("q_gain", _P), ("k_gain", _P), ("freqs", _P), ("n_freqs", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+_CARRY, _SPAN, _NORM, _ROWS = (ctypes.POINTER(t) for t in (DcCarry4, DcSpan, DcQkNorm, DcHeadRows))
+
 FLOW_SIGNATURES = {
     "dc_flow_blob_floats": ([ctypes.POINTER(DcFlowCfg)], ctypes.c_int64),
     "dc_flow_init": ([_P, ctypes.c_size_t, ctypes.POINTER(DcFlowCfg), ctypes.POINTER(_P)], ctypes.c_int),
@@ -57,6 +80,14 @@ FLOW_SIGNATURES = {
                          ctypes.POINTER(ctypes.c_int32)], ctypes.c_int),
     "dc_flow_last_error": ([_P], ctypes.c_char_p),
     "dc_flow_free": ([_P], None),
+    "dc_qk_norm_rope": ([_NORM, _SPAN, ctypes.c_int32, ctypes.c_int32, _ROWS, _ROWS, _ROWS, _ROWS, _P], ctypes.c_int),
+    "dc_carry4_bytes": ([_CARRY], ctypes.c_int64),
+    "dc_carry4_append": ([_CARRY, _NORM, _SPAN, ctypes.c_int32, _ROWS, _ROWS, _ROWS, _ROWS, _P], ctypes.c_int),
+    "dc_carry4_workspace": ([_CARRY, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32], ctypes.c_int64),
+    "dc_carry4_attend": ([_CARRY, _SPAN, ctypes.c_int32, _ROWS, _ROWS, ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
+                          _P, ctypes.c_int64, _P], ctypes.c_int),
+    "dc_carry4_read": ([_CARRY, _SPAN, ctypes.c_int32, _ROWS, _ROWS, _P], ctypes.c_int),
+    "dc_carry4_last_error": ([], ctypes.c_char_p),
 }
 
 _bound = False

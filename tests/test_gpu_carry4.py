@@ -1,0 +1,557 @@
+"""The attention operators on the GPU against plain 64-bit arithmetic: per-head
+norms and rotation, the 4-bit carry's stored values, attention over it, and a
+turn that uses all three.
+
+Bounds.  A bf16 rounding is off by at most 2^-8 of the value, an fp32 one by
+2^-24.  Stored values have no error: scaling by a power of two is exact, so
+they are compared for equality.
+  norm and rotation (fp32 part): the sum of D <= 128 squares passes at most 20
+  roundings, of which the root keeps half; three products, the fraction of a
+  turn (rounded at 2^-25, times 2 pi), sine and cosine and the rotation's own
+  come to less than 32 steps of 2^-24 of the two members' sum: 2^-18 of the
+  row's largest magnitude covers it.
+    The references' own angle is a 64-bit product, rounded at 2^-53 of itself:
+    at 7e10 radians (the largest here) 7.7e-6, which the bound adds.
+  attention: a score is off by at most e = (D + 8) 2^-24 scale sum |q||k|, a
+  probability by a factor of exp(2 e) and a few steps, the sums over K keys by
+  (K + 16) 2^-24 each; in bf16 the probabilities by 2^-8 and the result by
+  2^-8 of itself.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2609_35115_amd import DcError
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def carry4():
+    from paper_2609_35115_amd import carry4 as m
+    return m
+
+
+def held(x):
+    """The values that x [..., D] is held as, in 64 bits."""
+    y = x.double().cpu().unflatten(-1, (-1, 32))
+    top = y.abs().amax(-1, keepdim=True)
+    m, e = torch.frexp(torch.where(torch.isfinite(top), top, 1.0))
+    e = torch.where(m <= 0.75, e - 3, e - 2).clamp(-126, 126)
+    s = torch.ldexp(torch.ones_like(top), e)
+    a = y.abs() / s
+    step = torch.where(a >= 4, 2.0, torch.where(a >= 2, 1.0, 0.5)).double()
+    out = torch.sign(y) * torch.round(a / step) * step * s
+    out = torch.where(torch.isfinite(y).all(-1, keepdim=True), out, math.nan)
+    return out.flatten(-2)
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a.double().cpu(), nan=1e300), torch.nan_to_num(b.double().cpu(), nan=1e300))
+
+
+def turned(x, gain, pos, freqs, eps, interleaved):
+    """Norm and rotation in 64 bits of x [B][n][H][D]."""
+    x = x.double().cpu()
+    x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + eps)
+    if gain is not None:
+        x = x * gain.double().cpu()
+    if freqs is not None:
+        r = len(freqs)
+        t = ((pos.cpu()[:, None] + torch.arange(x.shape[1])).double()[..., None] * freqs.double().cpu())[:, :, None]
+        a, b = (x[..., 0:2 * r:2], x[..., 1:2 * r:2]) if interleaved else (x[..., :r], x[..., r:2 * r])
+        a, b = a * t.cos() - b * t.sin(), a * t.sin() + b * t.cos()
+        x = x.clone()
+        if interleaved:
+            x[..., 0:2 * r:2], x[..., 1:2 * r:2] = a, b
+        else:
+            x[..., :r], x[..., r:2 * r] = a, b
+    return x
+
+
+def near(got, want, rel, absolute):
+    """|got - want| <= rel |want| + absolute, NaN where want is."""
+    got, want = got.double().cpu(), want.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    off = torch.nan_to_num((got - want).abs() - rel * want.abs() - absolute, nan=-1.0)
+    if off.numel() == 0:   # an entry without tokens
+        return
+    assert off.max().item() <= 0, f"off by {off.max().item():.3e} more than its bound"
+
+
+class Model:
+    """Every token that a turn has stored, by entry and position, as held values."""
+
+    def __init__(self, B, H, D):
+        self.kv = [({}, {}) for _ in range(B)]
+
+    def append(self, k, v, pos, lens=None):
+        hk, hv = held(k), held(v)
+        for b in range(len(self.kv)):
+            for i in range(k.shape[1] if lens is None else int(lens[b])):
+                self.kv[b][0][int(pos[b]) + i], self.kv[b][1][int(pos[b]) + i] = hk[b, i], hv[b, i]
+
+    def attend(self, q, pos, window, lens, sinks, causal, scale=None):
+        """(result, absolute bound apart from bf16's) of every live row."""
+        q = q.double().cpu()
+        B, n, Hq, D = q.shape
+        out, bound = torch.zeros_like(q), torch.zeros(B, n, Hq, 1, dtype=torch.float64)
+        scale = D ** -0.5 if scale is None else scale
+        for b in range(B):
+            m = n if lens is None else int(lens[b])
+            for i in range(m):
+                p = int(pos[b]) + i
+                first = p - window + 1 if causal else int(pos[b]) - window
+                end = p + 1 if causal else int(pos[b]) + m
+                at = sorted(x for x in self.kv[b][0] if x < end and (x < sinks[b] or x >= first))
+                k, v = (torch.stack([t[x] for x in at]) for t in self.kv[b])   # [K][H][D]
+                g = Hq // k.shape[1]
+                for h in range(Hq):
+                    kk, vv = k[:, h // g], v[:, h // g]
+                    s = kk @ q[b, i, h] * scale
+                    out[b, i, h] = torch.softmax(s, 0) @ vv
+                    e = (D + 8) * 2.0 ** -24 * abs(scale) * float(torch.nan_to_num(kk.abs() @ q[b, i, h].abs()).max())
+                    bound[b, i, h] = (math.expm1(4 * e) + 4 * (len(at) + 16) * 2.0 ** -24) * float(torch.nan_to_num(vv.abs()).max())
+        return out, bound
+
+
+def rand(shape, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(*shape, generator=g).to(DT[dtype]).cuda()
+
+
+def index(x, dtype=torch.int64):
+    return torch.tensor(x, dtype=dtype, device="cuda")
+
+
+# ------------------------------------------------------------ norm and rotation
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,Hq,Hk,D,rot,inter", [
+    (1, 1, 1, 1, 64, 64, False), (2, 7, 8, 8, 64, 64, False), (3, 5, 6, 2, 128, 128, False), (2, 9, 3, 1, 128, 64, True),
+    (1, 33, 5, 5, 64, 16, False), (4, 3, 12, 4, 128, 16, True), (2, 2, 2, 2, 64, 0, False), (70, 1, 32, 8, 128, 128, False)])
+def test_norm_and_rotation(dtype, B, n, Hq, Hk, D, rot, inter):
+    q, k = rand((B, n, Hq, D), dtype, 1), rand((B, n, Hk, D), dtype, 2)
+    gq, gk = 1 + 0.3 * rand((D,), "f32", 3), 1 + 0.3 * rand((D,), "f32", 4)
+    freqs = (10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) * 2 / max(rot, 1))).float().cuda() if rot else None
+    pos = index([(b * 1234567 + 17) * (10 ** (b % 4)) for b in range(B)])
+    a, b = carry4().qk_norm_rope(q, k, pos, freqs, gq, gk, eps=1e-5, interleaved=inter)
+    rel = 2.0 ** -8 if dtype == "bf16" else 0.0
+    for got, x, g in ((a, q, gq), (b, k, gk)):
+        want = turned(x, g, pos, freqs, 1e-5, inter)
+        # (a pair turned by an angle that is off by d moves by at most d times its length: 2^1/2 of the larger member)
+        off = 2.0 ** -53 * (pos.cpu().double() + n)[:, None, None, None] * 2 ** 0.5 if rot else 0.0
+        near(got, want, rel, (2.0 ** -18 + off) * want.abs().amax(-1, keepdim=True) * (1 + rel))
+
+
+def test_norm_edges():
+    """Rows of zeros, of huge and tiny values, without gains, in place, ragged, unaligned rows."""
+    q = rand((2, 5, 3, 64), "f32", 5)
+    q[0, 0, 0] = 0
+    q[0, 1, 1] *= 1e15
+    q[1, 2, 2] *= 1e-15
+    k = rand((2, 5, 1, 64), "f32", 6)
+    pos, freqs, lens = index([0, 3]), torch.linspace(0.1, 1, 32).cuda(), index([5, 2], torch.int32)
+    q0, k0 = q.clone(), k.clone()
+    m = carry4()
+    m.qk_norm_rope(q, k, pos, freqs, lens=lens, out=(q, k))
+    for got, x in ((q, q0), (k, k0)):
+        want = turned(x, None, pos, freqs, 1e-6, False)
+        want[1, 2:] = x[1, 2:].double().cpu()
+        near(got, want, 0.0, 2.0 ** -18 * want.abs().amax(-1, keepdim=True))
+    # rows that start at odd elements: same bits as aligned ones
+    buf = torch.zeros(2 * 5 * 4 * 64 + 1, device="cuda")
+    view = buf[1:].view(2, 5, 4, 64)
+    view[:, :, :3], view[:, :, 3:] = q0, k0
+    a, b = m.qk_norm_rope(view[:, :, :3], view[:, :, 3:], pos, freqs, lens=lens)
+    assert torch.equal(a[0], q[0]) and torch.equal(b[0], k[0]) and torch.equal(a[1, :2], q[1, :2])
+    assert not a[1, 2:].any() and not b[1, 2:].any()
+
+
+# --------------------------------------------------------------- stored values
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_stored_values_are_exact(dtype, D):
+    """Every border between codes and its neighbours, at several scales, and random rows."""
+    m = carry4()
+    rows = []
+    grid = [0, 0.5, 1, 1.5, 2, 3, 4, 6]
+    for e in (0, 5, -20, 100, -126):
+        vals = grid + [(a + b) / 2 for a, b in zip(grid, grid[1:])]
+        x = torch.tensor(vals, dtype=torch.float64)
+        x = torch.cat([x, x * (1 + 2.0 ** -7), x * (1 - 2.0 ** -8)]) * 2.0 ** e
+        x = torch.cat([x, -x])
+        x = x[x.abs() <= 6 * 2.0 ** e]
+        x = torch.nn.functional.pad(x, (0, -len(x) % 31)).view(-1, 31)
+        rows.append(torch.cat([x, torch.full((len(x), 1), 6 * 2.0 ** e)], 1))   # every group's largest is 6 2^e
+    flat = torch.cat(rows)
+    flat = torch.cat([flat, torch.randn(200, 32, generator=torch.Generator().manual_seed(0), dtype=torch.float64) *
+                      torch.logspace(-30, 30, 200, dtype=torch.float64)[:, None], torch.zeros(1, 32, dtype=torch.float64),
+                      torch.full((1, 32), 1e-45, dtype=torch.float64)])
+    flat = torch.nn.functional.pad(flat, (0, 0, 0, -len(flat) % (D // 32)))
+    k = flat.view(1, -1, 1, D).to(DT[dtype]).cuda()
+    v = -k.flip(1)
+    n = k.shape[1]
+    c = m.Carry4(1, 1, D, sinks=3, ring=n)
+    c.append(k, v, index([0]))
+    for out in (torch.float32, torch.bfloat16):
+        a, b = c.read(index([0]), n, dtype=out)
+        # (bf16 and fp32 hold the smallest codes as subnormals; the conversion keeps them)
+        assert same(a, held(k)) and same(b, held(v))
+
+
+def test_stored_nan_and_infinity():
+    m = carry4()
+    k = rand((1, 4, 2, 64), "f32", 7)
+    v = k.clone()
+    k[0, 1, 0, 3], k[0, 2, 1, 40], v[0, 3, 1, 63] = math.nan, math.inf, -math.inf
+    c = m.Carry4(1, 2, 64, sinks=0, ring=4)
+    c.append(k, v, index([0]))
+    a, b = c.read(index([0]), 4)
+    assert same(a, held(k)) and same(b, held(v))
+    assert torch.isnan(a[0, 1, 0, :32]).all() and not torch.isnan(a[0, 1, 0, 32:]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_slots(dtype):
+    """First tokens and ring: what each position's slot holds after calls that
+    cross the border, wrap, exceed the ring, and leave entries out."""
+    m = carry4()
+    B, H, D, S, R = 4, 2, 64, 5, 7
+    c = m.Carry4(B, H, D, sinks=S, ring=R)
+    c.memory.fill_(255)
+    keep = index([5, 0, 3, 5], torch.int32)
+    model = Model(B, H, D)
+    far = 2 ** 40 + 11
+    pos = [0, 0, 0, far]
+    for step, (n, lens) in enumerate([(4, [4, 2, 4, 4]), (6, [6, 0, 1, 6]), (20, [20, 20, 3, 0]), (1, [1, 1, 1, 1])]):
+        k, v = rand((B, n, H, D), dtype, 10 + step), rand((B, n, H, D), dtype, 20 + step)
+        c.append(k, v, index(pos), lens=index(lens, torch.int32), sinks=keep)
+        model.append(k, v, pos, lens)
+        pos = [p + x for p, x in zip(pos, lens)]
+        for b in range(B):
+            s = int(keep[b])
+            want = [p for p in model.kv[b][0] if p < s or p >= pos[b] - R]
+            for p in want:
+                at = index([p if x == b else -1 for x in range(B)])
+                a, w = c.read(at, 1, lens=index([1] * B, torch.int32), sinks=keep)
+                assert same(a[b, 0], model.kv[b][0][p]) and same(w[b, 0], model.kv[b][1][p]), (step, b, p)
+                assert not a[:b].any() and not a[b + 1:].any()   # a negative position: no tokens
+
+
+def test_append_writes_its_slots_only():
+    m = carry4()
+    c = m.Carry4(2, 3, 128, sinks=2, ring=9)
+    c.memory.copy_(torch.randint(0, 256, c.memory.shape, generator=torch.Generator().manual_seed(1), dtype=torch.uint8))
+    before = c.memory.cpu()
+    k = rand((2, 3, 3, 128), "bf16", 3)
+    c.append(k, k, index([6, -1]))
+    after = c.memory.cpu()
+    N, region = 11, c.bytes // 6
+    wrote = {2 + (p - 2) % 9 for p in (6, 7, 8)}
+    changed = torch.zeros(c.bytes, dtype=torch.bool)
+    for h in range(3):   # entry 0 only
+        for s in wrote:
+            for kv in range(2):
+                a = h * region + (kv * N + s) * 64
+                changed[a:a + 64] = True
+                a = h * region + N * 128 + (kv * N + s) * 4
+                changed[a:a + 4] = True
+    assert torch.equal(after[~changed], before[~changed])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_rotated(D):
+    """The one-pass form: queries as qk_norm_rope gives them, keys stored from
+    their unrounded values.  In fp32 the separate calls give the same bits; in
+    bf16 a stored key is a code next to the 64-bit key's rounding."""
+    m = carry4()
+    B, n, Hq, H = 3, 6, 4, 2
+    pos, lens, freqs = index([0, 100, 7]), index([6, 2, 0], torch.int32), torch.linspace(1, 0.001, D // 2).cuda()
+    gq, gk = 1 + 0.3 * rand((D,), "f32", 3), 1 + 0.3 * rand((D,), "f32", 4)
+    for dtype in ("f32", "bf16"):
+        x = rand((B, n, Hq + 2 * H, D), dtype, 9)
+        q, k, v = x[:, :, :Hq], x[:, :, Hq:Hq + H], x[:, :, Hq + H:]
+        a, b = m.Carry4(B, H, D, sinks=2, ring=8), m.Carry4(B, H, D, sinks=2, ring=8)
+        qo, ko = m.qk_norm_rope(q, k, pos, freqs, gq, gk, lens=lens)
+        a.append(ko, v, pos, lens=lens)
+        got = b.append_rotated(q, k, v, pos, freqs, gq, gk, lens=lens)
+        assert torch.equal(got, qo)
+        (k1, v1), (k2, v2) = a.read(pos, n, lens=lens), b.read(pos, n, lens=lens)
+        assert torch.equal(v1, v2)
+        if dtype == "f32":
+            assert torch.equal(k1, k2)
+        want = turned(k, gk, pos, freqs, 1e-6, False)
+        for i in range(B):
+            w = want[i, :int(lens[i])]
+            top = w.unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True)
+            # the scale's power of two is at most a third of the largest magnitude, half a step
+            # one power of two at most (and the fp32 part's error)
+            near(k2[i, :int(lens[i])].unflatten(-1, (-1, 32)), w.unflatten(-1, (-1, 32)), 0.0, top / 3 * (1 + 2.0 ** -10))
+
+
+# ------------------------------------------------------------------- attention
+
+SHAPES = [
+    # B, n, Hq, H, D, sinks, window, causal, positions
+    (1, 1, 1, 1, 64, 0, 1, True, [0]),
+    (1, 1, 1, 1, 64, 0, 5, True, [3]),
+    (2, 1, 8, 2, 128, 4, 37, True, [0, 500]),
+    (3, 1, 16, 1, 64, 3, 300, True, [299, 2, 10 ** 9]),
+    (1, 1, 32, 1, 128, 0, 70, True, [69]),
+    (2, 1, 3, 3, 64, 302, 156, True, [302, 1000]),
+    (2, 5, 4, 2, 64, 2, 3, True, [0, 40]),
+    (2, 17, 2, 2, 128, 0, 16, True, [5, 16]),
+    (1, 33, 6, 2, 64, 9, 31, True, [4]),
+    (2, 56, 2, 2, 64, 302, 100, False, [302, 452]),
+    (2, 13, 6, 3, 64, 20, 16, False, [20, 1000]),
+    (1, 70, 1, 1, 128, 0, 0, False, [0]),
+    (3, 1, 2, 2, 128, 1, 0, False, [1, 0, 7]),
+    (1, 130, 4, 2, 128, 7, 64, True, [0]),
+    (1, 90, 8, 1, 64, 0, 200, True, [60]),
+    (17, 3, 4, 4, 64, 5, 40, True, [37 * b for b in range(17)]),
+]
+
+
+def turn(m, shape, dtype, seed, ragged=False, before=None):
+    """A carry that has stored a turn up to pos, with the call's own tokens; and its model."""
+    B, n, Hq, H, D, S, w, causal, pos = shape
+    ring = w + n + seed % 3
+    c, model = m.Carry4(B, H, D, sinks=S, ring=ring), Model(B, H, D)
+    c.memory.fill_(255)   # every slot that is not written is NaN
+    lens = [n] * B if not ragged else [(n * (b + 2) // 3) % (n + 1) for b in range(B)]
+    start = [max(0, p - ring) for p in pos]
+    if S:
+        some = [min(S, p) for p in pos]
+        if max(some):
+            k, v = rand((B, max(some), H, D), dtype, seed + 1), rand((B, max(some), H, D), dtype, seed + 2)
+            li = index(some, torch.int32)
+            c.append(k, v, index([0] * B), lens=li)
+            model.append(k, v, [0] * B, some)
+    start = [max(min(S, p), x) for p, x in zip(pos, start)]
+    some = [p - x for p, x in zip(pos, start)]
+    if max(some):
+        k, v = rand((B, max(some), H, D), dtype, seed + 3), rand((B, max(some), H, D), dtype, seed + 4)
+        c.append(k, v, index(start), lens=index(some, torch.int32))
+        model.append(k, v, start, some)
+    k, v = rand((B, n, H, D), dtype, seed + 5), rand((B, n, H, D), dtype, seed + 6)
+    if before:
+        before(k, v)
+    c.append(k, v, index(pos), lens=index(lens, torch.int32))
+    model.append(k, v, pos, lens)
+    return c, model, lens
+
+
+def check(got, model, q, shape, dtype, lens, scale=None, sinks=None):
+    B, n, Hq, H, D, S, w, causal, pos = shape
+    want, bound = model.attend(q, pos, w, lens, sinks or [S] * B, causal, scale)
+    rel = 0.0
+    if dtype == "bf16":
+        top = max([float(torch.nan_to_num(torch.stack(list(t[1].values())).abs()).max()) for t in model.kv if t[1]], default=0.0)
+        rel, bound = 2.0 ** -8, bound + 2.0 ** -8 * top * (1 + 2.0 ** -8)
+    for b in range(B):
+        m = lens[b]
+        near(got[b, :m], want[b, :m], rel, bound[b, :m] * (1 + rel))
+
+
+@pytest.mark.parametrize("ragged", [False, True], ids=["full", "ragged"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=[f"B{s[0]}n{s[1]}q{s[2]}h{s[3]}d{s[4]}s{s[5]}w{s[6]}{'c' if s[7] else 'b'}" for s in SHAPES])
+def test_attend(shape, dtype, ragged):
+    B, n, Hq, H, D, S, w, causal, pos = shape
+    m = carry4()
+    c, model, lens = turn(m, shape, dtype, 31, ragged)
+    q = rand((B, n, Hq, D), dtype, 77)
+    out = torch.full_like(q, 7.0)
+    c.attend(q, index(pos), w, lens=index(lens, torch.int32), causal=causal, out=out)
+    check(out, model, q, shape, dtype, lens)
+    for b in range(B):
+        assert (out[b, lens[b]:] == 7.0).all()   # rows behind an entry's last token are left as they were
+    again = c.attend(q, index(pos), w, lens=index(lens, torch.int32), causal=causal)
+    for b in range(B):
+        assert torch.equal(again[b, :lens[b]], out[b, :lens[b]])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attend_masked_nan_and_infinity(dtype):
+    """NaN among the keys and values of tokens that some rows see and others do
+    not: exactly the rows that see them are touched, a NaN value only in its own
+    32 dimensions."""
+    shape = (2, 24, 4, 2, 64, 0, 6, True, [0, 30])
+    m = carry4()
+
+    def plant(k, v):
+        k[0, 10, 0, 5] = math.nan
+        v[0, 20, 1, 40] = math.inf
+        v[1, 0, 0, 0] = math.nan
+        k[1, 22, 1, 33] = -math.inf
+    c, model, lens = turn(m, shape, dtype, 50, before=plant)
+    q = rand((2, 24, 4, 64), dtype, 78)
+    got = c.attend(q, index(shape[8]), shape[6])
+    check(got, model, q, shape, dtype, lens)
+    bad = torch.isnan(got).cpu()
+    assert bad[0, 10:16, :2].all() and not bad[0, :10].any() and not bad[0, 16:20].any()
+    assert bad[0, 20:24, 2:, 32:].all() and not bad[0, 20:24, 2:, :32].any() and not bad[0, 20:24, :2].any()
+
+
+def test_attend_scores_far_apart():
+    """One key whose score is far above the others', first, last and in the middle; a scale of zero and a negative one."""
+    m = carry4()
+    for at in (0, 33, 99):
+        shape = (1, 1, 2, 1, 64, 0, 100, True, [99])
+        c, model, lens = turn(m, shape, "f32", 60)
+        k = rand((1, 1, 1, 64), "f32", 61) * 40
+        v = rand((1, 1, 1, 64), "f32", 62)
+        c.append(k, v, index([at]))
+        model.append(k, v, [at])
+        q = k.expand(1, 1, 2, 64).contiguous()
+        check(c.attend(q, index([99]), 100), model, q, shape, "f32", lens)
+        for scale in (0.0, -0.01):
+            check(c.attend(q, index([99]), 100, scale=scale), model, q, shape, "f32", lens, scale)
+
+
+def test_attend_entry_sinks():
+    """Entries that keep different numbers of first tokens."""
+    m = carry4()
+    B, n, Hq, H, D, S, w = 3, 4, 2, 2, 64, 6, 5
+    keep, pos = [0, 6, 2], [20, 20, 20]
+    c, model = m.Carry4(B, H, D, sinks=S, ring=w + n), Model(B, H, D)
+    c.memory.fill_(255)
+    for p in range(0, 24, 4):
+        k, v = rand((B, 4, H, D), "bf16", p), rand((B, 4, H, D), "bf16", p + 100)
+        c.append(k, v, index([p] * B), sinks=index(keep, torch.int32))
+        model.append(k, v, [p] * B)
+    q = rand((B, n, Hq, D), "bf16", 5)
+    for causal in (True, False):
+        shape = (B, n, Hq, H, D, S, w, causal, pos)
+        got = c.attend(q, index(pos), w, sinks=index(keep, torch.int32), causal=causal)
+        check(got, model, q, shape, "bf16", [n] * B, sinks=keep)
+
+
+def test_attend_window_past_the_ring():
+    """A call longer than the ring leaves room for: its early queries see what the ring still holds."""
+    m = carry4()
+    B, n, Hq, H, D, S, w = 2, 9, 2, 1, 64, 4, 6
+    c, model = m.Carry4(B, H, D, sinks=S, ring=11), Model(B, H, D)
+    pos = [0, 3]
+    k, v = rand((B, 7, H, D), "f32", 1), rand((B, 7, H, D), "f32", 2)
+    c.append(k, v, index([0, 0]))
+    model.append(k, v, [0, 0])
+    pos = [7, 7]
+    k, v, q = rand((B, n, H, D), "f32", 3), rand((B, n, H, D), "f32", 4), rand((B, n, Hq, D), "f32", 5)
+    c.append(k, v, index(pos))
+    model.append(k, v, pos)
+    for kv in model.kv:   # positions 4 .. 15 were stored after the first tokens; the ring holds 5 .. 15
+        for t in kv:
+            del t[4]
+    check(c.attend(q, index(pos), w), model, q, (B, n, Hq, H, D, S, w, True, pos), "f32", [n] * B)
+
+
+def test_attend_rows_of_other_layouts():
+    """Queries and results as strided views, heads before tokens, unaligned rows: the same bits."""
+    shape = (2, 9, 4, 2, 64, 3, 20, True, [0, 50])
+    m = carry4()
+    c, model, lens = turn(m, shape, "bf16", 70)
+    q = rand((2, 9, 4, 64), "bf16", 71)
+    pos = index(shape[8])
+    want = c.attend(q, pos, 20)
+    check(want, model, q, shape, "bf16", lens)
+    t = q.transpose(1, 2).contiguous().transpose(1, 2)
+    assert torch.equal(c.attend(t, pos, 20, out=torch.zeros(2, 4, 9, 64, dtype=q.dtype, device="cuda").transpose(1, 2)), want)
+    buf = torch.zeros(2 * 9 * 4 * 64 + 3, dtype=q.dtype, device="cuda")
+    view, res = buf[3:].view(2, 9, 4, 64), torch.zeros_like(buf)[1:-2].view(2, 9, 4, 64)
+    view.copy_(q)
+    assert torch.equal(c.attend(view, pos, 20, out=res), want)
+
+
+def test_attend_does_not_depend_on_the_other_entries():
+    shape = (5, 3, 4, 2, 128, 2, 40, True, [0, 10, 41, 300, 5])
+    m = carry4()
+    c, _, _ = turn(m, shape, "bf16", 80)
+    q, pos = rand((5, 3, 4, 128), "bf16", 81), index(shape[8])
+    want = c.attend(q, pos, 40)
+    q2, p2 = q.clone(), pos.clone()
+    q2[:3], p2[:3] = 9.0, -1
+    assert torch.equal(c.attend(q2, p2, 40, out=torch.zeros_like(q))[3:], want[3:])
+
+
+def test_captured_step_and_streams():
+    """A serving step (norm and rotation into the carry, attention) captured
+    once and replayed with other positions and inputs, on a stream of its own,
+    against the same calls made eagerly on another carry, with eager work and
+    synchronisations between; two graphs captured from one pool."""
+    m = carry4()
+    B, n, Hq, H, D, S, w = 2, 1, 4, 2, 64, 3, 40
+    freqs = torch.linspace(1, 0.01, 32).cuda()
+    a, b = (m.Carry4(B, H, D, sinks=S, ring=w + n) for _ in range(2))
+    x, pos = torch.empty(B, n, Hq + 2 * H, D, device="cuda", dtype=torch.bfloat16), index([0, 0])
+
+    def step(c, x, pos):
+        q = c.append_rotated(x[:, :, :Hq], x[:, :, Hq:Hq + H], x[:, :, Hq + H:], pos, freqs)
+        return c.attend(q, pos, w)
+
+    x.copy_(rand(x.shape, "bf16", 0))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a, x, pos)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g, pool=graphs[0].pool() if outs else None):
+            outs.append(step(a, x, pos))
+    for t in range(60):
+        x.copy_(rand(x.shape, "bf16", 1000 + t))
+        pos.copy_(index([t, t]))
+        graphs[t % 2].replay()
+        got = outs[t % 2].clone()
+        want = step(b, x.clone(), pos.clone())
+        assert torch.equal(got, want), t
+        if t % 7 == 0:
+            torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_turn(dtype):
+    """A turn as a streaming model runs it: a prompt kept as first tokens, then
+    single tokens and short calls past the ring's end, every result against the
+    64-bit model of what the carry holds."""
+    m = carry4()
+    B, Hq, H, D, S, w = 2, 4, 2, 64, 10, 12
+    c, model = m.Carry4(B, H, D, sinks=S, ring=w + 6), Model(B, H, D)
+    freqs, g = torch.linspace(1, 0.01, 32).cuda(), 1 + 0.2 * rand((D,), "f32", 1)
+    pos = [0, 0]
+    for t, (n, lens) in enumerate([(10, [10, 8]), (1, [1, 1]), (6, [6, 3]), (1, [0, 1]), (5, [5, 5]), (6, [6, 6]), (1, [1, 1])]):
+        x = rand((B, n, Hq + 2 * H, D), dtype, 100 + t)
+        li, pi = index(lens, torch.int32), index(pos)
+        q, k = m.qk_norm_rope(x[:, :, :Hq], x[:, :, Hq:Hq + H], pi, freqs, g, g, lens=li)
+        v = x[:, :, Hq + H:]
+        c.append(k, v, pi, lens=li)
+        model.append(k, v, pos, lens)
+        got = c.attend(q, pi, w, lens=li)
+        check(got, model, q, (B, n, Hq, H, D, S, w, True, pos), dtype, lens)
+        pos = [p + x for p, x in zip(pos, lens)]
+
+
+def test_refusals_on_the_gpu():
+    m = carry4()
+    c = m.Carry4(2, 2, 64, sinks=1, ring=8)
+    k, pos = rand((2, 3, 2, 64), "bf16", 1), index([0, 0])
+    c.append(k, k, pos)
+    for call in (lambda: c.append(k.half(), k.half(), pos), lambda: c.append(k, k[:, :2], pos), lambda: c.append(k[:1], k[:1], pos),
+                 lambda: c.append(k, k.float(), pos), lambda: c.append(k, k, pos.int()), lambda: c.append(k, k, pos.cpu()),
+                 lambda: c.append(k, k, pos, lens=pos), lambda: c.append(k.cpu(), k.cpu(), pos),
+                 lambda: c.append(k.transpose(2, 3), k.transpose(2, 3), pos), lambda: c.append(k, k, None),
+                 lambda: c.attend(k, pos, 8), lambda: c.attend(k, pos, 0), lambda: c.attend(k[:, :, :1], pos, 2),
+                 lambda: c.attend(k, pos, 7, causal=False), lambda: c.attend(k, pos, 2, scale=math.inf),
+                 lambda: m.Carry4(2, 2, 96, sinks=0, ring=8), lambda: m.Carry4(2, 2, 64, sinks=0, ring=0),
+                 lambda: m.qk_norm_rope(k, k, pos, torch.ones(4, device="cuda")),
+                 lambda: m.qk_norm_rope(k, k, pos, torch.ones(40, device="cuda")),
+                 lambda: m.qk_norm_rope(k, k, pos, None, eps=-1.0)):
+        with pytest.raises(DcError):
+            call()
+    assert c.attend(k[:, :0], pos, 4).shape == (2, 0, 2, 64)   # a call of no tokens
+    c.append(k[:, :0], k[:, :0], pos)
