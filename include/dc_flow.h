@@ -81,7 +81,7 @@ typedef struct dc_flow_stats {
 /* Device time of one kernel role in one call (dc_flow_profile). */
 typedef struct dc_flow_kernel_stat {
     char name[48];            /* role: "assemble", "gemm:in", "gemm:qkv", "attn", "gemm:o",
-                                 "gemm:fc1", "gemm:fc2", "gemm:out", "euler"                           */
+                                 "heads" (with options), "gemm:fc1", "gemm:fc2", "gemm:out", "euler"                           */
     int32_t launches;         /* launches of this role per call                                      */
     int32_t mfma;             /* 1: the role is a matrix-core contraction                            */
     double us;                /* device time per call, summed over its launches (HIP events)        */
@@ -107,6 +107,37 @@ int64_t dc_flow_blob_floats(const dc_flow_cfg* cfg);
  * turn yet.  Errors: DC_EINVAL (bad cfg or blob size), DC_EVERSION,
  * DC_ENOMEM, DC_EDEVICE. */
 dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flow_cfg* cfg, dc_flow_state** out);
+
+/* Options of dc_flow_init_opt.
+ *
+ * qk_norm: every block normalises its queries and keys per head (RMS norm,
+ * eps qk_eps, with a gain per dimension) and rotates the first rope_dims of
+ * a head's 64 dimensions by the frame's position since the turn start: pair j
+ * is dimensions (j, j + rope_dims / 2), its frequency rope_base^(-2 j /
+ * rope_dims) radians a frame, rounded to float32 (dc_qk_norm_rope below).  The
+ * blob then holds, behind the tensors of dc_flow_blob_floats, the gains
+ * [depth][2][64] (queries, keys).  The carry holds keys as they are attended
+ * to, normalised and rotated.
+ *
+ * carry_bits 4: the stacked carry is held in 4 bits (dc_carry4 below: E2M1
+ * with one scale for 32 values): 34 bytes per head, frame and key or value
+ * instead of 128 (bf16) or 256.  A call's own frames are stored first and
+ * attended to as they are held. */
+#define DC_FLOW_OPT_VERSION 1
+typedef struct dc_flow_opt {
+    int32_t abi_version;      /* DC_FLOW_OPT_VERSION                                         */
+    int32_t carry_bits;       /* 0: the carry in the operand type; 4                         */
+    int32_t qk_norm;          /* 0 or 1                                                      */
+    int32_t rope_dims;        /* 0 (norm only) .. 64, a multiple of 16; 0 without qk_norm    */
+    float rope_base;          /* > 0, finite, with rope_dims                                 */
+    float qk_eps;             /* >= 0, finite, with qk_norm                                  */
+} dc_flow_opt;
+
+/* dc_flow_blob_floats and dc_flow_init with options (NULL: none, the same as
+ * without).  Errors as theirs; DC_EVERSION also for opt's. */
+int64_t dc_flow_blob_floats_opt(const dc_flow_cfg* cfg, const dc_flow_opt* opt);
+dc_status dc_flow_init_opt(const void* weights_blob, size_t blob_bytes, const dc_flow_cfg* cfg, const dc_flow_opt* opt,
+                           dc_flow_state** out);
 
 /* Start a turn of stream b: the prompt pass over `frames` frames (1 <=
  * frames <= f_prompt; mu and cond [frames][n_mel], spk [n_mel]) writes the

@@ -98,6 +98,11 @@ def _load():
         lib.ocf_blob_floats.restype = ctypes.c_long
         lib.ocf_open.argtypes = [FP, ctypes.c_int, F, ctypes.c_long, ctypes.c_uint64, ctypes.c_uint64]
         lib.ocf_open.restype = V
+        lib.ocf_open_opt.argtypes = [FP, ctypes.POINTER(_FlowOpt), ctypes.c_int, F, ctypes.c_long, ctypes.c_uint64,
+                                     ctypes.c_uint64]
+        lib.ocf_open_opt.restype = V
+        lib.ocf_qk.argtypes = [ctypes.c_int, D, D, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_int64]
+        lib.ocf_hold4.argtypes = [ctypes.c_int, D]
         lib.ocf_close.argtypes = [V]
         lib.ocf_prompt.argtypes = [V, ctypes.c_int, D, D, D, D]
         lib.ocf_prompt.restype = ctypes.c_int
@@ -128,6 +133,11 @@ class _FlowArch(ctypes.Structure):
         ("f_prompt", ctypes.c_int), ("f_retained", ctypes.c_int), ("f_chunk", ctypes.c_int),
         ("f_call", ctypes.c_int), ("cfg_rate", ctypes.c_double), ("temperature", ctypes.c_double),
     ]
+
+
+class _FlowOpt(ctypes.Structure):
+    _fields_ = [("carry_bits", ctypes.c_int), ("qk_norm", ctypes.c_int), ("rope_dims", ctypes.c_int),
+                ("rope_base", ctypes.c_double), ("qk_eps", ctypes.c_double)]
 
 
 def _p(a: np.ndarray, ct):
@@ -359,6 +369,20 @@ def attention(q, k, v) -> np.ndarray:
     return out
 
 
+def qk(x, gain, eps: float, rope_dims: int, base: float, position: int) -> np.ndarray:
+    """Norm and rotation of one head's row."""
+    x, gain = _f64(x).copy(), _f64(gain)
+    _load().ocf_qk(x.size, _p(x, ctypes.c_double), _p(gain, ctypes.c_double), eps, rope_dims, base, position)
+    return x
+
+
+def hold4(x) -> np.ndarray:
+    """The values that groups of 32 values are held as in 4 bits."""
+    x = _f64(x).copy()
+    _load().ocf_hold4(x.size, _p(x, ctypes.c_double))
+    return x
+
+
 def flow_noise(n_mel: int, temperature: float, seed: int, key: int, tau0: int, frames: int) -> np.ndarray:
     out = np.empty((frames, n_mel), dtype=np.float64)
     _load().ocf_noise(n_mel, temperature, seed, key, tau0, frames, _p(out, ctypes.c_double))
@@ -368,7 +392,8 @@ def flow_noise(n_mel: int, temperature: float, seed: int, key: int, tau0: int, f
 class FlowStream:
     """One stream of the flow decoder in fp64: prompt(), then chunk() calls.
 
-    dtype "bf16" rounds the per-step Linear weights to bfloat16 first.
+    dtype "bf16" rounds the per-step Linear weights to bfloat16 first.  The
+    options of arch: carry_bits, qk_norm, rope_dims, rope_base, qk_eps.
     """
 
     def __init__(self, arch: dict, dtype: str, blob: np.ndarray, seed: int = 0, key: int = 0):
@@ -376,8 +401,10 @@ class FlowStream:
         self._a = flow_arch_struct(arch)
         self._blob = np.ascontiguousarray(blob, dtype=np.float32)
         self._lib = _load()
-        self._h = self._lib.ocf_open(ctypes.byref(self._a), 1 if dtype == "bf16" else 0,
-                                     _p(self._blob, ctypes.c_float), self._blob.size, seed, key)
+        opt = _FlowOpt(arch.get("carry_bits", 0), arch.get("qk_norm", 0), arch.get("rope_dims", 0),
+                       arch.get("rope_base", 10000.0), arch.get("qk_eps", 1e-6))
+        self._h = self._lib.ocf_open_opt(ctypes.byref(self._a), ctypes.byref(opt), 1 if dtype == "bf16" else 0,
+                                         _p(self._blob, ctypes.c_float), self._blob.size, seed, key)
         if not self._h:
             raise ValueError("bad flow architecture or blob size")
 

@@ -45,6 +45,12 @@
  *   - noise: x_0 of the frame with index tau since the turn start (prompt
  *     frames first), mel pair j, is temperature * Box-Muller of the first two
  *     words of Philox4x64-10 at counter (tau, j, 2, 0), key (seed, stream key);
+ *   - options (off by default): per-head RMS norm of queries and keys with a
+ *     gain per dimension, then a rotation of pairs (j, j + rope_dims / 2) by
+ *     position * f_j, f_j = rope_base^(-2 j / rope_dims) rounded to float32;
+ *     a carry in 4 bits: a call's keys and values are replaced by the values
+ *     that 32-element groups of E2M1 elements with a power-of-two scale hold,
+ *     before any query reads them;
  *   - with bf16 parameters the weights of the estimator's Linear layers that
  *     run per solver step (in, qkv, o, fc1, fc2, out) are rounded to bfloat16;
  *     the arithmetic stays fp64.
@@ -68,6 +74,11 @@ typedef struct {
     double cfg_rate, temperature;
 } ocf_arch;
 
+typedef struct {
+    int carry_bits, qk_norm, rope_dims;   /* all 0: none */
+    double rope_base, qk_eps;
+} ocf_opt;
+
 /* y[r][o] = b[o] + sum_i W[o][i] x[r][i], W in PyTorch layout [out][in]. */
 typedef struct {
     const double* W;
@@ -77,6 +88,8 @@ typedef struct {
 
 typedef struct {
     ocf_arch a;
+    ocf_opt opt;
+    const double* gains;       /* [depth][2][dim / heads] with qk_norm */
     double* w;                 /* the blob in fp64 */
     ocf_lin t1, t2, in, fada, out;
     ocf_lin *ada, *qkv, *o, *fc1, *fc2;
@@ -165,6 +178,53 @@ void ocf_attention(int nq, int nk, int hd, const double* q, const double* k, con
     free(s);
 }
 
+/*
+ * Norm and rotation of one head's row x[hd] at a position: x <- x / sqrt(mean
+ * x^2 + eps) * gain, then pair (j, half + j), j < half = rope_dims / 2, turns by
+ * position * float32(base^(-2 j / rope_dims)).
+ */
+void ocf_qk(int hd, double* x, const double* gain, double eps, int rope_dims, double base, int64_t position)
+{
+    double ss = 0.0;
+    for (int i = 0; i < hd; i++) ss += x[i] * x[i];
+    const double inv = 1.0 / sqrt(ss / hd + eps);
+    for (int i = 0; i < hd; i++) x[i] = x[i] * inv * gain[i];
+    const int half = rope_dims / 2;
+    for (int j = 0; j < half; j++) {
+        const double f = (double)(float)pow(base, -2.0 * j / rope_dims);
+        const double c = cos((double)position * f), sn = sin((double)position * f);
+        const double a = x[j], b = x[half + j];
+        x[j] = a * c - b * sn;
+        x[half + j] = a * sn + b * c;
+    }
+}
+
+/*
+ * The values that n values (n a multiple of 32) are held as in 4 bits: per
+ * group of 32, scale 2^e with the least e in [-126, 126] for which 6 * 2^e is at
+ * least the largest magnitude; every value the nearest of +-{0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6} * 2^e, ties to the even place in that list.
+ */
+void ocf_hold4(int n, double* x)
+{
+    static const double grid[8] = {0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0};
+    for (int g = 0; g < n; g += 32) {
+        double top = 0.0;
+        for (int i = 0; i < 32; i++) top = fmax(top, fabs(x[g + i]));
+        int e = -126;
+        while (e < 126 && ldexp(6.0, e) < top) e++;
+        for (int i = 0; i < 32; i++) {
+            const double a = ldexp(fabs(x[g + i]), -e);
+            int best = 0;
+            for (int c = 1; c < 8; c++) {
+                const double d = fabs(a - grid[c]), b = fabs(a - grid[best]);
+                if (d < b || (d == b && c % 2 == 0)) best = c;
+            }
+            x[g + i] = copysign(ldexp(grid[best], e), x[g + i]);
+        }
+    }
+}
+
 /* The cosine time grid t_i = 1 - cos(pi/2 * i / n), i = 0 .. n. */
 void ocf_times(int n, double* t)
 {
@@ -232,11 +292,17 @@ static int valid_arch(const ocf_arch* a)
 
 /* Open a stream: weights, the time grid and the per-step modulations (they depend
  * only on t_i).  Returns NULL on a bad architecture or blob size. */
-ocf_stream* ocf_open(const ocf_arch* a, int bf16, const float* blob, long blob_n, uint64_t seed, uint64_t key)
+ocf_stream* ocf_open_opt(const ocf_arch* a, const ocf_opt* opt, int bf16, const float* blob, long blob_n, uint64_t seed,
+                         uint64_t key)
 {
-    if (!valid_arch(a) || blob_n != ocf_blob_floats(a)) return NULL;
+    if (!valid_arch(a)) return NULL;
+    const long gains = opt && opt->qk_norm ? (long)a->depth * 2 * (a->dim / a->heads) : 0;
+    if (blob_n != ocf_blob_floats(a) + gains) return NULL;
+    if (opt && (opt->rope_dims % 2 != 0 || opt->rope_dims > a->dim / a->heads)) return NULL;
+    if (opt && opt->carry_bits && (opt->carry_bits != 4 || a->dim / a->heads % 32 != 0)) return NULL;
     ocf_stream* s = calloc(1, sizeof(ocf_stream));
     s->a = *a;
+    if (opt) s->opt = *opt;
     s->seed = seed;
     s->key = key;
     s->w = malloc(sizeof(double) * (size_t)blob_n);
@@ -260,6 +326,7 @@ ocf_stream* ocf_open(const ocf_arch* a, int bf16, const float* blob, long blob_n
     }
     s->fada = take_lin(&cur, 2 * D, D);
     s->out = take_lin(&cur, M, D);
+    s->gains = cur;
     if (bf16) {
         round_lin(&s->in);
         round_lin(&s->out);
@@ -294,6 +361,11 @@ ocf_stream* ocf_open(const ocf_arch* a, int bf16, const float* blob, long blob_n
     s->V = calloc((size_t)NS * NL * 2 * s->cap * D, sizeof(double));
     s->spk = calloc(M, sizeof(double));
     return s;
+}
+
+ocf_stream* ocf_open(const ocf_arch* a, int bf16, const float* blob, long blob_n, uint64_t seed, uint64_t key)
+{
+    return ocf_open_opt(a, NULL, bf16, blob, blob_n, seed, key);
 }
 
 void ocf_close(ocf_stream* s)
@@ -382,6 +454,19 @@ static void solve(ocf_stream* s, int n, const double* mu, const double* cond, in
             const double *shift2 = md + 3 * D, *scale2 = md + 4 * D, *gate2 = md + 5 * D;
             for (int r = 0; r < R; r++) ocf_lnmod(D, h + (size_t)r * D, shift1, scale1, act + (size_t)r * D);
             linear(&s->qkv[l], R, act, qkv);
+            for (int r = 0; r < R; r++)
+                for (int hh = 0; hh < a->heads; hh++) {
+                    double* q = qkv + (size_t)r * 3 * D + hh * HD;
+                    const double* gain = s->gains + (size_t)l * 2 * HD;
+                    if (s->opt.qk_norm) {
+                        ocf_qk(HD, q, gain, s->opt.qk_eps, s->opt.rope_dims, s->opt.rope_base, s->pos + r % n);
+                        ocf_qk(HD, q + D, gain + HD, s->opt.qk_eps, s->opt.rope_dims, s->opt.rope_base, s->pos + r % n);
+                    }
+                    if (s->opt.carry_bits == 4) {
+                        ocf_hold4(HD, q + D);
+                        ocf_hold4(HD, q + 2 * D);
+                    }
+                }
             for (int c = 0; c < 2; c++) {
                 /* keys and values: the carry of (step i, block l, branch c), then the call's own frames */
                 const double* CK = carry_K(s, i, l, c);

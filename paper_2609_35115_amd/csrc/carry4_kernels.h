@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
         const int h = kind == 0 ? j : kind == 1 ? j - p.q.heads : j - p.q.heads - p.k.heads;
         const HeadRows& in = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
         float x[8] = {};
-        if (on) load8<BF16>(in.p, e * in.sb + i * in.st + h * in.sh + 8 * l, p.wide_in, x);
+        if (on) load8<BF16>(in.p, in.at(p.sp.div, e, i, h) + 8 * l, p.wide_in, x);
         if (p.norm && kind < 2) {
             float ss = 0.0f;
 #pragma unroll
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
         }
         if (kind == 0 || (kind == 1 && p.k_out.p)) {
             const HeadRows& o = kind == 0 ? p.q_out : p.k_out;
-            if (on) store8<OUT16>(o.p, e * o.sb + i * o.st + h * o.sh + 8 * l, p.wide_out, x);
+            if (on) store8<OUT16>(o.p, o.at(p.sp.div, e, i, h) + 8 * l, p.wide_out, x);
         } else {
             uint32_t top = 0;
 #pragma unroll
@@ -290,7 +290,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256) void read4_kernel(
     float x[8];
     decode8(w, s, x);
     const HeadRows& o = kv ? p.v : p.k;
-    store8<BF16>(o.p, e * o.sb + i * o.st + h * o.sh + 8 * l, p.wide, x);
+    store8<BF16>(o.p, o.at(p.sp.div, e, i, h) + 8 * l, p.wide, x);
 }
 
 hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
@@ -300,6 +300,35 @@ hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
     if (p.c.D == 64)
         return bf16 ? launch_with(read4_kernel<true, 64>, grid, block, st, p) : launch_with(read4_kernel<false, 64>, grid, block, st, p);
     return bf16 ? launch_with(read4_kernel<true, 128>, grid, block, st, p) : launch_with(read4_kernel<false, 128>, grid, block, st, p);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void carry4_gather_kernel(const Carry4 c, const Spans spans, int e, int kv, int f_chunk,
+                                                            int nh, int frames, float* out)
+{
+    constexpr int L = D / 8;
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / L;   // (frame, head)
+    const int l = (int)(u % L), f = (int)(row / c.heads), h = (int)(row % c.heads);
+    if (f >= frames) return;
+    const Span sp(spans, c, e);
+    const int64_t at = f < nh * f_chunk ? sp.pos - (int64_t)(f / f_chunk + 1) * f_chunk + f % f_chunk : f - nh * f_chunk;
+    int64_t slot = at < sp.sinks ? at : c.sinks + (at - sp.sinks) % c.ring;
+    slot = slot < 0 ? 0 : slot;
+    const int N = c.slots();
+    const uint8_t* reg = c.base + ((int64_t)e * c.heads + h) * c.region;
+    float x[8];
+    decode8(*(const uint32_t*)(reg + ((int64_t)kv * N + slot) * (D / 2) + 4 * l),
+            reg[(int64_t)N * D + ((int64_t)kv * N + slot) * (D / 32) + (l >> 2)], x);
+    store8<false>(out, row * D + 8 * l, 1, x);
+}
+
+hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv, int f_chunk, int nh, int frames,
+                                float* out, hipStream_t st)
+{
+    const unsigned blocks = (unsigned)(((int64_t)frames * c.heads * (c.D / 8) + 255) / 256);
+    if (c.D == 64) hipLaunchKernelGGL(carry4_gather_kernel<64>, dim3(blocks), dim3(256), 0, st, c, sp, e, kv, f_chunk, nh, frames, out);
+    else hipLaunchKernelGGL(carry4_gather_kernel<128>, dim3(blocks), dim3(256), 0, st, c, sp, e, kv, f_chunk, nh, frames, out);
+    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ attention
@@ -491,7 +520,7 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Params p)
     Planes<PL> qf[KS];
     {
         const int row = min(row0 + r, rows - 1), i = row / p.group, hq = h * p.group + row % p.group;
-        const int64_t at = e * p.q.sb + i * p.q.st + hq * p.q.sh + g * (D / 4);
+        const int64_t at = p.q.at(p.sp.div, e, i, hq) + g * (D / 4);
 #pragma unroll
         for (int c = 0; c < KS; c++) {
             float x[8];
@@ -637,7 +666,7 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Params p)
         if (p.splits == 1) {
             const int i = row / p.group, hq = h * p.group + row % p.group;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int64_t at = e * p.o.sb + i * p.o.st + hq * p.o.sh + d;
+            const int64_t at = p.o.at(p.sp.div, e, i, hq) + d;
             if (p.wide_out) {
                 store4<BF16>(p.o.p, at, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
             } else {
@@ -683,7 +712,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256) void attend4_join(
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int i = row / p.group, hq = h * p.group + row % p.group;
-    const int64_t at = e * p.o.sb + i * p.o.st + hq * p.o.sh + d;
+    const int64_t at = p.o.at(p.sp.div, e, i, hq) + d;
     if (p.wide_out) {
         store4<BF16>(p.o.p, at, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
     } else {

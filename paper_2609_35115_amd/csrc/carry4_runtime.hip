@@ -83,7 +83,7 @@ dc_status check_rows(const dc_head_rows* r, int64_t n, int32_t dtype, const char
     return DC_OK;
 }
 
-HeadRows rows(const dc_head_rows* r) { return HeadRows{r->data, r->stride_b, r->stride_t, r->stride_h, r->heads}; }
+HeadRows rows(const dc_head_rows* r) { return HeadRows{r->data, r->stride_b, r->stride_t, r->stride_h, r->heads, 0, nullptr, 0, 0}; }
 
 bool wide(const dc_head_rows* r, int32_t dtype)
 {

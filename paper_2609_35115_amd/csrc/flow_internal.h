@@ -169,12 +169,22 @@ struct Spans {
     int div, n, sinks_all;
 };
 
-// Rows of heads: head h of token i of entry e at p + e sb + i st + h sh, in
-// elements; a row's D elements are consecutive.
+// Rows of heads: head h of token i of entry e = b div + c at p + b sb + c sc +
+// (i + row0 + slot[b] row_step) st + h sh, in elements (no slot term where slot
+// is null); a row's D elements are consecutive.
 struct HeadRows {
     void* p;
     int64_t sb, st, sh;
     int heads;
+    int64_t sc;
+    const int* slot;
+    int row0, row_step;
+    __device__ __forceinline__ int64_t at(int div, int e, int i, int h) const
+    {
+        const int b = e / div;
+        const int64_t row = (int64_t)i + row0 + (slot ? (int64_t)slot[b] * row_step : 0);
+        return b * sb + (e % div) * sc + row * st + h * sh;
+    }
 };
 
 // Per-head norm and position rotation, the store into the carry, or both:
@@ -214,6 +224,11 @@ struct Read4Params {
     int entries, wide;       // wide: every row is 16-byte aligned
 };
 
+// The carry of (entry e, kv) in Eq. carry's logical order, widened to fp32: the
+// nh newest chunks of f_chunk tokens before pos, newest first, then the first
+// tokens; out [frames][heads * D].
+hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv, int f_chunk, int nh, int frames,
+                                float* out, hipStream_t st);
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st);
 // Key splits of an attention call, and the bytes of workspace they take.
 int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes);

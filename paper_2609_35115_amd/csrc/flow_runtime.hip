@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <chrono>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -29,10 +30,11 @@ struct BlobMap {
     std::vector<int64_t> ada, qkvW, qkvb, oW, ob, fc1W, fc1b, fc2W, fc2b;
     int64_t block_stride;
     int64_t fadaW, outW, outb;
+    int64_t gains;   // [depth][2][64] with qk_norm
     int64_t total;
 };
 
-BlobMap blob_map(const dc_flow_cfg& c)
+BlobMap blob_map(const dc_flow_cfg& c, const dc_flow_opt& opt)
 {
     const int64_t D = c.dim, M = c.n_mel, T = c.t_dim, H = c.mlp;
     BlobMap m{};
@@ -66,6 +68,7 @@ BlobMap blob_map(const dc_flow_cfg& c)
     take(2 * D);
     m.outW = take(M * D);
     m.outb = take(M);
+    m.gains = opt.qk_norm ? take((int64_t)c.depth * 2 * 64) : o;
     m.total = o;
     return m;
 }
@@ -90,10 +93,22 @@ std::string validate(const dc_flow_cfg* c)
     return "";
 }
 
+std::string validate_opt(const dc_flow_opt& o)
+{
+    if (o.carry_bits != 0 && o.carry_bits != 4) return "carry_bits must be 0 or 4";
+    if (o.qk_norm != 0 && o.qk_norm != 1) return "qk_norm must be 0 or 1";
+    if (o.rope_dims < 0 || o.rope_dims > 64 || o.rope_dims % 16 != 0) return "rope_dims must be a multiple of 16 in [0, 64]";
+    if (o.rope_dims && !o.qk_norm) return "rope_dims goes with qk_norm";
+    if (o.rope_dims && !(o.rope_base > 0.0f && std::isfinite(o.rope_base))) return "rope_base must be positive and finite";
+    if (o.qk_norm && !(o.qk_eps >= 0.0f && std::isfinite(o.qk_eps))) return "qk_eps must be >= 0 and finite";
+    return "";
+}
+
 }  // namespace
 
 struct dc_flow_state {
     dc_flow_cfg cfg{};
+    dc_flow_opt opt{};
     hipStream_t stream = nullptr;
     bool own_stream = false;
     bool bf = false;
@@ -118,7 +133,12 @@ struct dc_flow_state {
     void* carry = nullptr;
     int Pr = 0, Sl = 0, R = 0, Fr = 0;
     int64_t stream_stride = 0;
+    Carry4 carry4{};             // carry_bits 4: entry 0 = stream 0, conditional, of (step 0, block 0)
+    int64_t layer4 = 0;          // bytes between (step, block) pairs: all streams' regions
+    float *gains = nullptr, *freqs = nullptr;
     // per-call buffers
+    float *qkv = nullptr, *ws = nullptr;   // carry_bits 4: the projection's rows, the attention's workspace
+    int64_t ws_bytes = 0;
     void *xin = nullptr, *o = nullptr, *u = nullptr, *q = nullptr;
     float *h = nullptr, *v = nullptr, *x = nullptr;
     float *mu_in = nullptr, *mel_out = nullptr, *cond_in = nullptr, *gather = nullptr;
@@ -162,6 +182,95 @@ CarryRef carry_ref(const dc_flow_state* s, int i, int l)
     return r;
 }
 
+Carry4 carry4_ref(const dc_flow_state* s, int i, int l, int b0)
+{
+    Carry4 c = s->carry4;
+    c.base += ((int64_t)i * s->cfg.depth + l) * s->layer4 + (int64_t)b0 * 2 * c.heads * c.region;
+    return c;
+}
+
+// Where the streams of a call stand: entry 2 b' + c of streams from b0.  A
+// prompt pass begins at position 0 and keeps all its frames.
+Spans spans4(const dc_flow_state* s, int b0, int n, int prompt)
+{
+    if (prompt) return Spans{nullptr, nullptr, nullptr, 2, n, n};
+    return Spans{s->pos + b0, nullptr, s->plen + b0, 2, n, 0};
+}
+
+// The norm and rotation of block l.
+void set_qk(HeadsParams& p, const dc_flow_state* s, int l)
+{
+    p.norm = s->opt.qk_norm;
+    p.q_gain = s->gains + (size_t)l * 128;
+    p.k_gain = p.q_gain + 64;
+    p.freqs = s->freqs;
+    p.rot = s->opt.rope_dims;
+    p.eps = s->opt.qk_eps;
+}
+
+// carry_bits 4: the projection's fp32 rows [rows][3 dim] -> queries in the
+// operand type [rows][dim] and the call's keys and values into the carry.
+hipError_t enqueue_store4(const dc_flow_state* s, int i, int l, int b0, int Bc, int n, int prompt, hipStream_t st)
+{
+    const int D = s->cfg.dim, heads = s->cfg.heads;
+    HeadsParams p{};
+    auto part = [&](int k) {
+        return HeadRows{s->qkv + (size_t)k * D, (int64_t)2 * n * 3 * D, 3 * D, 64, heads, (int64_t)n * 3 * D, nullptr, 0, 0};
+    };
+    p.q = part(0);
+    p.k = part(1);
+    p.v = part(2);
+    p.q_out = HeadRows{s->q, (int64_t)2 * n * D, D, 64, heads, (int64_t)n * D, nullptr, 0, 0};
+    set_qk(p, s, l);
+    p.wide_in = p.wide_out = 1;
+    p.out_bf16 = s->bf ? 1 : 0;
+    p.c = carry4_ref(s, i, l, b0);
+    p.sp = spans4(s, b0, n, prompt);
+    p.entries = 2 * Bc;
+    return launch_heads(p, 64, 0, st);
+}
+
+// The carry in the operand type: norm and rotation of the queries and of the
+// call's keys where the projection has put them.
+hipError_t enqueue_qk(const dc_flow_state* s, const CarryRef& cr, int l, int b0, int Bc, int n, int Fq, int prompt,
+                      hipStream_t st)
+{
+    const int heads = s->cfg.heads;
+    HeadsParams p{};
+    p.q = HeadRows{s->q, (int64_t)2 * heads * Fq * 64, 64, (int64_t)Fq * 64, heads, (int64_t)heads * Fq * 64, nullptr, 0, 0};
+    p.k = HeadRows{(char*)cr.base + (size_t)b0 * cr.stream_stride * s->esz, cr.stream_stride, 64, (int64_t)cr.Fr * 64, heads,
+                   (int64_t)2 * heads * cr.Fr * 64, prompt ? nullptr : cr.slot + b0, prompt ? 0 : cr.Pr, cr.Sl};
+    p.q_out = p.q;
+    p.k_out = p.k;
+    set_qk(p, s, l);
+    p.wide_in = p.wide_out = 1;
+    p.out_bf16 = s->bf ? 1 : 0;
+    p.sp = spans4(s, b0, n, prompt);
+    p.entries = 2 * Bc;
+    return launch_heads(p, 64, s->bf ? 1 : 0, st);
+}
+
+hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc, int n, int prompt, hipStream_t st)
+{
+    const int D = s->cfg.dim, heads = s->cfg.heads;
+    Attend4Params p{};
+    p.q = HeadRows{s->q, (int64_t)2 * n * D, D, 64, heads, (int64_t)n * D, nullptr, 0, 0};
+    p.o = p.q;
+    p.o.p = s->o;
+    p.c = carry4_ref(s, i, l, b0);
+    p.sp = spans4(s, b0, n, prompt);
+    p.entries = 2 * Bc;
+    p.group = 1;
+    p.window = s->cfg.f_retained;
+    p.scale_log2 = 0.125f * 1.4426950408889634f;
+    p.wide_in = p.wide_out = 1;
+    int64_t need = 0;
+    p.splits = attend4_splits(p.c, p.entries, n, 1, p.window, &need);
+    if (need > s->ws_bytes) return hipErrorInvalidValue;
+    p.ws = s->ws;
+    return launch_attend4(p, s->bf ? 1 : 0, st);
+}
+
 // Per-launch timing: events recorded around each launch of a profiled call.
 struct Recorder {
     std::vector<std::string> role;
@@ -181,6 +290,7 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
     const int bf = s->bf ? 1 : 0;
     const int D = c.dim, M = c.n_mel, NL = c.depth, NS = c.n_steps;
     const int rows = Bc * 2 * n, Fq = round_up(n, 64);
+    const bool four = s->opt.carry_bits == 4;
     int k = 0;
     hipError_t e;
     const double es = (double)s->esz;
@@ -268,14 +378,28 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
             g.K = D;
             g.KS = k_steps(D, s->bf);
             g.carry = cr;
-            gemm_cost("gemm:qkv", 3 * D, D, 4, es, false);
-            DCF_TRY(launch_gemm(g, E_QKV, bf, st));
+            const double kv_bytes = four ? 34.0 : 64 * es;   // of a head's key or value in the carry
+            if (four) {
+                g.out = s->qkv;
+                gemm_cost("gemm:qkv", 3 * D, D, 4, 4, false);
+                DCF_TRY(launch_gemm(g, E_VEL, bf, st));
+                describe("heads", 0, (double)rows * (3 * D * 4 + D * es + 2 * c.heads * kv_bytes), 0);
+                DCF_TRY(enqueue_store4(s, i, l, b0, Bc, n, prompt, st));
+            } else {
+                gemm_cost("gemm:qkv", 3 * D, D, 4, es, false);
+                DCF_TRY(launch_gemm(g, E_QKV, bf, st));
+                if (s->opt.qk_norm) {
+                    describe("heads", 0, 4.0 * rows * D * es, 0);
+                    DCF_TRY(enqueue_qk(s, cr, l, b0, Bc, n, Fq, prompt, st));
+                }
+            }
             AttnParams at{s->q, Fq, cr, s->o, prompt, n, b0, c.heads, D, c.f_chunk,
                           s->R * ((c.f_chunk + 31) / 32) + (c.f_prompt + 31) / 32 + (n + 31) / 32};
             // per (stream, branch, head): n queries x its keys x 64, twice (scores, values)
             describe("attn", 4.0 * 2 * c.heads * 64 * (double)n * ext_keys,
-                     2.0 * 2 * c.heads * 64 * (double)ext_keys * es + 2.0 * rows * D * es, 1);
-            DCF_TRY(launch_attn(at, Bc, bf, st));
+                     2.0 * 2 * c.heads * (double)ext_keys * kv_bytes + 2.0 * rows * D * es, 1);
+            if (four) DCF_TRY(enqueue_attend4(s, i, l, b0, Bc, n, prompt, st));
+            else DCF_TRY(launch_attn(at, Bc, bf, st));
             plain(s->o);
             g.W = s->w_o[l];
             g.bias = s->b_o[l];
@@ -336,27 +460,41 @@ void host_advance(dc_flow_state* s, int n)
 
 extern "C" {
 
-int64_t dc_flow_blob_floats(const dc_flow_cfg* cfg)
+int64_t dc_flow_blob_floats(const dc_flow_cfg* cfg) { return dc_flow_blob_floats_opt(cfg, nullptr); }
+
+int64_t dc_flow_blob_floats_opt(const dc_flow_cfg* cfg, const dc_flow_opt* options)
 {
-    if (!cfg || !validate(cfg).empty()) return 0;
-    return blob_map(*cfg).total;
+    const dc_flow_opt opt = options ? *options : dc_flow_opt{};
+    if (!cfg || !validate(cfg).empty() || !validate_opt(opt).empty()) return 0;
+    return blob_map(*cfg, opt).total;
 }
 
 dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flow_cfg* cfg, dc_flow_state** out)
+{
+    return dc_flow_init_opt(weights_blob, blob_bytes, cfg, nullptr, out);
+}
+
+dc_status dc_flow_init_opt(const void* weights_blob, size_t blob_bytes, const dc_flow_cfg* cfg, const dc_flow_opt* options,
+                           dc_flow_state** out)
 {
     if (!out) return fail(nullptr, DC_EINVAL, "out is NULL");
     *out = nullptr;
     if (!cfg || !weights_blob) return fail(nullptr, DC_EINVAL, "cfg or weights is NULL");
     if (cfg->abi_version != DC_FLOW_ABI_VERSION) return fail(nullptr, DC_EVERSION, "abi_version mismatch");
-    const std::string why = validate(cfg);
+    if (options && options->abi_version != DC_FLOW_OPT_VERSION) return fail(nullptr, DC_EVERSION, "abi_version of the options");
+    const dc_flow_opt opt = options ? *options : dc_flow_opt{};
+    std::string why = validate(cfg);
+    if (why.empty()) why = validate_opt(opt);
     if (!why.empty()) return fail(nullptr, DC_EINVAL, why);
-    const BlobMap bm = blob_map(*cfg);
+    const BlobMap bm = blob_map(*cfg, opt);
     if (blob_bytes != (size_t)bm.total * sizeof(float))
         return fail(nullptr, DC_EINVAL, "blob size does not match the architecture");
 
     const auto t_start = std::chrono::steady_clock::now();
     dc_flow_state* s = new dc_flow_state();
     s->cfg = *cfg;
+    s->opt = opt;
+    const bool four = opt.carry_bits == 4;
     const dc_flow_cfg& c = s->cfg;
     s->bf = c.dtype == DC_BF16;
     s->esz = s->bf ? 2 : 4;
@@ -372,6 +510,11 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     s->R = c.f_retained / c.f_chunk;
     s->Fr = s->Pr + (s->R + 1) * s->Sl;
     s->stream_stride = (int64_t)NS * NL * 4 * c.heads * s->Fr * 64;
+    // in 4 bits: the prompt's slots, and a ring that holds the retained frames
+    // and a call's own
+    s->carry4 = Carry4{nullptr, carry4_region(c.f_prompt + c.f_retained + c.f_call, 64), c.heads, 64, c.f_prompt,
+                       c.f_retained + c.f_call};
+    s->layer4 = (int64_t)B * 2 * c.heads * s->carry4.region;
 
     // arena layout
     size_t off = 0;
@@ -399,6 +542,8 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
         o_bfc2[l] = place((size_t)D * 4);
     }
     const size_t o_bout = place((size_t)M * 4);
+    const size_t o_gains = place(opt.qk_norm ? (size_t)NL * 128 * 4 : 0);
+    const size_t o_freqs = place((size_t)opt.rope_dims / 2 * 4);
     const size_t weights_end = off;
     const size_t o_mods = place((size_t)NS * NL * 6 * D * 4);
     const size_t o_fmods = place((size_t)NS * 2 * D * 4);
@@ -412,7 +557,7 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     const size_t o_slot = place((size_t)B * 4);
     const size_t o_keys = place((size_t)B * 8);
     const size_t o_spk = place((size_t)B * M * 4);
-    const size_t o_carry = place((size_t)B * s->stream_stride * es);
+    const size_t o_carry = place(four ? (size_t)NS * NL * s->layer4 : (size_t)B * s->stream_stride * es);
     const size_t carry_end = off;
     const int rows_max = std::max(B * 2 * c.f_call, 2 * c.f_prompt);
     const int x_rows = std::max(B * c.f_call, c.f_prompt);
@@ -429,6 +574,19 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     const size_t o_mel = place((size_t)B * c.f_call * M * 4);
     const size_t o_cond = place((size_t)c.f_prompt * M * 4);
     const size_t o_gather = place((size_t)(c.f_retained + c.f_prompt) * D * 4);
+    const size_t o_qkv = place(four ? (size_t)rows_max * 3 * D * 4 : 0);
+    // the attention's workspace: of the call that needs most, chunk calls of
+    // all streams and prompt passes of one
+    auto ws_most = [&](int entries, int frames) {
+        for (int n = 1; four && n <= frames; n++) {
+            int64_t b = 0;
+            attend4_splits(s->carry4, entries, n, 1, c.f_retained, &b);
+            s->ws_bytes = std::max(s->ws_bytes, b);
+        }
+    };
+    ws_most(2 * B, c.f_call);
+    ws_most(2, c.f_prompt);
+    const size_t o_ws = place((size_t)s->ws_bytes);
     s->arena_bytes = off;
 
     hipError_t e = hipSuccess;
@@ -486,6 +644,11 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     s->mel_out = (float*)(A + o_mel);
     s->cond_in = (float*)(A + o_cond);
     s->gather = (float*)(A + o_gather);
+    s->gains = (float*)(A + o_gains);
+    s->freqs = (float*)(A + o_freqs);
+    s->qkv = (float*)(A + o_qkv);
+    s->ws = (float*)(A + o_ws);
+    s->carry4.base = (uint8_t*)(A + o_carry);
 
     // host image of the weight region: the per-step Linear weights in the
     // operand type (round to nearest even for bf16), biases in fp32
@@ -526,6 +689,11 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     }
     put_w(o_wout, bm.outW, M, D);
     put_b(o_bout, bm.outb, M);
+    if (opt.qk_norm) put_b(o_gains, bm.gains, (size_t)NL * 128);
+    for (int j = 0; j < opt.rope_dims / 2; j++) {
+        const float f = (float)std::pow((double)opt.rope_base, -2.0 * j / opt.rope_dims);
+        std::memcpy(host.data() + o_freqs + (size_t)j * 4, &f, 4);
+    }
     e = hipMemcpy(A, host.data(), weights_end, hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemsetAsync(A + weights_end, 0, s->arena_bytes - weights_end, s->stream);
 
@@ -578,7 +746,8 @@ dc_status dc_flow_init(const void* weights_blob, size_t blob_bytes, const dc_flo
     }
     s->st.weight_bytes = (int64_t)consts_end;
     s->st.carry_bytes = (int64_t)(carry_end - o_carry);
-    s->st.carry_live_bytes = (int64_t)B * NS * NL * 4 * (int64_t)(c.f_retained + c.f_prompt) * D * (int64_t)es;
+    s->st.carry_live_bytes = (int64_t)B * NS * NL * 4 * (int64_t)(c.f_retained + c.f_prompt) *
+                             (four ? (int64_t)c.heads * 34 : D * (int64_t)es);
     s->st.arena_bytes = (int64_t)s->arena_bytes;
     s->st.capture_ms = std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - t_start).count();
     *out = s;
@@ -678,8 +847,11 @@ dc_status dc_flow_carry_read(dc_flow_state* s, int32_t b, int32_t step, int32_t 
     const int ext = s->plen_host[b] == 0 ? 0 : (int)(nh * c.f_chunk + s->plen_host[b]);
     *frames = ext;
     if (!host_out || ext == 0) return DC_OK;
-    hipError_t e = launch_carry_gather(carry_ref(s, step, layer), b, branch, kv, c.heads, s->bf ? 1 : 0, ext,
-                                       c.f_chunk, s->gather, s->stream);
+    hipError_t e = s->opt.carry_bits == 4
+                       ? launch_carry4_gather(carry4_ref(s, step, layer, 0), spans4(s, 0, c.f_call, 0), 2 * b + branch, kv,
+                                              c.f_chunk, (int)nh, ext, s->gather, s->stream)
+                       : launch_carry_gather(carry_ref(s, step, layer), b, branch, kv, c.heads, s->bf ? 1 : 0, ext,
+                                             c.f_chunk, s->gather, s->stream);
     if (e == hipSuccess)
         e = hipMemcpyAsync(host_out, s->gather, (size_t)ext * c.dim * 4, hipMemcpyDeviceToHost, s->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(s->stream);

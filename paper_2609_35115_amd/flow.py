@@ -13,6 +13,7 @@ import numpy as np
 from . import DC_BF16, DC_F32, DC_HOST_PTRS, DC_NO_GRAPH, DC_OK, DcError, _ptr, lib  # noqa: F401
 
 DC_FLOW_ABI_VERSION = 1
+DC_FLOW_OPT_VERSION = 1
 _P = ctypes.c_void_p
 
 
@@ -25,6 +26,13 @@ class DcFlowCfg(ctypes.Structure):
         ("f_call", ctypes.c_int32), ("batch", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("flags", ctypes.c_uint32), ("cfg_rate", ctypes.c_float), ("temperature", ctypes.c_float),
         ("rng_seed", ctypes.c_uint64), ("hip_stream", ctypes.c_void_p),
+    ]
+
+
+class DcFlowOpt(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32), ("carry_bits", ctypes.c_int32), ("qk_norm", ctypes.c_int32),
+        ("rope_dims", ctypes.c_int32), ("rope_base", ctypes.c_float), ("qk_eps", ctypes.c_float),
     ]
 
 
@@ -70,6 +78,9 @@ _CARRY, _SPAN, _NORM, _ROWS = (ctypes.POINTER(t) for t in (DcCarry4, DcSpan, DcQ
 FLOW_SIGNATURES = {
     "dc_flow_blob_floats": ([ctypes.POINTER(DcFlowCfg)], ctypes.c_int64),
     "dc_flow_init": ([_P, ctypes.c_size_t, ctypes.POINTER(DcFlowCfg), ctypes.POINTER(_P)], ctypes.c_int),
+    "dc_flow_blob_floats_opt": ([ctypes.POINTER(DcFlowCfg), ctypes.POINTER(DcFlowOpt)], ctypes.c_int64),
+    "dc_flow_init_opt": ([_P, ctypes.c_size_t, ctypes.POINTER(DcFlowCfg), ctypes.POINTER(DcFlowOpt), ctypes.POINTER(_P)],
+                         ctypes.c_int),
     "dc_flow_prompt": ([_P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32], ctypes.c_int),
     "dc_flow_decode_chunk": ([_P, _P, ctypes.c_int32, _P], ctypes.c_int),
     "dc_flow_sync": ([_P], ctypes.c_int),
@@ -121,6 +132,12 @@ def make_flow_cfg(arch: dict, dtype: str, batch: int, flags: int = 0, stream: in
     return c
 
 
+def make_flow_opt(arch: dict) -> DcFlowOpt:
+    """The options that arch names: carry_bits (0 or 4), qk_norm (0 or 1), rope_dims, rope_base, qk_eps."""
+    return DcFlowOpt(DC_FLOW_OPT_VERSION, arch.get("carry_bits", 0), arch.get("qk_norm", 0), arch.get("rope_dims", 0),
+                     arch.get("rope_base", 10000.0), arch.get("qk_eps", 1e-6))
+
+
 def dc_flow_last_error(h) -> str:
     msg = flib().dc_flow_last_error(h)
     return msg.decode() if msg else ""
@@ -132,14 +149,15 @@ def _check(status: int, h) -> int:
     return status
 
 
-def dc_flow_blob_floats(cfg: DcFlowCfg) -> int:
-    return int(flib().dc_flow_blob_floats(ctypes.byref(cfg)))
+def dc_flow_blob_floats(cfg: DcFlowCfg, opt: DcFlowOpt | None = None) -> int:
+    return int(flib().dc_flow_blob_floats_opt(ctypes.byref(cfg), ctypes.byref(opt) if opt else None))
 
 
-def dc_flow_init(blob: np.ndarray, cfg: DcFlowCfg):
+def dc_flow_init(blob: np.ndarray, cfg: DcFlowCfg, opt: DcFlowOpt | None = None):
     blob = np.ascontiguousarray(blob, dtype=np.float32)
     h = ctypes.c_void_p()
-    st = flib().dc_flow_init(blob.ctypes.data, blob.nbytes, ctypes.byref(cfg), ctypes.byref(h))
+    st = flib().dc_flow_init_opt(blob.ctypes.data, blob.nbytes, ctypes.byref(cfg), ctypes.byref(opt) if opt else None,
+                                 ctypes.byref(h))
     if st != DC_OK:
         raise DcError(st, dc_flow_last_error(None))
     return h
@@ -192,7 +210,8 @@ def dc_flow_free(h) -> None:
 
 class FlowDecoder:
     """One dc_flow_state on the current GPU; device memory from torch-ROCm,
-    every call ordered on a dedicated torch stream."""
+    every call ordered on a dedicated torch stream.  arch may name options
+    (make_flow_opt): a carry in 4 bits, per-head norms and rotation."""
 
     def __init__(self, arch: dict, dtype: str, blob: np.ndarray, batch: int, flags: int = 0, rng_seed: int = 0):
         import torch
@@ -201,7 +220,7 @@ class FlowDecoder:
         self.host = bool(flags & DC_HOST_PTRS)
         self.stream = torch.cuda.Stream()
         self.cfg = make_flow_cfg(arch, dtype, batch, flags, self.stream.cuda_stream, rng_seed)
-        self.h = dc_flow_init(blob, self.cfg)
+        self.h = dc_flow_init(blob, self.cfg, make_flow_opt(arch))
 
     def close(self):
         if self.h is not None:

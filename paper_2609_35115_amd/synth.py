@@ -109,6 +109,7 @@ SAMPLE_RATE = 24000  # output rate of the real architecture (960 samples / 25 Hz
 #                  qkv.W [3*dim][dim], qkv.b [3*dim], o.W [dim][dim], o.b [dim],
 #                  fc1.W [mlp][dim], fc1.b [mlp], fc2.W [dim][mlp], fc2.b [dim]
 #     final:       ada.W [2*dim][dim], ada.b [2*dim], out.W [n_mel][dim], out.b [n_mel]
+#     with qk_norm: gains of queries and keys [depth][2][64], 1 + N(0, 0.2^2)
 #
 # drawn like the vocoder's blob (N(0, 1/fan_in), fan_in = in-features, from
 # SeedSequence([seed, 0]) in blob order).
@@ -261,6 +262,8 @@ def flow_tensor_list(arch: dict):
                 (f"b{l}.fc2.W", (D, H), H), (f"b{l}.fc2.b", (D,), H)]
     out += [("f.ada.W", (2 * D, D), D), ("f.ada.b", (2 * D,), D),
             ("out.W", (M, D), D), ("out.b", (M,), D)]
+    if arch.get("qk_norm", 0):
+        out.append(("qk.gain", (arch["depth"], 2, 64), 1))
     return out
 
 
@@ -273,7 +276,10 @@ def make_flow_weights(arch: dict, seed: int = 0) -> np.ndarray:
     rng = np.random.default_rng(np.random.SeedSequence([seed, 0]))
     parts = []
     for _name, shape, fan_in in flow_tensor_list(arch):
-        parts.append((rng.standard_normal(math.prod(shape)) / math.sqrt(fan_in)).astype(np.float32))
+        x = rng.standard_normal(math.prod(shape)) / math.sqrt(fan_in)
+        if _name == "qk.gain":   # around one
+            x = 1.0 + 0.2 * x
+        parts.append(x.astype(np.float32))
     return np.concatenate(parts)
 
 
