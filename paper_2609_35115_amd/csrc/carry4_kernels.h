@@ -55,40 +55,57 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
     }));
 }
 
-// Eight consecutive elements of a row.
-template <bool BF16> __device__ __forceinline__ void load8(const void* p, int64_t at, int wide, float (&x)[8])
+template <bool BF16> struct Raw8 { u32x4 w[BF16 ? 1 : 2]; };   // eight elements as they are stored
+
+template <bool BF16> __device__ __forceinline__ Raw8<BF16> load_raw(const void* p, int64_t at, int wide)
 {
+    Raw8<BF16> r;
     if constexpr (BF16) {
         const uint16_t* s = (const uint16_t*)p + at;
         if (wide) {
-            const u32x4 w = *(const u32x4*)s;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                x[2 * j] = bf2f(w[j] & 0xffffu);
-                x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
+            r.w[0] = *(const u32x4*)s;
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = bf2f(s[j]);
+            for (int j = 0; j < 4; j++) r.w[0][j] = s[2 * j] | (uint32_t)s[2 * j + 1] << 16;
         }
     } else {
-        const float* s = (const float*)p + at;
+        const uint32_t* s = (const uint32_t*)p + at;
         if (wide) {
-            const f32x4 a = *(const f32x4*)s, b = *(const f32x4*)(s + 4);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                x[j] = a[j];
-                x[4 + j] = b[j];
-            }
+            r.w[0] = *(const u32x4*)s;
+            r.w[1] = *(const u32x4*)(s + 4);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = s[j];
+            for (int j = 0; j < 4; j++) {
+                r.w[0][j] = s[j];
+                r.w[1][j] = s[4 + j];
+            }
+        }
+    }
+    return r;
+}
+template <bool BF16> __device__ __forceinline__ void widen(const Raw8<BF16>& r, float (&x)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        if constexpr (BF16) {
+            x[2 * j] = bf2f(r.w[0][j] & 0xffffu);
+            x[2 * j + 1] = __uint_as_float(r.w[0][j] & 0xffff0000u);
+        } else {
+            x[j] = __uint_as_float(r.w[0][j]);
+            x[4 + j] = __uint_as_float(r.w[1][j]);
         }
     }
 }
+
+template <bool BF16> __device__ __forceinline__ void load8(const void* p, int64_t at, int wide, float (&x)[8])
+{
+    widen<BF16>(load_raw<BF16>(p, at, wide), x);
+}
 template <bool BF16> __device__ __forceinline__ void store8(void* p, int64_t at, int wide, const float (&x)[8])
 {
-    if (wide) {
+    if (BF16 && wide) {
+        *(u32x4*)((uint16_t*)p + at) = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+    } else if (wide) {
         store4<BF16>(p, at, f32x4{x[0], x[1], x[2], x[3]});
         store4<BF16>(p, at + 4, f32x4{x[4], x[5], x[6], x[7]});
     } else {
@@ -111,9 +128,10 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 
 // ------------------------------- norms, rotation and the store into the carry
 //
-// D / 8 lanes hold a head's row, eight consecutive elements each, and a wave
-// 64 / (D / 8) tokens, whose heads it walks; so the cosines and sines of a
-// lane's token and dimensions are computed once for all its heads.
+// D / 8 lanes hold a head's row, eight consecutive elements each, and a block's
+// four waves the same 64 / (D / 8) tokens, whose heads they share out; so the
+// cosines and sines of a lane's token and dimensions are computed once for all
+// of the block's heads.
 //
 // y = x / sqrt(mean(x^2) + eps) gain, sums in fp32.  The angle position *
 // freqs[j] is taken in 64 bits (fp32 would be off by half a radian at position
@@ -127,42 +145,53 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 // cut), and an element is the nearest E2M1 value of x 2^-e, ties to even.
 // Scaling by a power of two is exact, so the codes do not depend on the
 // precision they are computed in.  A group with a NaN or an infinity is NaN.
-template <bool BF16, bool OUT16, int D>
+// The value of the lane whose number differs by half a row's lanes (D = 64:
+// lane ^ 4; 128: lane ^ 8), without an LDS round trip.
+template <int L> __device__ __forceinline__ float half_row(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    if constexpr (L == 16) return __uint_as_float(dpp<0x128>(u));        // row_ror:8
+    return __uint_as_float(dpp<0x1B>(dpp<0x141>(u)));                    // row_half_mirror (^ 7), quad_perm 3 2 1 0 (^ 3)
+}
+
+template <bool BF16, int D>
 __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
 {
     constexpr int L = D / 8, TPW = 64 / L;   // lanes of a row, tokens of a wave
-    const int lane = threadIdx.x & 63, l = lane % L;
-    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    __shared__ __align__(16) float turn[2][64][8];   // cosines, sines
+    const int lane = threadIdx.x & 63, l = lane % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = p.sp.n;
     const int64_t tokens = (int64_t)p.entries * n;
-    const int64_t t = (int64_t)(wave / p.splits) * TPW + lane / L;
+    const int64_t t = (int64_t)(blockIdx.x / p.splits) * TPW + lane / L;
     const int e = (int)(min(t, tokens - 1) / n), i = (int)(min(t, tokens - 1) % n);
     const Span sp(p.sp, p.c, e);
     const bool on = t < tokens && i < sp.len;
     const int64_t pos = sp.pos + i;
 
     const int jobs = p.q.heads + p.k.heads + p.v.heads;
-    const int part = wave % p.splits;
-    const int j0 = (int)((int64_t)jobs * part / p.splits), j1 = (int)((int64_t)jobs * (part + 1) / p.splits);
+    const int part = 4 * (blockIdx.x % p.splits) + wave, parts = 4 * p.splits;
+    const int j0 = (int)((int64_t)jobs * part / parts), j1 = (int)((int64_t)jobs * (part + 1) / parts);
 
-    // the rotation of this lane's dimensions; identity past rot
+    // the rotation of this lane's dimensions (identity past rot), a quarter by
+    // each wave
     float cs[8], sn[8];
     const bool inter = p.interleaved != 0;
     const int half = p.rot >> 1;
     const bool first = 8 * l < half;                     // half-split pairs: this lane holds the pairs' first members
-    if (p.norm) {
+    if (p.norm && p.rot) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int j = 2 * wave + k, d = 8 * l + j, f = inter ? d >> 1 : first ? d : d - half;
+            float c = 1.0f, s = 0.0f;
+            if (d < p.rot) sincospif(2.0f * turn_fraction(pos, p.freqs[f]), &s, &c);
+            turn[0][lane][j] = c;
+            turn[1][lane][j] = !inter && first ? -s : s;   // the sign that the pair's other member enters with
+        }
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            const int d = 8 * l + j, f = inter ? d >> 1 : first ? d : d - half;
-            cs[j] = 1.0f;
-            sn[j] = 0.0f;
-            if (d < p.rot && !(inter && (j & 1))) {
-                sincospif(2.0f * turn_fraction(pos, p.freqs[f]), &sn[j], &cs[j]);
-            }
-            if (inter && (j & 1)) {
-                cs[j] = cs[j - 1];
-                sn[j] = sn[j - 1];
-            }
+            cs[j] = turn[0][lane][j];
+            sn[j] = turn[1][lane][j];
         }
     }
     const int partner = (lane & ~(L - 1)) | ((8 * l < p.rot ? (first ? l + half / 8 : l - half / 8) : l) & (L - 1));
@@ -175,40 +204,52 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
         else if (pos + p.c.ring >= sp.total) slot = p.c.sinks + (pos - sp.sinks) % p.c.ring;
     }
 
-    for (int j = j0; j < j1; j++) {
-        const int kind = j < p.q.heads ? 0 : j < p.q.heads + p.k.heads ? 1 : 2;
-        const int h = kind == 0 ? j : kind == 1 ? j - p.q.heads : j - p.q.heads - p.k.heads;
-        const HeadRows& in = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-        float x[8] = {};
-        if (on) load8<BF16>(in.p, in.at(p.sp.div, e, i, h) + 8 * l, p.wide_in, x);
-        if (p.norm && kind < 2) {
-            float ss = 0.0f;
+    // one kind of rows after the other, the next row loaded while this one is
+    // worked on
+    int jb = 0;
+    auto rows_of = [&](int kind, const HeadRows& in, const HeadRows& out, const float* gains) {
+        const int h0 = max(j0 - jb, 0), h1 = min(j1 - jb, in.heads);
+        jb += in.heads;
+        if (h0 >= h1) return;
+        float gain[8];
+        const bool norm = p.norm && kind < 2;
 #pragma unroll
-            for (int k = 0; k < 8; k++) ss = fmaf(x[k], x[k], ss);
-            ss = lanes_sum<L>(ss);
-            const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
-            const float* gain = kind == 0 ? p.q_gain : p.k_gain;
+        for (int k = 0; k < 8; k++) gain[k] = norm && gains ? gains[8 * l + k] : 1.0f;
+        const int64_t at0 = in.at(p.sp.div, e, i, 0) + 8 * l;
+        const int64_t out0 = out.p ? out.at(p.sp.div, e, i, 0) + 8 * l : 0;
+        Raw8<BF16> next{};
+        if (on) next = load_raw<BF16>(in.p, at0 + h0 * in.sh, p.wide_in);
+        for (int h = h0; h < h1; h++) {
+            float x[8];
+            widen<BF16>(next, x);
+            if (on && h + 1 < h1) next = load_raw<BF16>(in.p, at0 + (h + 1) * in.sh, p.wide_in);
+            if (norm) {
+                float ss = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 8; k++) x[k] = x[k] * r * (gain ? gain[8 * l + k] : 1.0f);
-            if (inter) {
+                for (int k = 0; k < 8; k++) ss = fmaf(x[k], x[k], ss);
+                ss = lanes_sum<L>(ss);
+                const float r = __builtin_amdgcn_rsqf(ss * (1.0f / D) + p.eps);   // 1 ulp
 #pragma unroll
-                for (int k = 0; k < 8; k += 2) {
-                    const float a = x[k], b = x[k + 1];
-                    x[k] = a * cs[k] - b * sn[k];
-                    x[k + 1] = b * cs[k] + a * sn[k];
-                }
-            } else {
+                for (int k = 0; k < 8; k++) x[k] = x[k] * r * gain[k];
+                if (inter) {
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
-                    const float y = __shfl(x[k], partner);
-                    x[k] = x[k] * cs[k] + (first ? -y : y) * sn[k];
+                    for (int k = 0; k < 8; k += 2) {
+                        const float a = x[k], b = x[k + 1];
+                        x[k] = a * cs[k] - b * sn[k];
+                        x[k + 1] = b * cs[k] + a * sn[k];
+                    }
+                } else if (p.rot == D) {
+#pragma unroll
+                    for (int k = 0; k < 8; k++) x[k] = x[k] * cs[k] + half_row<L>(x[k]) * sn[k];
+                } else if (p.rot) {
+#pragma unroll
+                    for (int k = 0; k < 8; k++) x[k] = x[k] * cs[k] + __shfl(x[k], partner) * sn[k];
                 }
             }
-        }
-        if (kind == 0 || (kind == 1 && p.k_out.p)) {
-            const HeadRows& o = kind == 0 ? p.q_out : p.k_out;
-            if (on) store8<OUT16>(o.p, o.at(p.sp.div, e, i, h) + 8 * l, p.wide_out, x);
-        } else {
+            if (out.p) {
+                if (on) store8<BF16>(out.p, out0 + h * out.sh, p.wide_out, x);
+                continue;
+            }
             uint32_t top = 0;
 #pragma unroll
             for (int k = 0; k < 8; k++) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);   // NaN and infinity are the largest
@@ -231,28 +272,30 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
                 if ((l & 3) == 0) reg[(int64_t)N * D + ((int64_t)kv * N + slot) * (D / 32) + (l >> 2)] = (uint8_t)s;
             }
         }
-    }
+    };
+    rows_of(0, p.q, p.q_out, p.q_gain);
+    rows_of(1, p.k, p.k_out, p.k_gain);
+    rows_of(2, p.v, HeadRows{}, nullptr);
 }
 
-template <bool BF16, bool OUT16, int D> hipError_t launch_heads_d(HeadsParams p, hipStream_t st)
+template <bool BF16, int D> hipError_t launch_heads_d(HeadsParams p, hipStream_t st)
 {
     constexpr int TPW = 64 / (D / 8);
     const int64_t tokens = (int64_t)p.entries * p.sp.n, groups = (tokens + TPW - 1) / TPW;
     const int jobs = p.q.heads + p.k.heads + p.v.heads;
-    // a wave walks all heads of its tokens unless that leaves few waves
+    // a block walks all heads of its tokens unless that leaves fewer than two blocks
+    // a CU (14,336 rows of 16 heads: 16.3 us, 28.7 with four times the blocks; 4,011
+    // of 12: 11.2 and 20.6)
     int64_t splits = 1;
-    while (splits < jobs && groups * splits < 4096) splits *= 2;
-    p.splits = (int)(splits < jobs ? splits : jobs);
-    return launch_with(heads_kernel<BF16, OUT16, D>, dim3((unsigned)((groups * p.splits + 3) / 4)), dim3(256), st, p);
+    while (4 * splits < jobs && groups * splits < 512) splits *= 2;
+    p.splits = (int)splits;
+    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)(groups * splits)), dim3(256), st, p);
 }
 
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st)
 {
-    if (D == 64)
-        return bf16 ? launch_heads_d<true, true, 64>(p, st)
-                    : p.out_bf16 ? launch_heads_d<false, true, 64>(p, st) : launch_heads_d<false, false, 64>(p, st);
-    return bf16 ? launch_heads_d<true, true, 128>(p, st)
-                : p.out_bf16 ? launch_heads_d<false, true, 128>(p, st) : launch_heads_d<false, false, 128>(p, st);
+    if (D == 64) return bf16 ? launch_heads_d<true, 64>(p, st) : launch_heads_d<false, 64>(p, st);
+    return bf16 ? launch_heads_d<true, 128>(p, st) : launch_heads_d<false, 128>(p, st);
 }
 
 // ---------------------------------------------------------------- carry read
@@ -271,37 +314,45 @@ __device__ __forceinline__ void decode8(uint32_t w, uint32_t s, float (&x)[8])
 #undef DCF_PAIR
 }
 
+// Lanes and tokens as in heads_kernel; a wave walks a share of the (kv, head) rows.
 template <bool BF16, int D> __global__ __launch_bounds__(256) void read4_kernel(const Read4Params p)
 {
-    constexpr int L = D / 8;
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;   // (entry, token, head)
-    const int l = threadIdx.x % L, kv = blockIdx.y;
-    if (row >= (int64_t)p.entries * p.sp.n * p.c.heads) return;
-    const int h = (int)(row % p.c.heads), i = (int)(row / p.c.heads % p.sp.n), e = (int)(row / p.c.heads / p.sp.n);
+    constexpr int L = D / 8, TPW = 64 / L;
+    const int lane = threadIdx.x & 63, l = lane % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = p.sp.n, heads = p.c.heads;
+    const int64_t t = (int64_t)blockIdx.x * TPW + lane / L;
+    const int e = (int)(min(t, (int64_t)p.entries * n - 1) / n), i = (int)(min(t, (int64_t)p.entries * n - 1) % n);
     const Span sp(p.sp, p.c, e);
-    if (i >= sp.len) return;
+    if (t >= (int64_t)p.entries * n || i >= sp.len) return;
     const int64_t pos = sp.pos + i;
-    const int64_t slot = pos < sp.sinks ? pos : p.c.sinks + (p.c.ring ? (pos - sp.sinks) % p.c.ring : 0);
-    if (slot >= p.c.slots()) return;
+    const int64_t slot = pos < sp.sinks ? pos : p.c.sinks + (pos - sp.sinks) % p.c.ring;
     const int N = p.c.slots();
-    const uint8_t* reg = p.c.base + ((int64_t)e * p.c.heads + h) * p.c.region;
-    const uint32_t w = *(const uint32_t*)(reg + ((int64_t)kv * N + slot) * (D / 2) + 4 * l);
-    const uint32_t s = reg[(int64_t)N * D + ((int64_t)kv * N + slot) * (D / 32) + (l >> 2)];
-    float x[8];
-    decode8(w, s, x);
-    const HeadRows& o = kv ? p.v : p.k;
-    store8<BF16>(o.p, o.at(p.sp.div, e, i, h) + 8 * l, p.wide, x);
+    for (int kv = 0; kv < 2; kv++) {
+        const HeadRows& o = kv ? p.v : p.k;
+        const int64_t at = o.at(p.sp.div, e, i, 0) + 8 * l;
+        const uint8_t* codes = p.c.base + (int64_t)e * heads * p.c.region + ((int64_t)kv * N + slot) * (D / 2) + 4 * l;
+        const uint8_t* scale = p.c.base + (int64_t)e * heads * p.c.region + (int64_t)N * D + ((int64_t)kv * N + slot) * (D / 32) + (l >> 2);
+#pragma unroll 2
+        for (int h = wave; h < heads; h += 4) {
+            float x[8];
+            decode8(*(const uint32_t*)(codes + h * p.c.region), scale[h * p.c.region], x);
+            store8<BF16>(o.p, at + h * o.sh, p.wide, x);
+        }
+    }
+}
+
+template <bool BF16, int D> hipError_t launch_read4_d(const Read4Params& p, hipStream_t st)
+{
+    constexpr int TPW = 64 / (D / 8);
+    const unsigned blocks = (unsigned)(((int64_t)p.entries * p.sp.n + TPW - 1) / TPW);
+    return launch_with(read4_kernel<BF16, D>, dim3(blocks), dim3(256), st, p);
 }
 
 hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
 {
-    const int64_t threads = (int64_t)p.entries * p.sp.n * p.c.heads * (p.c.D / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256), 2), block(256);
-    if (p.c.D == 64)
-        return bf16 ? launch_with(read4_kernel<true, 64>, grid, block, st, p) : launch_with(read4_kernel<false, 64>, grid, block, st, p);
-    return bf16 ? launch_with(read4_kernel<true, 128>, grid, block, st, p) : launch_with(read4_kernel<false, 128>, grid, block, st, p);
+    if (p.c.D == 64) return bf16 ? launch_read4_d<true, 64>(p, st) : launch_read4_d<false, 64>(p, st);
+    return bf16 ? launch_read4_d<true, 128>(p, st) : launch_read4_d<false, 128>(p, st);
 }
-
 template <int D>
 __global__ __launch_bounds__(256) void carry4_gather_kernel(const Carry4 c, const Spans spans, int e, int kv, int f_chunk,
                                                             int nh, int frames, float* out)
@@ -379,6 +430,10 @@ template <int PL> __device__ __forceinline__ Planes<PL> split8(const float (&x)[
 // The rows' visible members of the block's list.
 struct RowSpan {
     int sink_hi, lo, hi;   // visible: [0, sink_hi) and [lo, hi)
+    __device__ __forceinline__ bool sees(int key) const   // (no short circuits: a branch a score)
+    {
+        return (key < sink_hi) | ((uint32_t)(key - lo) < (uint32_t)max(hi - lo, 0));
+    }
 };
 
 struct KeyList {
@@ -586,7 +641,7 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Params p)
             for (int i = 0; i < 4; i++) {
                 s[b][i] *= p.scale_log2;
                 const int key = t0 + 16 * b + 4 * g + i;
-                const bool see = open || (key < mine.sink_hi || (key >= mine.lo && key < mine.hi));
+                const bool see = open | mine.sees(key);
                 if (!see) s[b][i] = -INFINITY;
                 if ((nanv[b] != 0) && see) {
                     const uint64_t x = nanv[b] >> (4 * g + i);
@@ -685,31 +740,339 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Params p)
     }
 }
 
-// Joins the splits of a row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-template <bool BF16, int D> __global__ __launch_bounds__(256) void attend4_join(const Attend4Params p)
+// Calls of many query rows: a block of NW waves works on 16 QG NW rows, each wave
+// on its own 16 QG; 64-key tiles are decoded once for the block, into LDS as bf16
+// rows (keys for 16-byte operand reads, values for transposing ones), with the
+// next tile's codes loaded into registers meanwhile.  The running maximum is
+// only moved when a score passes it by more than 2^8 (a probability's rounding
+// to bf16 is relative, and 2^8 times more fits fp32 with room), so the output
+// is rarely rescaled; in bf16 the probabilities' sum is one more row of the
+// second product (ones), not vector work.
+constexpr int kWideTile = 64;
+constexpr float kSlack = 8.0f;
+
+template <bool BF16, int D, int QG, int NW> struct Wide4 {
+    static constexpr int KROW = 2 * D + 16, VROW = 2 * D + 32;   // bytes: an LDS row's banks shift from row to row
+    static constexpr int G = D / 32;
+    // 16-byte code chunks (32 values, one scale) a thread: wave w's are sets w + NW c
+    // of 2 G sets of 64, the keys' first
+    static constexpr int CH = 2 * G / NW;
+    static_assert(kWideTile == 64 && CH * NW == 2 * G);
+    static constexpr int LDS = kWideTile * (KROW + VROW) + kWideTile * G + 16;
+};
+
+template <bool BF16, int D, int QG, int NW>
+__global__ __launch_bounds__(64 * NW, QG == 2 ? (D == 64 ? 3 : 2) : BF16 ? (D == 64 ? 5 : 3) : 2) void attend4_wide(const Attend4Params p)
 {
-    constexpr int CH = D / 4;
-    const int rows = p.sp.n * p.group;
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, regions = (int64_t)p.entries * p.c.heads;
-    const int64_t id = u / CH;
-    const int d = 4 * (int)(u % CH);
-    if (id >= regions * rows) return;
-    const int eh = (int)(id / rows), row = (int)(id % rows), e = eh / p.c.heads, h = eh % p.c.heads;
+    using W = Wide4<BF16, D, QG, NW>;
+    constexpr int PL = BF16 ? 1 : 3, KS = D / 32, DB = D / 16, VB = 4, RB = 16 * QG * NW;
+    __shared__ __align__(16) unsigned char smem[W::LDS];
+    unsigned char *kt = smem, *vt = smem + kWideTile * W::KROW;
+    uint8_t* nanb = vt + kWideTile * W::VROW;          // [key][group of 32 values]: the values are NaN
+    uint8_t* nany = nanb + kWideTile * W::G;           // [wave]: some of its chunks are, and it has set nanb for them
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int regions = p.entries * p.c.heads, split = blockIdx.x % p.splits;
+    const int eh = blockIdx.x / p.splits % regions, e = eh / p.c.heads, h = eh % p.c.heads;
     const Span sp(p.sp, p.c, e);
-    if (row >= sp.len * p.group) return;
-    const int64_t parts = regions * rows * p.splits;
-    const float* ml = p.ws + parts * D + 2 * id * p.splits;
-    float m = -INFINITY, l = 0.0f;
-    for (int s = 0; s < p.splits; s++) m = fmaxf(m, ml[2 * s]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    f32x4 o = {0, 0, 0, 0};
-    for (int s = 0; s < p.splits; s++) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
-        l += ml[2 * s + 1] * f;
-        const f32x4 x = *(const f32x4*)(p.ws + (id * p.splits + s) * D + d);
+    const int rows = sp.len * p.group, row0 = RB * (blockIdx.x / p.splits / regions);
+    if (row0 >= rows) return;
+    const int last = min(row0 + RB - 1, rows - 1);
+    const KeyList list(p, sp, row0 / p.group, last / p.group);
+    const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
+    const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;
+    const int N = p.c.slots();
+    const uint8_t* reg = p.c.base + (int64_t)eh * p.c.region;
+
+    RowSpan mine[QG];
+    Planes<PL> qf[QG][KS];
 #pragma unroll
-        for (int k = 0; k < 4; k++) o[k] += x[k] * f;
+    for (int u = 0; u < QG; u++) {
+        const int row = min(row0 + 16 * (QG * wave + u) + r, rows - 1), i = row / p.group, hq = h * p.group + row % p.group;
+        mine[u] = list.row(p, sp, i);
+        const int64_t at = p.q.at(p.sp.div, e, i, hq) + 8 * g;
+#pragma unroll
+        for (int c = 0; c < KS; c++) {
+            float x[8];
+            load8<BF16>(p.q.p, at + 32 * c, p.wide_in, x);
+            qf[u][c] = split8<PL>(x);
+        }
     }
+
+    const int tiles = (list.nk + kWideTile - 1) / kWideTile;
+    const int t_lo = (int)((int64_t)tiles * split / p.splits), t_hi = (int)((int64_t)tiles * (split + 1) / p.splits);
+
+    struct Chunks {
+        u32x4 w[W::CH];
+        uint32_t s[W::CH];
+    } cur;
+    auto load = [&](int t) {
+#pragma unroll
+        for (int c = 0; c < W::CH; c++) {
+            const int kv = (wave + NW * c) / W::G, u = (wave + NW * c) % W::G * 64 + lane;
+            const uint32_t slot = (uint32_t)list.slot(t * kWideTile + u / W::G) + (uint32_t)(kv * N), grp = (uint32_t)(u % W::G);
+            cur.w[c] = *(const u32x4*)(reg + (slot * (uint32_t)(D / 2) + 16 * grp));
+            cur.s[c] = reg[(uint32_t)N * D + slot * (uint32_t)W::G + grp];
+        }
+    };
+    auto store = [&]() {
+        bool any = false;   // NaN values are kept out of the products and noted
+#pragma unroll
+        for (int c = 0; c < W::CH; c++)
+            if ((wave + NW * c) / W::G) any |= __any(cur.s[c] == 255);
+        nany[wave] = any;
+        if (__builtin_expect(any, 0)) {
+#pragma unroll
+            for (int c = 0; c < W::CH; c++)
+                if ((wave + NW * c) / W::G) {
+                    const bool nan = cur.s[c] == 255;
+                    nanb[(wave + NW * c) % W::G * 64 + lane] = nan;
+                    if (nan) {
+                        cur.w[c] = u32x4{0, 0, 0, 0};
+                        cur.s[c] = 127;
+                    }
+                }
+        }
+#pragma unroll
+        for (int c = 0; c < W::CH; c++) {
+            const int kv = (wave + NW * c) / W::G, u = (wave + NW * c) % W::G * 64 + lane;
+            const int key = u / W::G, grp = u % W::G;
+            unsigned char* to = (kv ? vt + key * W::VROW : kt + key * W::KROW) + 64 * grp;
+#pragma unroll
+            for (int k = 0; k < 4; k++) *(bf16x8_t*)(to + 16 * k) = decode_frag(cur.w[c][k], cur.s[c]);
+        }
+    };
+
+    f32x4 o[QG][DB], ls[QG];   // ls: the probabilities' sums (bf16: every row the whole sum; fp32: [0], this lane's keys)
+    float base[QG], limit[QG];   // of a row: what its scores are taken from (0 before any), and what moves it
+    uint32_t nan_seen[QG];
+#pragma unroll
+    for (int u = 0; u < QG; u++) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[u][b] = f32x4{0, 0, 0, 0};
+        ls[u] = f32x4{0, 0, 0, 0};
+        base[u] = 0.0f;
+        limit[u] = -INFINITY;
+        nan_seen[u] = 0;
+    }
+    bf16x8_t ones;
+#pragma unroll
+    for (int j = 0; j < 8; j++) ones[j] = (__bf16)1.0f;
+
+    if (t_lo < t_hi) load(t_lo);
+    for (int t = t_lo; t < t_hi; t++) {
+        if (t > t_lo) __syncthreads();   // the previous tile has been read
+        store();
+        if (t + 1 < t_hi) load(t + 1);
+        __syncthreads();
+        const int t0 = t * kWideTile;
+        // a scale that turns the scores' order around takes the masking path too
+        const bool open = ((t0 + kWideTile <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + kWideTile <= lead.hi))) & (p.scale_log2 > 0.0f);
+
+        // scores: the next score block's key fragments are read while this one's
+        // are multiplied
+        f32x4 s[QG][4];
+        bf16x8_t kf[2][KS];
+        auto read_k = [&](int b) {
+#pragma unroll
+            for (int c = 0; c < KS; c++) kf[b & 1][c] = *(const bf16x8_t*)(kt + (16 * b + r) * W::KROW + 64 * c + 16 * g);
+        };
+        read_k(0);
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            if (b + 1 < 4) read_k(b + 1);
+#pragma unroll
+            for (int u = 0; u < QG; u++) s[u][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < KS; c++)
+#pragma unroll
+                for (int u = 0; u < QG; u++)
+#pragma unroll
+                    for (int k = PL - 1; k >= 0; k--)
+                        s[u][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b & 1][c], qf[u][c].f[k], s[u][b], 0, 0, 0);
+        }
+        // the first values' fragments, read while the probabilities are computed
+        bf16x8_t vf[2][VB];
+        auto read_v = [&](int half, int b0) {
+#pragma unroll
+            for (int b = 0; b < VB; b++) {
+                const unsigned char* a = vt + (32 * half + 4 * g + (r >> 2)) * W::VROW + 32 * (b0 + b) + 8 * (r & 3);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 16 * W::VROW));
+                struct Two { s16x4 a, b; } two = {lo, hi};
+                vf[(half * DB + b0) / VB & 1][b] = __builtin_bit_cast(bf16x8_t, two);
+            }
+        };
+        read_v(0, 0);
+        const float mul = open ? p.scale_log2 : 1.0f;
+        uint32_t nan_waves = 0;
+#pragma unroll
+        for (int w = 0; w < NW; w++) nan_waves |= nany[w];
+
+#pragma unroll
+        for (int u = 0; u < QG; u++) {
+            // (masked scores are scaled before their mask: 0 times an infinity is NaN)
+            if (!open) {
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        s[u][b][i] = mine[u].sees(t0 + 16 * b + 4 * g + i) ? s[u][b][i] * p.scale_log2 : -INFINITY;
+            }
+            if (__builtin_expect(nan_waves != 0, 0)) {
+#pragma unroll 1
+                for (int k = 0; k < 16; k++) {
+                    const int at = 16 * (k >> 2) + 4 * g + (k & 3);
+                    for (int gg = 0; gg < W::G; gg++)
+                        if (mine[u].sees(t0 + at) && nany[(W::G + (at * W::G + gg) / 64) % NW] && nanb[at * W::G + gg])
+                            nan_seen[u] |= 1u << gg;
+                }
+            }
+            // (the lanes of a row compare their own keys; they meet only to move its base)
+            float top = s[u][0][0];
+#pragma unroll
+            for (int k = 1; k < 16; k++) top = fmaxf(top, s[u][k >> 2][k & 3]);
+            if (__any(top * mul > limit[u])) {
+                top = max_xor16_32(top) * mul;
+                const bool move = top > limit[u];
+                const float f = move ? __builtin_amdgcn_exp2f((limit[u] - kSlack) - top) : 1.0f;
+                if (move) {
+                    limit[u] = top + kSlack;
+                    base[u] = top;
+                }
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[u][b][i] *= f;
+#pragma unroll
+                for (int i = 0; i < 4; i++) ls[u][i] *= f;
+            }
+        }
+        // each half tile's probabilities and products (a list that ends in the
+        // first half has no second)
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            if (D == 64 && half && t0 + 32 >= list.nk) break;
+            Planes<PL> pf[QG];
+#pragma unroll
+            for (int u = 0; u < QG; u++) {
+                float pr[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    pr[j] = __builtin_amdgcn_exp2f(fmaf(s[u][2 * half + (j >> 2)][j & 3], mul, -base[u]));
+                if constexpr (!BF16) {
+#pragma unroll
+                    for (int j = 0; j < 8; j++) ls[u][0] += pr[j];
+                }
+                pf[u] = split8<PL>(pr);
+            }
+#pragma unroll
+            for (int b0 = 0; b0 < DB; b0 += VB) {
+                if (b0 + VB < DB) read_v(half, b0 + VB);
+                else if (half == 0) read_v(1, 0);
+#pragma unroll
+                for (int b = 0; b < VB; b++)
+#pragma unroll
+                    for (int u = 0; u < QG; u++)
+#pragma unroll
+                        for (int k = PL - 1; k >= 0; k--)
+                            o[u][b0 + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[(half * DB + b0) / VB & 1][b], pf[u].f[k], o[u][b0 + b], 0, 0, 0);
+            }
+            if constexpr (BF16) {
+#pragma unroll
+                for (int u = 0; u < QG; u++) ls[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[u].f[0], ls[u], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < QG; u++) {
+        const float l = BF16 ? ls[u][0] : sum_xor16_32(ls[u][0]);
+        const uint32_t nan = or_xor16_32(nan_seen[u]);
+        const int row = row0 + 16 * (QG * wave + u) + r;
+        if (row > last) continue;
+        const int i = row / p.group, hq = h * p.group + row % p.group;
+        const int64_t at = p.o.at(p.sp.div, e, i, hq);
+        const int64_t part = ((int64_t)eh * p.sp.n * p.group + row) * p.splits + split;
+        const int64_t parts = (int64_t)regions * p.sp.n * p.group * p.splits;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int b = 0; b < DB; b++) {
+            f32x4 x = o[u][b];
+            if ((nan >> (b / 2)) & 1) x = f32x4{NAN, NAN, NAN, NAN};
+            const int d = 16 * b + 4 * g;
+            if (p.splits > 1) {
+                *(f32x4*)(p.ws + part * D + d) = x;
+            } else if (p.wide_out) {
+                store4<BF16>(p.o.p, at + d, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k++) store1<BF16>(p.o.p, at + d + k, x[k] * inv);
+            }
+        }
+        if (p.splits > 1 && g == 0) {
+            p.ws[parts * D + 2 * part] = limit[u] - kSlack;
+            p.ws[parts * D + 2 * part + 1] = l;
+        }
+    }
+}
+
+// Joins the splits of a row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// NG groups of D / 4 threads share a row's splits, each with its own running
+// maximum, and meet in LDS (512 splits of 60 rows: 130 -> 8 us against one thread
+// for all of them).
+template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void attend4_join(const Attend4Params p)
+{
+    constexpr int CH = D / 4, ROWS = 256 / (CH * NG);   // rows of a block
+    __shared__ __align__(16) float sm[NG > 1 ? ROWS * NG * (D + 2) : 1];
+    const int rows = p.sp.n * p.group;
+    const int64_t regions = (int64_t)p.entries * p.c.heads;
+    const int ch = threadIdx.x % CH, grp = threadIdx.x / CH % NG, local = threadIdx.x / (CH * NG), d = 4 * ch;
+    const int64_t id = (int64_t)blockIdx.x * ROWS + local;
+    const bool in = id < regions * rows;
+    const int64_t at_id = in ? id : 0;
+    const int eh = (int)(at_id / rows), row = (int)(at_id % rows), e = eh / p.c.heads, h = eh % p.c.heads;
+    const Span sp(p.sp, p.c, e);
+    const bool on = in && row < sp.len * p.group;
+    const int64_t parts = regions * rows * p.splits;
+    const float* ml = p.ws + parts * D + 2 * at_id * p.splits;
+    const float* po = p.ws + at_id * p.splits * D + d;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    if (on) {
+        for (int s = grp; s < p.splits; s += NG) {
+            const float ms = ml[2 * s], top = fmaxf(m, ms), base = top == -INFINITY ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - base), b = __builtin_amdgcn_exp2f(ms - base);
+            const f32x4 x = *(const f32x4*)(po + (int64_t)s * D);
+            m = top;
+            l = l * a + ml[2 * s + 1] * b;
+#pragma unroll
+            for (int k = 0; k < 4; k++) o[k] = o[k] * a + x[k] * b;
+        }
+    }
+    if constexpr (NG > 1) {
+        *(f32x4*)(sm + (local * NG + grp) * D + d) = o;
+        float* stat = sm + ROWS * NG * D + 2 * (local * NG + grp);
+        if (ch == 0) {
+            stat[0] = m;
+            stat[1] = l;
+        }
+        __syncthreads();
+        if (grp) return;
+        const float* all = sm + ROWS * NG * D + 2 * local * NG;
+        for (int g = 0; g < NG; g++) m = fmaxf(m, all[2 * g]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        l = 0.0f;
+        o = f32x4{0, 0, 0, 0};
+        for (int g = 0; g < NG; g++) {
+            const float f = __builtin_amdgcn_exp2f(all[2 * g] - base);
+            const f32x4 x = *(const f32x4*)(sm + (local * NG + g) * D + d);
+            l += all[2 * g + 1] * f;
+#pragma unroll
+            for (int k = 0; k < 4; k++) o[k] += x[k] * f;
+        }
+    }
+    if (!on) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int i = row / p.group, hq = h * p.group + row % p.group;
     const int64_t at = p.o.at(p.sp.div, e, i, hq) + d;
@@ -721,25 +1084,61 @@ template <bool BF16, int D> __global__ __launch_bounds__(256) void attend4_join(
     }
 }
 
+// Which kernel an attention call takes, and over how many blocks its keys are
+// split.  Us of a call in a graph, bf16, both sides of each border:
+//   16 rows a block up to 32 rows (20 rows, 256 regions, 3,025 keys of 128: 50,
+//     in 64-row blocks 103; 60 rows, 256 regions, 560 keys 25 and 17), and for
+//     fewer than 32 wider blocks of short lists (56 rows, 16 regions, 458 keys: 9.0
+//     and 9.8);
+//   128 rows from two blocks a CU on (16,384 rows, 4 regions, 4,100 keys of 128:
+//     148, in 64-row blocks 197, in 256-row ones 146; 256 rows, 64 regions, 1,000
+//     keys: 35, 24 and 53);
+//   splits for up to 512 blocks of 16 rows or 256 wider ones, of 256 and 512 keys
+//     at least: the join is a launch of its own, about 3 us (2,000 keys, 8
+//     regions 9.6 split in 7, 17.9 unsplit; 458 keys 7.6 unsplit, 9.0 in two; 56
+//     rows, 256 blocks 16.3 unsplit, 25.5 in two).
+struct Plan4 {
+    int rows;     // query rows of a block: 16 (one set for four waves), 64 or 128 (16 or 32 a wave)
+    int splits;
+};
+static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
+{
+    const int64_t rows = (int64_t)n * group, regions = (int64_t)entries * c.heads;
+    const int64_t most = (int64_t)c.sinks + (window < c.ring ? window : c.ring) + n;   // keys of a list
+    Plan4 pl;
+    if (rows <= 32 || (regions * ((rows + 63) / 64) < 32 && most < 1024)) pl.rows = 16;
+    else pl.rows = rows > 96 && regions * ((rows + 127) / 128) >= 512 ? 128 : 64;
+    const int64_t blocks = regions * ((rows + pl.rows - 1) / pl.rows);
+    int64_t s = (pl.rows == 16 ? 512 : 256) / (blocks > 0 ? blocks : 1);
+    const int64_t most_splits = most / (pl.rows == 16 ? 256 : 512);
+    if (s > most_splits) s = most_splits;
+    pl.splits = s < 1 ? 1 : (int)s;
+    return pl;
+}
+
 int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes)
 {
-    const int64_t rows = (int64_t)n * group, blocks = (int64_t)entries * c.heads * ((rows + 15) / 16);
-    const int64_t most = (int64_t)c.sinks + (window < c.ring ? window : c.ring) + n;
-    int64_t s = 1024 / (blocks > 0 ? blocks : 1), per = (most + 8 * kKeyTile - 1) / (8 * kKeyTile);
-    if (s > per) s = per;
-    if (s < 1) s = 1;
-    if (ws_bytes) *ws_bytes = s > 1 ? (int64_t)entries * c.heads * rows * s * (c.D + 2) * 4 : 0;
-    return (int)s;
+    const Plan4 pl = plan4(c, entries, n, group, window);
+    if (ws_bytes)
+        *ws_bytes = pl.splits > 1 ? (int64_t)entries * c.heads * n * group * pl.splits * (c.D + 2) * 4 : 0;
+    return pl.splits;
 }
 
 template <bool BF16, int D> hipError_t launch_attend4_d(const Attend4Params& p, hipStream_t st)
 {
-    const int rows = p.sp.n * p.group;
-    const unsigned blocks = (unsigned)((int64_t)p.splits * p.entries * p.c.heads * ((rows + 15) / 16));
-    hipError_t e = launch_with(attend4_kernel<BF16, D>, dim3(blocks), dim3(256), st, p);
+    const int64_t rows = (int64_t)p.sp.n * p.group;
+    int rb = plan4(p.c, p.entries, p.sp.n, p.group, p.window).rows;
+    if (!BF16 && rb == 128) rb = 64;   // (three planes of 32 rows do not fit the registers)
+    const dim3 grid((unsigned)((int64_t)p.splits * p.entries * p.c.heads * ((rows + rb - 1) / rb)));
+    hipError_t e = hipErrorInvalidValue;
+    if (rb == 16) e = launch_with(attend4_kernel<BF16, D>, grid, dim3(256), st, p);
+    else if (rb == 64 || !BF16) e = launch_with(attend4_wide<BF16, D, 1, 4>, grid, dim3(256), st, p);
+    else if constexpr (BF16) e = launch_with(attend4_wide<BF16, D, 2, 4>, grid, dim3(256), st, p);
     if (e != hipSuccess || p.splits == 1) return e;
-    const int64_t threads = (int64_t)p.entries * p.c.heads * rows * (D / 4);
-    return launch_with(attend4_join<BF16, D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), st, p);
+    const int64_t all = (int64_t)p.entries * p.c.heads * rows;
+    constexpr int per = 256 / (D / 4);   // rows of a block, or groups of one row
+    if (p.splits <= 4) return launch_with(attend4_join<BF16, D, 1>, dim3((unsigned)((all + per - 1) / per)), dim3(256), st, p);
+    return launch_with(attend4_join<BF16, D, per>, dim3((unsigned)all), dim3(256), st, p);
 }
 
 hipError_t launch_attend4(const Attend4Params& p, int bf16, hipStream_t st)

@@ -44,6 +44,7 @@ enum Epi : int {
     E_RES = 2,   // h += gate * (acc + bias)              (fp32)
     E_GELU = 3,  // out = GELU_tanh(acc + bias)           (operand type)
     E_VEL = 4,   // out = acc + bias                      (fp32)
+    E_ROWS = 5,  // out = acc + bias                      (operand type)
 };
 
 struct CarryRef {
@@ -72,7 +73,7 @@ struct GemmParams {
     int groups, nsplit;      // many rows: column groups per wave, blocks per row tile
     float* h;                // E_H, E_RES: [M][N]
     const float* gate;       // E_RES: [N]
-    void* out;               // E_GELU (operand type), E_VEL (fp32): [M][N]
+    void* out;               // E_GELU, E_ROWS (operand type), E_VEL (fp32): [M][N]
     void* q;                 // E_QKV: [Bc][2][heads][Fq][64]
     int Fq;
     CarryRef carry;
@@ -200,7 +201,6 @@ struct HeadsParams {
     Carry4 c;                       // base null: no carry
     Spans sp;
     int entries;
-    int out_bf16;
     int splits;                     // set at the launch
 };
 

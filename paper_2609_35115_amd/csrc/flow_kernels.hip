@@ -136,6 +136,8 @@ __device__ __forceinline__ void epilogue4(const GemmParams& p, int row, int col,
 #pragma unroll
         for (int r = 0; r < 4; r++) z[r] = gelu_tanh<BF16>(y[r]);
         store4<BF16>(p.out, (size_t)row * p.N + col, z);
+    } else if constexpr (EPI == E_ROWS) {
+        store4<BF16>(p.out, (size_t)row * p.N + col, y);
     } else if constexpr (EPI == E_VEL) {
         *(f32x4*)((float*)p.out + (size_t)row * p.N + col) = y;
     } else {   // E_QKV
@@ -192,7 +194,7 @@ template <bool BF16, bool LN> __host__ __device__ constexpr int panel_row(int KS
     return (LN ? KS : kStepPad) * (BF16 ? 32 : 16) + (BF16 ? 8 : 4);   // padded: conflict-free 16-byte reads
 }
 
-template <int EPI> constexpr bool ln_operand() { return EPI == E_QKV || EPI == E_GELU || EPI == E_VEL; }
+template <int EPI> constexpr bool ln_operand() { return EPI == E_QKV || EPI == E_GELU || EPI == E_VEL || EPI == E_ROWS; }
 
 constexpr int kBigK = 1024;   // K from which a plain operand's GEMM takes more waves (few rows) or more rows a block
 
@@ -465,7 +467,7 @@ __global__ __launch_bounds__((64 * gemm_waves<MB, NB>()), 2) void gemm_kernel(co
                             for (int e = 0; e < 4; e++) y[e] = gelu_tanh<BF16>(y[e]);
                             store4<BF16>(p.out, at + 16 * j, y);
                         } else {
-                            store4<false>(p.out, at + 16 * j, y);
+                            store4<BF16 && EPI == E_ROWS>(p.out, at + 16 * j, y);
                         }
                     }
                 }
@@ -824,9 +826,9 @@ hipError_t launch_gemm(const GemmParams& p, int epi, int bf16, hipStream_t st)
     if (bf16 == B && epi == E && ln == L) return launch_one<B, E, L>(p, st);
     // the LayerNorm operand exists for exactly the GEMMs that follow one
     DCF_GEMM(1, E_H, false) DCF_GEMM(1, E_QKV, true) DCF_GEMM(1, E_RES, false) DCF_GEMM(1, E_GELU, true)
-    DCF_GEMM(1, E_VEL, true)
+    DCF_GEMM(1, E_VEL, true) DCF_GEMM(1, E_ROWS, true)
     DCF_GEMM(0, E_H, false) DCF_GEMM(0, E_QKV, true) DCF_GEMM(0, E_RES, false) DCF_GEMM(0, E_GELU, true)
-    DCF_GEMM(0, E_VEL, true)
+    DCF_GEMM(0, E_VEL, true) DCF_GEMM(0, E_ROWS, true)
 #undef DCF_GEMM
     return hipErrorInvalidValue;
 }

@@ -137,7 +137,8 @@ struct dc_flow_state {
     int64_t layer4 = 0;          // bytes between (step, block) pairs: all streams' regions
     float *gains = nullptr, *freqs = nullptr;
     // per-call buffers
-    float *qkv = nullptr, *ws = nullptr;   // carry_bits 4: the projection's rows, the attention's workspace
+    void* qkv = nullptr;         // carry_bits 4: the projection's rows (operand type), the attention's workspace
+    float* ws = nullptr;
     int64_t ws_bytes = 0;
     void *xin = nullptr, *o = nullptr, *u = nullptr, *q = nullptr;
     float *h = nullptr, *v = nullptr, *x = nullptr;
@@ -208,14 +209,14 @@ void set_qk(HeadsParams& p, const dc_flow_state* s, int l)
     p.eps = s->opt.qk_eps;
 }
 
-// carry_bits 4: the projection's fp32 rows [rows][3 dim] -> queries in the
-// operand type [rows][dim] and the call's keys and values into the carry.
+// carry_bits 4: the projection's rows [rows][3 dim] -> queries [rows][dim] and the
+// call's keys and values into the carry.
 hipError_t enqueue_store4(const dc_flow_state* s, int i, int l, int b0, int Bc, int n, int prompt, hipStream_t st)
 {
     const int D = s->cfg.dim, heads = s->cfg.heads;
     HeadsParams p{};
     auto part = [&](int k) {
-        return HeadRows{s->qkv + (size_t)k * D, (int64_t)2 * n * 3 * D, 3 * D, 64, heads, (int64_t)n * 3 * D, nullptr, 0, 0};
+        return HeadRows{(char*)s->qkv + (size_t)k * D * s->esz, (int64_t)2 * n * 3 * D, 3 * D, 64, heads, (int64_t)n * 3 * D, nullptr, 0, 0};
     };
     p.q = part(0);
     p.k = part(1);
@@ -223,11 +224,10 @@ hipError_t enqueue_store4(const dc_flow_state* s, int i, int l, int b0, int Bc, 
     p.q_out = HeadRows{s->q, (int64_t)2 * n * D, D, 64, heads, (int64_t)n * D, nullptr, 0, 0};
     set_qk(p, s, l);
     p.wide_in = p.wide_out = 1;
-    p.out_bf16 = s->bf ? 1 : 0;
     p.c = carry4_ref(s, i, l, b0);
     p.sp = spans4(s, b0, n, prompt);
     p.entries = 2 * Bc;
-    return launch_heads(p, 64, 0, st);
+    return launch_heads(p, 64, s->bf ? 1 : 0, st);
 }
 
 // The carry in the operand type: norm and rotation of the queries and of the
@@ -244,7 +244,6 @@ hipError_t enqueue_qk(const dc_flow_state* s, const CarryRef& cr, int l, int b0,
     p.k_out = p.k;
     set_qk(p, s, l);
     p.wide_in = p.wide_out = 1;
-    p.out_bf16 = s->bf ? 1 : 0;
     p.sp = spans4(s, b0, n, prompt);
     p.entries = 2 * Bc;
     return launch_heads(p, 64, s->bf ? 1 : 0, st);
@@ -381,9 +380,9 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
             const double kv_bytes = four ? 34.0 : 64 * es;   // of a head's key or value in the carry
             if (four) {
                 g.out = s->qkv;
-                gemm_cost("gemm:qkv", 3 * D, D, 4, 4, false);
-                DCF_TRY(launch_gemm(g, E_VEL, bf, st));
-                describe("heads", 0, (double)rows * (3 * D * 4 + D * es + 2 * c.heads * kv_bytes), 0);
+                gemm_cost("gemm:qkv", 3 * D, D, 4, es, false);
+                DCF_TRY(launch_gemm(g, E_ROWS, bf, st));
+                describe("heads", 0, (double)rows * (4 * D * es + 2 * c.heads * kv_bytes), 0);
                 DCF_TRY(enqueue_store4(s, i, l, b0, Bc, n, prompt, st));
             } else {
                 gemm_cost("gemm:qkv", 3 * D, D, 4, es, false);
@@ -574,7 +573,7 @@ dc_status dc_flow_init_opt(const void* weights_blob, size_t blob_bytes, const dc
     const size_t o_mel = place((size_t)B * c.f_call * M * 4);
     const size_t o_cond = place((size_t)c.f_prompt * M * 4);
     const size_t o_gather = place((size_t)(c.f_retained + c.f_prompt) * D * 4);
-    const size_t o_qkv = place(four ? (size_t)rows_max * 3 * D * 4 : 0);
+    const size_t o_qkv = place(four ? (size_t)rows_max * 3 * D * es : 0);
     // the attention's workspace: of the call that needs most, chunk calls of
     // all streams and prompt passes of one
     auto ws_most = [&](int entries, int frames) {
@@ -646,7 +645,7 @@ dc_status dc_flow_init_opt(const void* weights_blob, size_t blob_bytes, const dc
     s->gather = (float*)(A + o_gather);
     s->gains = (float*)(A + o_gains);
     s->freqs = (float*)(A + o_freqs);
-    s->qkv = (float*)(A + o_qkv);
+    s->qkv = A + o_qkv;
     s->ws = (float*)(A + o_ws);
     s->carry4.base = (uint8_t*)(A + o_carry);
 

@@ -375,6 +375,81 @@ def test_attend(shape, dtype, ragged):
         assert torch.equal(again[b, :lens[b]], out[b, :lens[b]])
 
 
+def dense(kv, q, at, first, window, causal, sinks, scale=None):
+    """One entry's result and bound, in 64 bits and whole matrices: kv the held
+    values [T][H][D] of positions first .. first + T, q [n][Hq][D] at positions at."""
+    k, v = (x.double().cpu().transpose(0, 1) for x in kv)
+    q = q.double().cpu().transpose(0, 1)
+    H, T, D = k.shape
+    g = q.shape[0] // H
+    key_at, at = torch.arange(first, first + T), torch.as_tensor(at)[:, None]
+    see = (key_at < sinks) | (key_at > at - window if causal else key_at >= at[0] - window)
+    see &= key_at <= at if causal else key_at <= at[-1]
+    scale = D ** -0.5 if scale is None else scale
+    s = (q.unflatten(0, (H, g)) @ k.transpose(-1, -2)[:, None] * scale).masked_fill(~see, -math.inf)
+    out = (torch.softmax(s, -1) @ v[:, None]).flatten(0, 1).transpose(0, 1)
+    e = (D + 8) * 2.0 ** -24 * abs(scale) * (q.abs().unflatten(0, (H, g)) @ k.abs().transpose(-1, -2)[:, None]).amax(-1)
+    bound = (torch.expm1(4 * e) + 4 * (T + 16) * 2.0 ** -24) * v.abs().amax((1, 2))[:, None, None]
+    return out, bound.flatten(0, 1).transpose(0, 1)[..., None], float(v.abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,Hq,H,D,sinks,window,causal,ring", [
+    (1, 1, 2, 1, 64, 0, 3001, True, 3001),        # 16 rows, many splits
+    (1, 1, 8, 8, 128, 4, 1100, True, 1107),       # a few splits
+    (3, 2, 8, 2, 64, 100, 1000, False, 1111),     # splits of a window that wraps
+    (1, 40, 1, 1, 64, 0, 3000, True, 3050),       # 64 rows, splits
+    (1, 300, 4, 2, 128, 7, 2500, True, 3000),
+    (2, 64, 1, 1, 128, 0, 64, False, 128),        # 64 rows exactly, keys in whole tiles
+    (2, 63, 1, 1, 64, 1, 63, True, 126),
+    (4, 16, 6, 2, 64, 3, 90, True, 200),          # 48 rows: shared heads straddle the blocks' waves
+    (32, 200, 8, 8, 64, 5, 70, True, 300),        # 128 rows a block
+    (32, 200, 8, 8, 128, 70, 150, False, 351),
+    (16, 70, 64, 16, 128, 0, 33, True, 128),
+])
+def test_attend_block_shapes(B, n, Hq, H, D, sinks, window, causal, ring, dtype):
+    """Each block shape, splits and their join, of entries at different positions."""
+    m = carry4()
+    c = m.Carry4(B, H, D, sinks=sinks, ring=ring)
+    c.memory.fill_(255)
+    T = sinks + ring + 37   # tokens before the call: past the ring's end
+    k, v = rand((B, T + n, H, D), dtype, 1), rand((B, T + n, H, D), dtype, 2)
+    pos = [T - (b % 3) * 17 for b in range(B)]
+    zero = index([0] * B)
+    c.append(k[:, :T], v[:, :T], zero, lens=index(pos, torch.int32))
+    lens = [n - (b % 4) * (n // 4) for b in range(B)]
+    own = [torch.stack([x[b, pos[b]:pos[b] + n] for b in range(B)]) for x in (k, v)]
+    li = index(lens, torch.int32)
+    c.append(*own, index(pos), lens=li)
+    q = rand((B, n, Hq, D), dtype, 3)
+    out = c.attend(q, index(pos), window, lens=li, causal=causal)
+    for b in sorted({0, 1, B // 2, B - 1}) if B > 1 else [0]:
+        N, L = pos[b] + lens[b], lens[b]
+        want, bound, top = dense((held(k[b, :N]), held(v[b, :N])), q[b, :L], range(pos[b], N), 0, window, causal, sinks)
+        rel = 2.0 ** -8 if dtype == "bf16" else 0.0
+        near(out[b, :L], want, rel, (bound + rel * top * (1 + rel)) * (1 + rel))
+        assert not out[b, L:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 24, 4, 2, 64, 0, 6, True, [0, 30]), (2, 100, 1, 1, 128, 3, 40, True, [0, 3000])])
+def test_attend_nan_of_a_wide_block(shape, dtype):
+    """NaN keys and values in 64-row blocks: the rows and dimensions that see them, no others."""
+    m = carry4()
+    B, n, Hq, H, D, S, w, causal, pos = shape
+
+    def plant(k, v):
+        k[0, 15, 0, 5] = math.nan
+        v[0, n - 1, H - 1, D - 1] = math.inf
+        v[1, 1, 0, 33] = math.nan
+    c, model, lens = turn(m, shape, dtype, 51, before=plant)
+    q = rand((B, n, Hq, D), dtype, 79)
+    got = c.attend(q, index(pos), w)
+    check(got, model, q, shape, dtype, lens)
+    bad = torch.isnan(got).cpu()
+    assert bad[0, 15:min(15 + w, n), 0].all() and not bad[0, :15].any() and not bad[1, 0].any() and bad[1, 1, 0, 32:64].all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attend_masked_nan_and_infinity(dtype):
     """NaN among the keys and values of tokens that some rows see and others do
