@@ -97,6 +97,23 @@ def test_partial_calls_flush_and_new_turn(name):
     dec.close()
 
 
+@pytest.mark.parametrize("shape", [
+    dict(f_retained=0),                                            # the ring holds a call's own frames only
+    dict(f_chunk=1, f_call=1, f_retained=3, f_prompt=1),           # single frames
+    dict(f_chunk=7, f_call=40, f_retained=42, f_prompt=37, heads=1, dim=64),   # a long lookahead, six slots
+    dict(f_chunk=70, f_call=75, f_retained=140, f_prompt=500, depth=1, n_steps=2),   # wide blocks, a prompt longer than the ring
+], ids=["no_history", "single", "lookahead", "long"])
+def test_clock_shapes_match_oracle(shape):
+    a = dict(TINY, **OPTIONS["qk_carry4"], **shape)
+    blob = synth.make_flow_weights(a, 3)
+    calls = [a["f_call"]] * 4 + [max(1, a["f_chunk"] - 1), a["f_chunk"]]
+    dec, outs, mu, prompts = _run_gpu(a, "f32", blob, 2, a["f_prompt"], calls)
+    for b in range(2):
+        s = _check(a, "f32", blob, b, outs, mu[b], prompts[b], calls)
+        _audit(dec, s, a, "f32", b, [(0, 0, 0, 0), (0, 0, 1, 1)])
+    dec.close()
+
+
 @pytest.mark.parametrize("name", ["qk", "carry4", "qk_carry4"])
 def test_replay_equals_direct_and_batch(name):
     flow = _flow()
