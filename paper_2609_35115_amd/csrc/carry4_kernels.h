@@ -2,6 +2,7 @@
 // rotation, the store of keys and values into a carry held in 4 bits, and the
 // attention over it.  Part of flow_kernels.hip (one code object), whose vector
 // types and cross-lane helpers it uses.
+#include "carry4_internal.h"
 
 namespace dcf {
 

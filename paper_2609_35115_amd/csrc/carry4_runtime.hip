@@ -5,8 +5,8 @@
 #include <cmath>
 #include <cstdio>
 
+#include "carry4_internal.h"
 #include "dc_flow.h"
-#include "flow_internal.h"
 
 using namespace dcf;
 

@@ -8,9 +8,10 @@
 // keys and values in place.  Rows never interact outside the attention, and the
 // order of every sum is fixed by the layer and by two switches on the call's
 // size, at 512 rows (the few-row GEMM, which splits K, and the many-row one) and
-// at 64 blocks of 64 queries (the two attention shapes).  Between calls on the
-// same side of both, a stream's result does not depend on the batch or on which
-// other streams share the call.
+// at 64 blocks of 64 queries (the two attention shapes; with the carry in 4 bits,
+// plan4's shapes and splits instead).  Between calls on the same side of both, a
+// stream's result does not depend on the batch or on which other streams share
+// the call.
 #include <type_traits>
 
 #include "dc_philox.h"
@@ -1594,4 +1595,5 @@ hipError_t launch_carry_gather(const CarryRef& c, int b, int branch, int kv, int
 
 }  // namespace dcf
 
+// the attention operators, which run in the same calls (one code object)
 #include "carry4_kernels.h"

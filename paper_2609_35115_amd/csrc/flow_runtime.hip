@@ -12,6 +12,7 @@
 #include <string>
 #include <vector>
 
+#include "carry4_internal.h"
 #include "dc_flow.h"
 #include "flow_internal.h"
 
