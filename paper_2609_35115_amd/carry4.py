@@ -6,7 +6,7 @@ Argument marshalling only, over torch tensors on one GPU; every step runs in
 the gfx950 kernels of libdc.so on the caller's current stream, as a torch
 operation does (a captured call takes the values of pos, lens and sinks at
 each replay).  Arguments that the C call would misread raise DcError before
-anything is launched.
+anything is launched.  For inference: no gradients are recorded.
 """
 from __future__ import annotations
 
@@ -182,7 +182,7 @@ class Carry4:
         carry (which holds the call's own tokens already): the first tokens
         and, causal, the positions in (p - window, p] of a query at p; else
         those in [pos - window, pos + len) for all of an entry's queries.
-        scale: head_dim ** -0.5 by default."""
+        scale: head_dim ** -0.5 by default.  out may be q itself."""
         dt = _dtype(q, "q")
         torch = _torch
         B, n, Hq, _ = q.shape

@@ -146,6 +146,12 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 // cut), and an element is the nearest E2M1 value of x 2^-e, ties to even.
 // Scaling by a power of two is exact, so the codes do not depend on the
 // precision they are computed in.  A group with a NaN or an infinity is NaN.
+//
+// What bounds it: HBM.  Norm and rotation of 32,768 tokens of 40 heads of 128 (671 MB)
+// 139 us, 4.8 TB/s; of 14,336 of 16 heads of 64 16 us.  A load of the next row
+// before this one is worked on, partners by DPP instead of LDS and one reciprocal
+// root took the first from 315 to 161, the block's shared sines to 139.  The store
+// of 16,384 tokens of 8 heads of 128 (85 MB) 23 us.
 // The value of the lane whose number differs by half a row's lanes (D = 64:
 // lane ^ 4; 128: lane ^ 8), without an LDS round trip.
 template <int L> __device__ __forceinline__ float half_row(float v)
@@ -361,18 +367,17 @@ hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
     if (p.c.D == 64) return bf16 ? launch_read4_d<true, 64>(p, st) : launch_read4_d<false, 64>(p, st);
     return bf16 ? launch_read4_d<true, 128>(p, st) : launch_read4_d<false, 128>(p, st);
 }
-template <int D>
+// Eq. carry's order of one (entry, kv), for audits (heads of 64, the flow decoder's).
 __global__ __launch_bounds__(256) void carry4_gather_kernel(const Carry4 c, const Spans spans, int e, int kv, int f_chunk,
                                                             int nh, int frames, float* out)
 {
-    constexpr int L = D / 8;
+    constexpr int D = 64, L = D / 8;
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / L;   // (frame, head)
     const int l = (int)(u % L), f = (int)(row / c.heads), h = (int)(row % c.heads);
     if (f >= frames) return;
     const Span sp(spans, c, e);
     const int64_t at = f < nh * f_chunk ? sp.pos - (int64_t)(f / f_chunk + 1) * f_chunk + f % f_chunk : f - nh * f_chunk;
-    int64_t slot = at < sp.sinks ? at : c.sinks + (at - sp.sinks) % c.ring;
-    slot = slot < 0 ? 0 : slot;
+    const int64_t slot = at < sp.sinks ? max(at, (int64_t)0) : c.sinks + (at - sp.sinks) % c.ring;
     const int N = c.slots();
     const uint8_t* reg = c.base + ((int64_t)e * c.heads + h) * c.region;
     float x[8];
@@ -384,9 +389,9 @@ __global__ __launch_bounds__(256) void carry4_gather_kernel(const Carry4 c, cons
 hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv, int f_chunk, int nh, int frames,
                                 float* out, hipStream_t st)
 {
-    const unsigned blocks = (unsigned)(((int64_t)frames * c.heads * (c.D / 8) + 255) / 256);
-    if (c.D == 64) hipLaunchKernelGGL(carry4_gather_kernel<64>, dim3(blocks), dim3(256), 0, st, c, sp, e, kv, f_chunk, nh, frames, out);
-    else hipLaunchKernelGGL(carry4_gather_kernel<128>, dim3(blocks), dim3(256), 0, st, c, sp, e, kv, f_chunk, nh, frames, out);
+    if (c.D != 64) return hipErrorInvalidValue;
+    const unsigned blocks = (unsigned)(((int64_t)frames * c.heads * 8 + 255) / 256);
+    hipLaunchKernelGGL(carry4_gather_kernel, dim3(blocks), dim3(256), 0, st, c, sp, e, kv, f_chunk, nh, frames, out);
     return hipGetLastError();
 }
 
@@ -412,7 +417,13 @@ hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv,
 // of both halves of the tile; its value fragment, eight keys of one dimension,
 // comes from LDS by transposing reads of the tile's values as bf16.
 // fp32 rows: queries and probabilities as the sum of three bf16 planes, so
-// three products give the fp32 one (keys and values are exact in bf16).
+// three products give the fp32 one (keys and values are exact in bf16).  bf16
+// rows: a probability is rounded to bf16 for the product, half a step of the
+// result's own type; its sum is not.
+//
+// What bounds it: long lists HBM (131,004 keys of 128, 64 regions, 1.14 GB: 224 us,
+// 5.1 TB/s, the rate of a large copy; 242 at three waves a SIMD, the compiler's
+// choice without a bound), short ones latency (458 keys of 64: 7.2 us in a graph).
 constexpr int kKeyTile = 32;
 
 template <int PL> struct Planes { bf16x8_t f[PL]; };
@@ -755,7 +766,15 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
 // only moved when a score passes it by more than 2^8 (a probability's rounding
 // to bf16 is relative, and 2^8 times more fits fp32 with room), so the output
 // is rarely rescaled; in bf16 the probabilities' sum is one more row of the
-// second product (ones), not vector work.
+// second product (ones, so the sum is of the rounded ones), not vector work.
+//
+// What bounds it: the vector unit.  56 queries over 458 keys of 64, 2,048 regions: 35 us
+// (67% of the cycles issue vector work, an exponential taking four; the matrix unit
+// 23%, LDS 49%); 80 where every 16 rows decoded the keys.  A causal prompt of 8,192
+// queries, 4 to a key head of 128, window 4,096: 289 us, 966 TFLOP/s; two waves a
+// SIMD whose vector (46%) and matrix work (39%) overlap only in part.
+// Queries scaled in two bf16 planes, so that scores come ready for the exponential,
+// were slower (38 us); so were waves of 32 rows for the short lists (44).
 constexpr int kWideTile = 64;
 constexpr float kSlack = 8.0f;
 

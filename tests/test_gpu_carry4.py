@@ -589,6 +589,39 @@ def test_captured_step_and_streams():
             torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("B,H,slots", [(1, 1, 1 << 24), (40, 8, 100_000)], ids=["one_region", "many"])
+def test_offsets_past_32_bits(B, H, slots):
+    """One region of 2.3 GB (the largest), and a carry of 4.4 GB: the last slots of the last region."""
+    m = carry4()
+    D, T = 128, 1100 if B == 1 else 6            # (lists of 1,024 keys take the wider blocks also in one region)
+    c = m.Carry4(B, H, D, sinks=0, ring=slots)
+    assert c.bytes > 1 << 31
+    pos = slots - T // 2                         # the last slots, then the first
+    k, v, q = rand((B, T, H, D), "bf16", 1), rand((B, T, H, D), "bf16", 2), rand((B, 6, 7 * H, D), "bf16", 3)
+    at = index([pos] * B)
+    c.append(k, v, at)
+    a, b = c.read(at, T, dtype=torch.bfloat16)
+    assert same(a[-1], held(k[-1:])[0]) and same(b[-1], held(v[-1:])[0])
+    kv = [held(x[-1:])[0] for x in (k, v)]
+    for n in (1, 6):                             # 7 and 42 rows: 16-row and wider blocks
+        first = pos + T - n
+        out = c.attend(q[:, 6 - n:], index([first] * B), T - n, causal=False)   # all T tokens
+        want, bound, top = dense(kv, q[-1, 6 - n:], range(first, pos + T), pos, T - n, False, 0)
+        near(out[-1], want, 2.0 ** -8, (bound + 2.0 ** -8 * top * 1.01) * 1.01)
+
+
+def test_attend_in_place():
+    """Results over their own queries, in each block shape: the same bits."""
+    m = carry4()
+    for B, n, Hq, H, D, w in [(2, 3, 4, 2, 64, 40), (2, 50, 4, 2, 128, 40), (32, 200, 8, 8, 64, 30), (1, 1, 2, 2, 64, 2000)]:
+        c = m.Carry4(B, H, D, sinks=0, ring=w + n)
+        k, pos = rand((B, w + n, H, D), "bf16", 1), index([w] * B)
+        c.append(k, k, index([0] * B))
+        q = rand((B, n, Hq, D), "bf16", 2)
+        want = c.attend(q, pos, w)
+        assert c.attend(q, pos, w, out=q) is q and torch.equal(q, want)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_turn(dtype):
     """A turn as a streaming model runs it: a prompt kept as first tokens, then
