@@ -10,6 +10,8 @@ anything is launched.  For inference: no gradients are recorded.
 """
 from __future__ import annotations
 
+import struct
+import threading
 from ctypes import byref
 
 from . import DC_BF16, DC_EINVAL, DC_F32, DcError
@@ -34,6 +36,22 @@ def _t():
     return _torch
 
 
+class _Frame(threading.local):
+    """A thread's argument structures, filled by one pack a kind: building them
+    anew takes 2 us of a call of four row sets."""
+
+    def __init__(self):
+        self.rows_, self.span_, self.norm_ = bytearray(4 * 40), bytearray(32), bytearray(40)
+        self.rows = [byref(DcHeadRows.from_buffer(self.rows_, 40 * i)) for i in range(4)]
+        self.span, self.norm = byref(DcSpan.from_buffer(self.span_)), byref(DcQkNorm.from_buffer(self.norm_))
+
+
+_frame = _Frame()
+_pack_rows = {n: struct.Struct("@" + n * "Pqqqi4x").pack_into for n in (2, 4)}
+_pack_span = struct.Struct("@PPPii").pack_into
+_pack_norm = struct.Struct("@PPPiif4x").pack_into
+
+
 def _refuse(why: str):
     raise DcError(DC_EINVAL, why)
 
@@ -43,59 +61,65 @@ def _check(status: int):
         raise DcError(status, flib().dc_carry4_last_error().decode())
 
 
-def _rows(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int) -> DcHeadRows:
-    """A row set of x [batch][n][heads][head_dim], in place."""
+def _rows(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int):
+    """The fields of a row set of x [batch][n][heads][head_dim], in place."""
     if x.dtype != dtype or x.device != device:
         _refuse(f"{name} must be {dtype} on {device}, not {x.dtype} on {x.device}")
     shape = x.shape
-    if len(shape) != 4 or shape[0] != batch or shape[1] != n or shape[3] != head_dim or (heads and shape[2] != heads):
+    if len(shape) != 4:
+        _refuse(f"{name} must have four dimensions, not {len(shape)}")
+    b, t, h, d = shape
+    if b != batch or t != n or d != head_dim or (heads and h != heads):
         _refuse(f"{name} must be [{batch}][{n}][{heads or 'heads'}][{head_dim}], not {list(shape)}")
     sb, st, sh, sd = x.stride()
     if sd != 1:
         _refuse(f"{name}: a head's elements must be consecutive")
-    return DcHeadRows(x.data_ptr(), sb, st, sh, shape[2])
+    return x.data_ptr(), sb, st, sh, h
 
 
-def _index(x, name: str, device, dtype, batch: int):
+def _index(x, name: str, device, dtype, batch: int) -> int:
     """Address of a device array [batch] (None: NULL)."""
     if x is None:
-        return None
+        return 0
     if x.dtype != dtype or x.device != device or x.dim() != 1 or x.shape[0] != batch or not x.is_contiguous():
         _refuse(f"{name} must be a contiguous {dtype} tensor [{batch}] on {device}")
     return x.data_ptr()
 
 
-def _span(device, batch: int, n: int, pos, lens, sinks) -> DcSpan:
+def _span(device, batch: int, n: int, pos, lens, sinks):
     torch = _torch
     if pos is None:
         _refuse("pos is None")
-    return DcSpan(_index(pos, "pos", device, torch.int64, batch), _index(lens, "lens", device, torch.int32, batch),
-                  _index(sinks, "sinks", device, torch.int32, batch), batch, n)
+    _pack_span(_frame.span_, 0, _index(pos, "pos", device, torch.int64, batch), _index(lens, "lens", device, torch.int32, batch),
+               _index(sinks, "sinks", device, torch.int32, batch), batch, n)
+    return _frame.span
 
 
-def _norm(device, head_dim: int, freqs, q_gain, k_gain, eps: float, interleaved: bool) -> DcQkNorm:
-    torch = _torch
-    ptr = []
-    for x, name, size in ((q_gain, "q_gain", head_dim), (k_gain, "k_gain", head_dim), (freqs, "freqs", None)):
-        if x is None:
-            ptr.append(None)
-            continue
-        if x.dtype != torch.float32 or x.device != device or x.dim() != 1 or not x.is_contiguous() or (
-                size and x.shape[0] != size):
-            _refuse(f"{name} must be a contiguous float32 tensor{f' [{size}]' if size else ''} on {device}")
-        ptr.append(x.data_ptr())
-    return DcQkNorm(ptr[0], ptr[1], ptr[2], 0 if freqs is None else freqs.shape[0], int(interleaved), eps)
+def _vector(x, name: str, device, size) -> int:
+    """Address of a float32 vector (None: NULL)."""
+    if x is None:
+        return 0
+    if x.dtype != _torch.float32 or x.device != device or x.dim() != 1 or not x.is_contiguous() or (size and x.shape[0] != size):
+        _refuse(f"{name} must be a contiguous float32 tensor{f' [{size}]' if size else ''} on {device}")
+    return x.data_ptr()
+
+
+def _norm(device, head_dim: int, freqs, q_gain, k_gain, eps: float, interleaved: bool):
+    _pack_norm(_frame.norm_, 0, _vector(q_gain, "q_gain", device, head_dim), _vector(k_gain, "k_gain", device, head_dim),
+               _vector(freqs, "freqs", device, None), 0 if freqs is None else freqs.shape[0], int(interleaved), eps)
+    return _frame.norm
 
 
 def _dtype(x, name: str) -> int:
     _t()
-    if x.dtype not in _dtypes:
+    dt = _dtypes.get(x.dtype)
+    if dt is None:
         _refuse(f"{name} must be float32 or bfloat16, not {x.dtype}")
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         _refuse(f"{name} must be on a GPU, not {x.device}")
     if x.dim() != 4:
         _refuse(f"{name} must have four dimensions, not {x.dim()}")
-    return _dtypes[x.dtype]
+    return dt
 
 
 def _launch(device, fn, *args):
@@ -116,17 +140,18 @@ def qk_norm_rope(q, k, pos, freqs, q_gain=None, k_gain=None, eps: float = 1e-6, 
     the two results' tensors, which may be q and k themselves; rows behind
     lens are left as they are (zeros where out is None)."""
     dt = _dtype(q, "q")
-    torch, device = _torch, q.device
+    device, dtype = q.device, q.dtype
     B, n, Hq, D = q.shape
-    a, b = _rows(q, "q", device, q.dtype, B, n, None, D), _rows(k, "k", device, q.dtype, B, n, None, D)
+    a, b = _rows(q, "q", device, dtype, B, n, None, D), _rows(k, "k", device, dtype, B, n, None, D)
     if out is None:
-        new = torch.empty if lens is None else torch.zeros
-        out = (new(q.shape, dtype=q.dtype, device=device), new(k.shape, dtype=q.dtype, device=device))
-    c, d = _rows(out[0], "out[0]", device, q.dtype, B, n, Hq, D), _rows(out[1], "out[1]", device, q.dtype, B, n, k.shape[2], D)
-    m = _norm(device, D, freqs, q_gain, k_gain, eps, interleaved)
-    s = _span(device, B, n, pos, lens, None)
-    _launch(device, flib().dc_qk_norm_rope, byref(m), byref(s), D, dt, byref(a), byref(b), byref(c), byref(d))
-    return tuple(out)
+        new = _torch.empty if lens is None else _torch.zeros
+        out = (new(q.shape, dtype=dtype, device=device), new(k.shape, dtype=dtype, device=device))
+    qo, ko = out
+    c, d = _rows(qo, "out[0]", device, dtype, B, n, Hq, D), _rows(ko, "out[1]", device, dtype, B, n, b[4], D)
+    m, s = _norm(device, D, freqs, q_gain, k_gain, eps, interleaved), _span(device, B, n, pos, lens, None)
+    _pack_rows[4](_frame.rows_, 0, *a, *b, *c, *d)
+    _launch(device, flib().dc_qk_norm_rope, m, s, D, dt, *_frame.rows)
+    return qo, ko
 
 
 class Carry4:
@@ -150,31 +175,33 @@ class Carry4:
     def bytes(self) -> int:
         return self.memory.numel()
 
-    def _kv(self, k, v, what=("k", "v")):
-        dt = _dtype(k, what[0])
+    def _kv(self, k, v):
+        """(dtype, n, fields of k, of v)."""
+        dt, dtype = _dtype(k, "k"), k.dtype
         n = k.shape[1]
-        return dt, n, *(_rows(x, w, self.device, k.dtype, self.batch, n, self.heads, self.head_dim)
-                        for x, w in zip((k, v), what))
+        return (dt, n, _rows(k, "k", self.device, dtype, self.batch, n, self.heads, self.head_dim),
+                _rows(v, "v", self.device, dtype, self.batch, n, self.heads, self.head_dim))
 
     def append(self, k, v, pos, lens=None, sinks=None):
         """Store k, v [batch][n][heads][head_dim] at positions pos[b] + i."""
         dt, n, a, b = self._kv(k, v)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
-        _launch(self.device, flib().dc_carry4_append, self._ref, None, byref(s), dt, None, byref(a), byref(b), None)
+        _pack_rows[2](_frame.rows_, 0, *a, *b)
+        _launch(self.device, flib().dc_carry4_append, self._ref, None, s, dt, None, *_frame.rows[:2], None)
 
     def append_rotated(self, q, k, v, pos, freqs, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
                        lens=None, sinks=None, out=None):
         """qk_norm_rope of q and k and the store of the keys and v in one pass;
         returns the queries."""
         dt, n, a, b = self._kv(k, v)
-        torch = _torch
         r = _rows(q, "q", self.device, k.dtype, self.batch, n, None, self.head_dim)
         if out is None:
-            out = (torch.empty if lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=self.device)
-        o = _rows(out, "out", self.device, k.dtype, self.batch, n, q.shape[2], self.head_dim)
+            out = (_torch.empty if lens is None else _torch.zeros)(q.shape, dtype=q.dtype, device=self.device)
+        o = _rows(out, "out", self.device, k.dtype, self.batch, n, r[4], self.head_dim)
         m = _norm(self.device, self.head_dim, freqs, q_gain, k_gain, eps, interleaved)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
-        _launch(self.device, flib().dc_carry4_append, self._ref, byref(m), byref(s), dt, byref(r), byref(a), byref(b), byref(o))
+        _pack_rows[4](_frame.rows_, 0, *r, *a, *b, *o)
+        _launch(self.device, flib().dc_carry4_append, self._ref, m, s, dt, *_frame.rows)
         return out
 
     def attend(self, q, pos, window: int, lens=None, sinks=None, causal: bool = True, scale: float | None = None, out=None):
@@ -183,28 +210,29 @@ class Carry4:
         and, causal, the positions in (p - window, p] of a query at p; else
         those in [pos - window, pos + len) for all of an entry's queries.
         scale: head_dim ** -0.5 by default.  out may be q itself."""
-        dt = _dtype(q, "q")
-        torch = _torch
-        B, n, Hq, _ = q.shape
-        a = _rows(q, "q", self.device, q.dtype, self.batch, n, None, self.head_dim)
+        dt, dtype = _dtype(q, "q"), q.dtype
+        n = q.shape[1]
+        a = _rows(q, "q", self.device, dtype, self.batch, n, None, self.head_dim)
         if out is None:
-            out = (torch.empty if lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=self.device)
-        o = _rows(out, "out", self.device, q.dtype, self.batch, n, Hq, self.head_dim)
+            out = (_torch.empty if lens is None else _torch.zeros)(q.shape, dtype=dtype, device=self.device)
+        o = _rows(out, "out", self.device, dtype, self.batch, n, a[4], self.head_dim)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
         L = flib()
-        size = L.dc_carry4_workspace(self._ref, Hq, n, window)
-        ws = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
-        _launch(self.device, L.dc_carry4_attend, self._ref, byref(s), dt, byref(a), byref(o), window, int(causal),
+        size = L.dc_carry4_workspace(self._ref, a[4], n, window)
+        # (held until both launches are on the stream: another thread may take freed memory at once)
+        ws = _torch.empty(size, dtype=_torch.uint8, device=self.device) if size else None
+        _pack_rows[2](_frame.rows_, 0, *a, *o)
+        _launch(self.device, L.dc_carry4_attend, self._ref, s, dt, *_frame.rows[:2], window, int(causal),
                 self.head_dim ** -0.5 if scale is None else scale, ws.data_ptr() if size else None, size)
         return out
 
     def read(self, pos, n: int, lens=None, sinks=None, dtype=None):
         """(k, v) [batch][n][heads][head_dim]: the values held for positions
         pos[b] + i (float32 or bfloat16, exact in both)."""
-        torch = _t()
-        new = torch.empty if lens is None else torch.zeros
-        k, v = (new((self.batch, n, self.heads, self.head_dim), dtype=dtype or torch.float32, device=self.device) for _ in "kv")
+        new = _t().empty if lens is None else _torch.zeros
+        k, v = new((2, self.batch, n, self.heads, self.head_dim), dtype=dtype or _torch.float32, device=self.device)
         dt, n, a, b = self._kv(k, v)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
-        _launch(self.device, flib().dc_carry4_read, self._ref, byref(s), dt, byref(a), byref(b))
+        _pack_rows[2](_frame.rows_, 0, *a, *b)
+        _launch(self.device, flib().dc_carry4_read, self._ref, s, dt, *_frame.rows[:2])
         return k, v
