@@ -216,7 +216,8 @@ void dc_flow_free(dc_flow_state* s);
  * negatives) with one scale for 32 consecutive dimensions: 2^e, e the least
  * integer in [-126, 126] for which 6 * 2^e is at least the group's largest
  * magnitude; ties to the even code.  4.25 bits a value.  A group with a NaN
- * or an infinity is held as NaN.
+ * or an infinity is held as NaN (and a magnitude of 3.5 * 2^126 and more, which
+ * rounds to 2^128, as an infinity).
  *
  * Every call is launched on hip_stream, a stream of the current device, and
  * returns without waiting; nothing is allocated, so calls can be captured.
@@ -268,7 +269,8 @@ typedef struct dc_qk_norm {
 
 /* q_out, k_out = norm and rotation of q, k (head_dim 64 or 128, dtype DC_F32
  * or DC_BF16; sums in fp32, one rounding).  An output may be its input (the
- * same rows); otherwise rows may not overlap. */
+ * same rows); otherwise rows may not overlap.  A row's mean square plus eps has
+ * to be a normal fp32 number: larger rows give 0, smaller ones infinities. */
 dc_status dc_qk_norm_rope(const dc_qk_norm* norm, const dc_span* span, int32_t head_dim, int32_t dtype,
                           const dc_head_rows* q, const dc_head_rows* k, const dc_head_rows* q_out,
                           const dc_head_rows* k_out, void* hip_stream);

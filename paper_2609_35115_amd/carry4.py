@@ -18,6 +18,7 @@ from . import DC_BF16, DC_EINVAL, DC_F32, DcError
 from .flow import DcCarry4, DcHeadRows, DcQkNorm, DcSpan, flib
 
 DC_CARRY4_ABI_VERSION = 1
+_INT32 = 2 ** 31 - 1   # ctypes cuts integers to their field without a word
 
 _torch = None
 _dtypes = {}
@@ -161,6 +162,8 @@ class Carry4:
 
     def __init__(self, batch: int, heads: int, head_dim: int, sinks: int, ring: int, device=None):
         torch = _t()
+        if not all(0 <= x <= _INT32 for x in (batch, heads, head_dim, sinks, ring)):
+            _refuse("batch, heads, head_dim, sinks and ring must be in [0, 2^31)")
         self.batch, self.heads, self.head_dim, self.sinks, self.ring = batch, heads, head_dim, sinks, ring
         self.c = DcCarry4(DC_CARRY4_ABI_VERSION, batch, heads, head_dim, sinks, ring, None)
         size = flib().dc_carry4_bytes(byref(self.c))
@@ -211,6 +214,8 @@ class Carry4:
         those in [pos - window, pos + len) for all of an entry's queries.
         scale: head_dim ** -0.5 by default.  out may be q itself."""
         dt, dtype = _dtype(q, "q"), q.dtype
+        if not 0 <= window <= _INT32:
+            _refuse(f"window must be in [0, 2^31), not {window}")
         n = q.shape[1]
         a = _rows(q, "q", self.device, dtype, self.batch, n, None, self.head_dim)
         if out is None:

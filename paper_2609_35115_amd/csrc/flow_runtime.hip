@@ -250,7 +250,8 @@ hipError_t enqueue_qk(const dc_flow_state* s, const CarryRef& cr, int l, int b0,
     return launch_heads(p, 64, s->bf ? 1 : 0, st);
 }
 
-hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc, int n, int prompt, hipStream_t st)
+hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc, int n, int prompt, hipStream_t st,
+                           int* launches)
 {
     const int D = s->cfg.dim, heads = s->cfg.heads;
     Attend4Params p{};
@@ -267,6 +268,7 @@ hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc,
     int64_t need = 0;
     p.splits = attend4_splits(p.c, p.entries, n, 1, p.window, &need);
     if (need > s->ws_bytes) return hipErrorInvalidValue;
+    *launches = p.splits > 1 ? 2 : 1;   // the join
     p.ws = s->ws;
     return launch_attend4(p, s->bf ? 1 : 0, st);
 }
@@ -398,8 +400,13 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
             // per (stream, branch, head): n queries x its keys x 64, twice (scores, values)
             describe("attn", 4.0 * 2 * c.heads * 64 * (double)n * ext_keys,
                      2.0 * 2 * c.heads * (double)ext_keys * kv_bytes + 2.0 * rows * D * es, 1);
-            if (four) DCF_TRY(enqueue_attend4(s, i, l, b0, Bc, n, prompt, st));
-            else DCF_TRY(launch_attn(at, Bc, bf, st));
+            if (four) {
+                int launches = 1;
+                DCF_TRY(enqueue_attend4(s, i, l, b0, Bc, n, prompt, st, &launches));
+                k += launches - 1;
+            } else {
+                DCF_TRY(launch_attn(at, Bc, bf, st));
+            }
             plain(s->o);
             g.W = s->w_o[l];
             g.bias = s->b_o[l];

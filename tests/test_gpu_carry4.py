@@ -553,13 +553,14 @@ def test_attend_does_not_depend_on_the_other_entries():
     assert torch.equal(c.attend(q2, p2, 40, out=torch.zeros_like(q))[3:], want[3:])
 
 
-def test_captured_step_and_streams():
+@pytest.mark.parametrize("w", [40, 2500], ids=["short", "split"])
+def test_captured_step_and_streams(w):
     """A serving step (norm and rotation into the carry, attention) captured
     once and replayed with other positions and inputs, on a stream of its own,
     against the same calls made eagerly on another carry, with eager work and
     synchronisations between; two graphs captured from one pool."""
     m = carry4()
-    B, n, Hq, H, D, S, w = 2, 1, 4, 2, 64, 3, 40
+    B, n, Hq, H, D, S = 2, 1, 4, 2, 64, 3
     freqs = torch.linspace(1, 0.01, 32).cuda()
     a, b = (m.Carry4(B, H, D, sinks=S, ring=w + n) for _ in range(2))
     x, pos = torch.empty(B, n, Hq + 2 * H, D, device="cuda", dtype=torch.bfloat16), index([0, 0])
@@ -655,6 +656,7 @@ def test_refusals_on_the_gpu():
                  lambda: c.append(k.transpose(2, 3), k.transpose(2, 3), pos), lambda: c.append(k, k, None),
                  lambda: c.attend(k, pos, 8), lambda: c.attend(k, pos, 0), lambda: c.attend(k[:, :, :1], pos, 2),
                  lambda: c.attend(k, pos, 7, causal=False), lambda: c.attend(k, pos, 2, scale=math.inf),
+                 lambda: c.attend(k, pos, 2 ** 32 + 3), lambda: m.Carry4(2, 2, 64, sinks=0, ring=2 ** 32 + 8),
                  lambda: m.Carry4(2, 2, 96, sinks=0, ring=8), lambda: m.Carry4(2, 2, 64, sinks=0, ring=0),
                  lambda: m.qk_norm_rope(k, k, pos, torch.ones(4, device="cuda")),
                  lambda: m.qk_norm_rope(k, k, pos, torch.ones(40, device="cuda")),
