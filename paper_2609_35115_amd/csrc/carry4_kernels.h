@@ -2,6 +2,8 @@
 // rotation, the store of keys and values into a carry held in 4 bits, and the
 // attention over it.  Part of flow_kernels.hip (one code object), whose vector
 // types and cross-lane helpers it uses.
+#include <algorithm>
+
 #include "carry4_internal.h"
 
 namespace dcf {
@@ -1117,13 +1119,20 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     in 64-row blocks 103; 60 rows, 256 regions, 560 keys 25 and 17), and for
 //     fewer than 32 wider blocks of short lists (56 rows, 16 regions, 458 keys: 9.0
 //     and 9.8);
-//   128 rows from two blocks a CU on (16,384 rows, 4 regions, 4,100 keys of 128:
-//     148, in 64-row blocks 197, in 256-row ones 146; 256 rows, 64 regions, 1,000
-//     keys: 35, 24 and 53);
-//   splits for up to 512 blocks of 16 rows or 256 wider ones, of 256 and 512 keys
-//     at least: the join is a launch of its own, about 3 us (2,000 keys, 8
-//     regions 9.6 split in 7, 17.9 unsplit; 458 keys 7.6 unsplit, 9.0 in two; 56
-//     rows, 256 blocks 16.3 unsplit, 25.5 in two).
+//   128 rows from 1.5 blocks a CU on, its own splits included (16,384 rows, 4
+//     regions, 4,100 keys of 128: 148, in 64-row blocks 197, in 256-row ones 146;
+//     101 rows, 215 regions, 3,230 keys: 73 and 86; 256 rows, 64 regions, 1,000
+//     keys: 27, 18 and 53);
+//   splits: the join is a launch of its own, about 2 us, which grows with them.
+//     16 rows: for a block a CU, of 128 keys or more (2,000 keys, 8 regions 8.4,
+//     of 256 9.2, unsplit 16.9; 458 keys 7.2 unsplit, 8.1 split); all of two
+//     blocks a CU where that leaves 448 (8,000 keys of 128, 32 regions 16.5, one a
+//     CU 17.4; 19,000, 8 regions 15.8 and 14.0); up to eight a CU of 1,024, as
+//     rounds of blocks come out more even (17,400 keys, 200 regions 63 in ten, 85
+//     in two, 116 unsplit), in 32 splits at most;
+//     wider: for a block a CU of 512 keys, or two of 1,024 (20,000 keys of 128, 32
+//     regions 44 and 51; 56 rows, 256 blocks 16.3 unsplit, 25.5 in two; 2,100
+//     keys, 32 regions of 128 rows 20.4 and, in two a CU, 25.5).
 struct Plan4 {
     int rows;     // query rows of a block: 16 (one set for four waves), 64 or 128 (16 or 32 a wave)
     int splits;
@@ -1132,15 +1141,18 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
 {
     const int64_t rows = (int64_t)n * group, regions = (int64_t)entries * c.heads;
     const int64_t most = (int64_t)c.sinks + (window < c.ring ? window : c.ring) + n;   // keys of a list
-    Plan4 pl;
-    if (rows <= 32 || (regions * ((rows + 63) / 64) < 32 && most < 1024)) pl.rows = 16;
-    else pl.rows = rows > 96 && regions * ((rows + 127) / 128) >= 512 ? 128 : 64;
-    const int64_t blocks = regions * ((rows + pl.rows - 1) / pl.rows);
-    int64_t s = (pl.rows == 16 ? 512 : 256) / (blocks > 0 ? blocks : 1);
-    const int64_t most_splits = most / (pl.rows == 16 ? 256 : 512);
-    if (s > most_splits) s = most_splits;
-    pl.splits = s < 1 ? 1 : (int)s;
-    return pl;
+    const int64_t in16 = regions * ((rows + 15) / 16), in64 = regions * ((rows + 63) / 64),
+                  in128 = regions * ((rows + 127) / 128);
+    // the most splits that make up to `blocks` blocks of `of` and leave each `keys` keys or more
+    auto split = [&](int64_t of, int64_t blocks, int64_t keys) { return std::max((int64_t)1, std::min(blocks / of, most / keys)); };
+    if (rows <= 32 || (in64 < 32 && most < 1024)) {
+        const int64_t two = 512 / in16;
+        const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), std::min((int64_t)32, split(in16, 2048, 1024)));
+        return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
+    }
+    const int64_t s = split(in128, 512, 1024);
+    if (rows > 96 && in128 * s >= 384) return {128, (int)s};
+    return {64, (int)std::max(split(in64, 256, 512), split(in64, 512, 1024))};
 }
 
 int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes)
