@@ -64,7 +64,7 @@ struct HeadsParams {
     Carry4 c;                       // base null: no carry
     Spans sp;
     int entries;
-    int splits;                     // set at the launch
+    int waves, splits;              // set at the launch
 };
 
 struct Attend4Params {

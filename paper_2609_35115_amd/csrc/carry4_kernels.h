@@ -131,9 +131,9 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 
 // ------------------------------- norms, rotation and the store into the carry
 //
-// D / 8 lanes hold a head's row, eight consecutive elements each, and a block's
-// four waves the same 64 / (D / 8) tokens, whose heads they share out; so the
-// cosines and sines of a lane's token and dimensions are computed once for all
+// D / 8 lanes hold a head's row, eight consecutive elements each, and `waves` of
+// a block's four waves the same 64 / (D / 8) tokens, whose heads they share out;
+// so the cosines and sines of those tokens' 256 angles are computed once for all
 // of the block's heads.
 //
 // y = x / sqrt(mean(x^2) + eps) gain, sums in fp32.  The angle position *
@@ -167,40 +167,49 @@ template <bool BF16, int D>
 __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
 {
     constexpr int L = D / 8, TPW = 64 / L;   // lanes of a row, tokens of a wave
-    __shared__ __align__(16) float turn[2][64][8];   // cosines, sines
-    const int lane = threadIdx.x & 63, l = lane % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __align__(16) float turn[4][2][TPW][D / 2];   // of each group: cosines, sines
+    const int lane = threadIdx.x & 63, l = lane % L;
+    // `waves` waves work on a group of tokens, wave `wave` of group `group` of the block's
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.waves;
+    const int wave = all & (waves - 1), group = all / waves;
     const int n = p.sp.n;
     const int64_t tokens = (int64_t)p.entries * n;
-    const int64_t t = (int64_t)(blockIdx.x / p.splits) * TPW + lane / L;
+    const int64_t t = ((int64_t)(blockIdx.x / p.splits) * (4 / waves) + group) * TPW + lane / L;
     const int e = (int)(min(t, tokens - 1) / n), i = (int)(min(t, tokens - 1) % n);
     const Span sp(p.sp, p.c, e);
     const bool on = t < tokens && i < sp.len;
     const int64_t pos = sp.pos + i;
 
     const int jobs = p.q.heads + p.k.heads + p.v.heads;
-    const int part = 4 * (blockIdx.x % p.splits) + wave, parts = 4 * p.splits;
+    const int part = waves * (blockIdx.x % p.splits) + wave, parts = waves * p.splits;
     const int j0 = (int)((int64_t)jobs * part / parts), j1 = (int)((int64_t)jobs * (part + 1) / parts);
 
-    // the rotation of this lane's dimensions (identity past rot), a quarter by
-    // each wave
+    // the rotation of this lane's dimensions (identity past rot): a group's 256
+    // angles are shared out over its lanes
     float cs[8], sn[8];
     const bool inter = p.interleaved != 0;
     const int half = p.rot >> 1;
     const bool first = 8 * l < half;                     // half-split pairs: this lane holds the pairs' first members
     if (p.norm && p.rot) {
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const int j = 2 * wave + k, d = 8 * l + j, f = inter ? d >> 1 : first ? d : d - half;
+        for (int a = wave; a < 4; a += waves) {
+            const int u = 64 * a + lane, f = u % (D / 2), of = u / (D / 2);
+            const int64_t at = ((int64_t)__shfl((int)(pos >> 32), of * L) << 32) | (uint32_t)__shfl((int)pos, of * L);
             float c = 1.0f, s = 0.0f;
-            if (d < p.rot) sincospif(2.0f * turn_fraction(pos, p.freqs[f]), &s, &c);
-            turn[0][lane][j] = c;
-            turn[1][lane][j] = !inter && first ? -s : s;   // the sign that the pair's other member enters with
+            if (f < half) sincospif(2.0f * turn_fraction(at, p.freqs[f]), &s, &c);
+            turn[group][0][of][f] = c;
+            turn[group][1][of][f] = s;
         }
         __syncthreads();
+        const int f0 = (inter ? 4 * l : first ? 8 * l : 8 * l - half) & (D / 2 - 1), f4 = (f0 + 4) & (D / 2 - 1);
+        const float *c = turn[group][0][lane / L], *s = turn[group][1][lane / L];
+        const f32x4 ca = *(const f32x4*)(c + f0), cb = *(const f32x4*)(c + f4);
+        const f32x4 sa = *(const f32x4*)(s + f0), sb = *(const f32x4*)(s + f4);
+        const float sign = !inter && first ? -1.0f : 1.0f;   // that the pair's other member enters with
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            cs[j] = turn[0][lane][j];
-            sn[j] = turn[1][lane][j];
+            const bool on = 8 * l + j < p.rot;
+            cs[j] = !on ? 1.0f : inter ? ca[j >> 1] : j < 4 ? ca[j & 3] : cb[j & 3];
+            sn[j] = !on ? 0.0f : sign * (inter ? sa[j >> 1] : j < 4 ? sa[j & 3] : sb[j & 3]);
         }
     }
     const int partner = (lane & ~(L - 1)) | ((8 * l < p.rot ? (first ? l + half / 8 : l - half / 8) : l) & (L - 1));
@@ -294,11 +303,17 @@ template <bool BF16, int D> hipError_t launch_heads_d(HeadsParams p, hipStream_t
     const int jobs = p.q.heads + p.k.heads + p.v.heads;
     // a block walks all heads of its tokens unless that leaves fewer than two blocks
     // a CU (14,336 rows of 16 heads: 16.3 us, 28.7 with four times the blocks; 4,011
-    // of 12: 11.2 and 20.6)
+    // of 12: 11.2 and 20.6).  Where the groups alone fill the card, a wave walks
+    // three heads or more: what it does once a token (angles, the place in the carry)
+    // costs as much as a few rows (us with one, two and four waves a group: 2
+    // rows, 74,046 tokens 21, 22 and 28; 6, 13,146 18, 17 and 23; 40, 32,768 -,
+    // 146 and 136; but 10 waves or fewer in all, 4.6 with four and 6.6 with one).
     int64_t splits = 1;
+    p.waves = groups < 1024 || jobs > 16 ? 4 : jobs > 4 ? 2 : 1;
     while (4 * splits < jobs && groups * splits < 512) splits *= 2;
     p.splits = (int)splits;
-    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)(groups * splits)), dim3(256), st, p);
+    const int64_t per = 4 / p.waves;   // groups of a block
+    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)((groups + per - 1) / per * splits)), dim3(256), st, p);
 }
 
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st)
