@@ -1131,9 +1131,10 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 // Which kernel an attention call takes, and over how many blocks its keys are
 // split.  Us of a call in a graph, bf16, both sides of each border:
 //   16 rows a block up to 32 rows (20 rows, 256 regions, 3,025 keys of 128: 50,
-//     in 64-row blocks 103; 60 rows, 256 regions, 560 keys 25 and 17), and for
-//     fewer than 32 wider blocks of short lists (56 rows, 16 regions, 458 keys: 9.0
-//     and 9.8);
+//     in 64-row blocks 103; 60 rows, 256 regions, 560 keys 25 and 17), and for as
+//     many keys in all as a block of 832 on each CU visits (40 rows, 64 regions, 540
+//     keys: 8.2 and 11.1; 128 rows, 32 regions, 828 keys of 128: 12.1 and 15.3; 36
+//     rows, 88 regions, 836 keys: 16.6 and 15.7);
 //   128 rows from 1.5 blocks a CU on, its own splits included (16,384 rows, 4
 //     regions, 4,100 keys of 128: 148, in 64-row blocks 197, in 256-row ones 146;
 //     101 rows, 215 regions, 3,230 keys: 73 and 86; 256 rows, 64 regions, 1,000
@@ -1145,8 +1146,8 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     CU 17.4; 19,000, 8 regions 15.8 and 14.0); up to eight a CU of 1,024, as
 //     rounds of blocks come out more even (17,400 keys, 200 regions 63 in ten, 85
 //     in two, 116 unsplit), in 32 splits at most;
-//     wider: for a block a CU of 512 keys, or two of 1,024 (20,000 keys of 128, 32
-//     regions 44 and 51; 56 rows, 256 blocks 16.3 unsplit, 25.5 in two; 2,100
+//     wider: for a block a CU of 256 keys, or two of 1,024 (836 keys of 128, 88
+//     regions 15.7 in two, 19.0 unsplit; 20,000, 32 regions 43 and 51; 56 rows, 256 blocks 16.3 unsplit, 25.5 in two; 2,100
 //     keys, 32 regions of 128 rows 20.4 and, in two a CU, 25.5).
 struct Plan4 {
     int rows;     // query rows of a block: 16 (one set for four waves), 64 or 128 (16 or 32 a wave)
@@ -1160,14 +1161,14 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
                   in128 = regions * ((rows + 127) / 128);
     // the most splits that make up to `blocks` blocks of `of` and leave each `keys` keys or more
     auto split = [&](int64_t of, int64_t blocks, int64_t keys) { return std::max((int64_t)1, std::min(blocks / of, most / keys)); };
-    if (rows <= 32 || (in64 < 32 && most < 1024)) {
+    if (rows <= 32 || in16 * most <= 256 * 832) {
         const int64_t two = 512 / in16;
         const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), std::min((int64_t)32, split(in16, 2048, 1024)));
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
     }
     const int64_t s = split(in128, 512, 1024);
     if (rows > 96 && in128 * s >= 384) return {128, (int)s};
-    return {64, (int)std::max(split(in64, 256, 512), split(in64, 512, 1024))};
+    return {64, (int)std::max(split(in64, 256, 256), split(in64, 512, 1024))};
 }
 
 int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes)
