@@ -445,19 +445,34 @@ constexpr int kKeyTile = 32;
 
 template <int PL> struct Planes { bf16x8_t f[PL]; };
 
+// The high halves of eight fp32 words.
+__device__ __forceinline__ bf16x8_t high8(const uint32_t (&y)[8])
+{
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) r[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x07060302u);
+    return __builtin_bit_cast(bf16x8_t, r);
+}
+
+// x rounded to bf16, or whole in three planes: eight of its bits each, cut off
+// one after the other (rounded planes take a conversion more: fp32 calls of the wide
+// kernel 5 to 9% slower).
 template <int PL> __device__ __forceinline__ Planes<PL> split8(const float (&x)[8])
 {
     Planes<PL> r;
-    float y[8];
+    if constexpr (PL == 1) {
 #pragma unroll
-    for (int j = 0; j < 8; j++) y[j] = x[j];
+        for (int j = 0; j < 8; j++) r.f[0][j] = (__bf16)x[j];
+    } else {
+        uint32_t y[8];
 #pragma unroll
-    for (int k = 0; k < PL; k++) {
+        for (int j = 0; j < 8; j++) y[j] = __float_as_uint(x[j]);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const __bf16 b = (__bf16)y[j];
-            r.f[k][j] = b;
-            if (k + 1 < PL) y[j] -= (float)b;
+        for (int k = 0; k < PL; k++) {
+            r.f[k] = high8(y);
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                y[j] = __float_as_uint(__uint_as_float(y[j]) - __uint_as_float(y[j] & 0xffff0000u));
         }
     }
     return r;
@@ -584,10 +599,34 @@ template <int D> struct Running {
     uint32_t bad;   // groups of 32 dimensions in which a visible value is NaN
 };
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_kernel(const Attend4Params p)
+// The plane that a lane of column group `plane` holds (the fourth is zero).
+__device__ __forceinline__ bf16x8_t plane8(const float (&x)[8], int plane)
 {
-    constexpr int PL = BF16 ? 1 : 3, KS = D / 32, DB = D / 16;
+    uint32_t y[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        float v = x[j];
+#pragma unroll
+        for (int k = 0; k < 3; k++) v -= __uint_as_float(__float_as_uint(v) & (k < plane ? 0xffff0000u : 0u));
+        y[j] = __float_as_uint(v);
+    }
+    return high8(y);
+}
+// The sum of a row of 16 lanes' four quads, in every quad.
+__device__ __forceinline__ float sum_quads(float v)
+{
+    v += __uint_as_float(dpp<0x128>(__float_as_uint(v)));          // row_ror:8
+    return v + __uint_as_float(dpp<0x124>(__float_as_uint(v)));    // row_ror:4
+}
+
+// FOLD: calls of up to four fp32 rows.  The planes of a row are columns of one
+// product instead of products of their own (column 4 k + q: plane k of row q), and
+// meet after it (one token, 20,000 keys of 128, 144 regions: 120 -> 91 us, bf16
+// rows 83; 11,800 of 64, 135 regions 49 -> 43 and 36).
+template <bool BF16, int D, bool FOLD>
+__global__ __launch_bounds__(256, !BF16 && !FOLD ? 1 : D == 128 ? 4 : 5) void attend4_kernel(const Attend4Params p)
+{
+    constexpr int PL = BF16 || FOLD ? 1 : 3, KS = D / 32, DB = D / 16, RB = FOLD ? 4 : 16;
     constexpr int VROW = 2 * D + 32;   // bytes of a value row in LDS: eight banks on from row to row
     constexpr int WAVE_LDS = kKeyTile * VROW > 16 * D * 4 + 128 ? kKeyTile * VROW : 16 * D * 4 + 128;
     __shared__ __align__(16) unsigned char smem[4 * WAVE_LDS];
@@ -597,11 +636,11 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
     const int regions = p.entries * p.c.heads, split = blockIdx.x % p.splits;
     const int eh = blockIdx.x / p.splits % regions, e = eh / p.c.heads, h = eh % p.c.heads;
     const Span sp(p.sp, p.c, e);
-    const int rows = sp.len * p.group, row0 = 16 * (blockIdx.x / p.splits / regions);
+    const int rows = sp.len * p.group, row0 = RB * (blockIdx.x / p.splits / regions);
     if (row0 >= rows) return;                       // (uniform: the block's rows are behind the entry's last token)
-    const int last = min(row0 + 15, rows - 1);
+    const int last = min(row0 + RB - 1, rows - 1), my_row = min(row0 + r % RB, rows - 1);
     const KeyList list(p, sp, row0 / p.group, last / p.group);
-    const RowSpan mine = list.row(p, sp, min(row0 + r, rows - 1) / p.group);
+    const RowSpan mine = list.row(p, sp, my_row / p.group);
     const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
     const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;   // members visible to every row
     const int N = p.c.slots();
@@ -610,13 +649,14 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
     // queries as B operand: lane (q, g) holds dimensions g D / 4 + 8 c .. + 7
     Planes<PL> qf[KS];
     {
-        const int row = min(row0 + r, rows - 1), i = row / p.group, hq = h * p.group + row % p.group;
+        const int i = my_row / p.group, hq = h * p.group + my_row % p.group;
         const int64_t at = p.q.at(p.sp.div, e, i, hq) + g * (D / 4);
 #pragma unroll
         for (int c = 0; c < KS; c++) {
             float x[8];
             load8<BF16>(p.q.p, at + 8 * c, p.wide_in, x);
-            qf[c] = split8<PL>(x);
+            if constexpr (FOLD) qf[c].f[0] = plane8(x, r >> 2);
+            else qf[c] = split8<PL>(x);
         }
     }
 
@@ -675,6 +715,7 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
+                if constexpr (FOLD) s[b][i] = sum_quads(s[b][i]);
                 s[b][i] *= p.scale_log2;
                 const int key = t0 + 16 * b + 4 * g + i;
                 const bool see = open | mine.sees(key);
@@ -700,7 +741,9 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
                 sum += pr[4 * b + i];
             }
         acc.l = acc.l * alpha + sum;   // this lane's keys; the lanes of a query are summed at the end
-        const Planes<PL> pf = split8<PL>(pr);
+        Planes<PL> pf;
+        if constexpr (FOLD) pf.f[0] = plane8(pr, r >> 2);
+        else pf = split8<PL>(pr);
         // (the wave's own region: its LDS operations complete in order)
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -716,6 +759,12 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
             for (int k = PL - 1; k >= 0; k--) acc.o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf.f[k], acc.o[b], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();
+    }
+    if constexpr (FOLD) {
+#pragma unroll
+        for (int b = 0; b < DB; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) acc.o[b][i] = sum_quads(acc.o[b][i]);
     }
     acc.l = sum_xor16_32(acc.l);
     acc.bad = or_xor16_32(acc.bad);
@@ -736,7 +785,7 @@ __global__ __launch_bounds__(256, !BF16 ? 1 : D == 128 ? 4 : 5) void attend4_ker
     }
     __syncthreads();
     constexpr int CH = D / 4;                         // four dimensions a thread
-    for (int u = threadIdx.x; u < 16 * CH; u += 256) {
+    for (int u = threadIdx.x; u < RB * CH; u += 256) {
         const int q = u / CH, d = 4 * (u % CH);
         if (row0 + q > last) continue;
         float m = -INFINITY, l = 0.0f;
@@ -1143,9 +1192,10 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     16 rows: for a block a CU, of 128 keys or more (2,000 keys, 8 regions 8.4,
 //     of 256 9.2, unsplit 16.9; 458 keys 7.2 unsplit, 8.1 split); all of two
 //     blocks a CU where that leaves 448 (8,000 keys of 128, 32 regions 16.5, one a
-//     CU 17.4; 19,000, 8 regions 15.8 and 14.0); up to eight a CU of 1,024, as
-//     rounds of blocks come out more even (17,400 keys, 200 regions 63 in ten, 85
-//     in two, 116 unsplit), in 32 splits at most;
+//     CU 17.4; 19,000, 8 regions 15.8 and 14.0); from fewer than two
+//     a CU, up to eight of 1,024 in 32 splits, so that a CU always holds its four
+//     or five (17,400 keys, 200 regions 63 in ten, 85 in two, 116 unsplit; 7,600,
+//     492 regions 65 in four, 72; but 5,200 of 128, 707 regions 105 in two, 100);
 //     wider: for a block a CU of 256 keys, or two of 1,024 (836 keys of 128, 88
 //     regions 15.7 in two, 19.0 unsplit; 20,000, 32 regions 43 and 51; 56 rows, 256 blocks 16.3 unsplit, 25.5 in two; 2,100
 //     keys, 32 regions of 128 rows 20.4 and, in two a CU, 25.5).
@@ -1163,7 +1213,7 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
     auto split = [&](int64_t of, int64_t blocks, int64_t keys) { return std::max((int64_t)1, std::min(blocks / of, most / keys)); };
     if (rows <= 32 || in16 * most <= 256 * 832) {
         const int64_t two = 512 / in16;
-        const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), std::min((int64_t)32, split(in16, 2048, 1024)));
+        const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), in16 > 512 ? 1 : std::min((int64_t)32, split(in16, 2048, 1024)));
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
     }
     const int64_t s = split(in128, 512, 1024);
@@ -1186,7 +1236,8 @@ template <bool BF16, int D> hipError_t launch_attend4_d(const Attend4Params& p, 
     if (!BF16 && rb == 128) rb = 64;   // (three planes of 32 rows do not fit the registers)
     const dim3 grid((unsigned)((int64_t)p.splits * p.entries * p.c.heads * ((rows + rb - 1) / rb)));
     hipError_t e = hipErrorInvalidValue;
-    if (rb == 16) e = launch_with(attend4_kernel<BF16, D>, grid, dim3(256), st, p);
+    if (rb == 16 && !BF16 && rows <= 4) e = launch_with(attend4_kernel<BF16, D, !BF16>, grid, dim3(256), st, p);
+    else if (rb == 16) e = launch_with(attend4_kernel<BF16, D, false>, grid, dim3(256), st, p);
     else if (rb == 64 || !BF16) e = launch_with(attend4_wide<BF16, D, 1, 4>, grid, dim3(256), st, p);
     else if constexpr (BF16) e = launch_with(attend4_wide<BF16, D, 2, 4>, grid, dim3(256), st, p);
     if (e != hipSuccess || p.splits == 1) return e;
