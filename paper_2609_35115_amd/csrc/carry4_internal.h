@@ -45,9 +45,9 @@ struct HeadRows {
     int row0, row_step;
     __device__ __forceinline__ int64_t at(int div, int e, int i, int h) const
     {
-        const int b = e / div;
+        const int b = div == 1 ? e : e / div;
         const int64_t row = (int64_t)i + row0 + (slot ? (int64_t)slot[b] * row_step : 0);
-        return b * sb + (e % div) * sc + row * st + h * sh;
+        return b * sb + (e - b * div) * sc + row * st + h * sh;
     }
 };
 
@@ -64,7 +64,7 @@ struct HeadsParams {
     Carry4 c;                       // base null: no carry
     Spans sp;
     int entries;
-    int waves, splits;              // set at the launch
+    int waves, split_bits, share;   // set at the launch: waves of a token group, blocks (a power of two), rows of a wave
 };
 
 struct Attend4Params {

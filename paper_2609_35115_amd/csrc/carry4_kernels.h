@@ -23,12 +23,37 @@ struct Span {
     int len, sinks;
     __device__ __forceinline__ Span(const Spans& s, const Carry4& c, int e)
     {
-        const int b = e / s.div;
+        const int b = s.div == 1 ? e : e / s.div;
         pos = s.pos ? s.pos[b] : 0;
         len = s.lens ? min(max(s.lens[b], 0), s.n) : s.n;
         sinks = min(max(s.sinks ? s.sinks[b] : s.sinks_all, 0), c.sinks);
         if (pos < 0 || pos > (int64_t)1 << 60) pos = len = 0;
         total = pos + len;
+    }
+};
+
+// Token `off` of the `per` that start at token t0 (of entries of n tokens each;
+// t0, n uniform): a 64-bit division a lane costs as much as a head's row.
+struct Token {
+    int e, i;   // of the last token, past the end
+    bool on;
+    __device__ __forceinline__ Token(int64_t t0, int off, int per, int entries, int n)
+    {
+        const int64_t tokens = (int64_t)entries * n, t = t0 + off;
+        on = t < tokens;
+        if (tokens <= INT32_MAX) {
+            const uint32_t u = (uint32_t)min(t0, tokens - 1), e0 = u / (uint32_t)n, x = u - e0 * (uint32_t)n + off;
+            const uint32_t q = n >= per ? (x >= (uint32_t)n ? 1 : 0) : x / (uint32_t)n;
+            e = (int)(e0 + q);
+            i = (int)(x - q * (uint32_t)n);
+        } else {
+            e = (int)(min(t, tokens - 1) / n);
+            i = (int)(min(t, tokens - 1) % n);
+        }
+        if (!on) {
+            e = entries - 1;
+            i = n - 1;
+        }
     }
 };
 
@@ -171,18 +196,17 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
     const int lane = threadIdx.x & 63, l = lane % L;
     // `waves` waves work on a group of tokens, wave `wave` of group `group` of the block's
     const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.waves;
-    const int wave = all & (waves - 1), group = all / waves;
-    const int n = p.sp.n;
-    const int64_t tokens = (int64_t)p.entries * n;
-    const int64_t t = ((int64_t)(blockIdx.x / p.splits) * (4 / waves) + group) * TPW + lane / L;
-    const int e = (int)(min(t, tokens - 1) / n), i = (int)(min(t, tokens - 1) % n);
+    const int wave = all & (waves - 1), group = all >> __builtin_ctz(waves);
+    const int64_t g = (int64_t)(blockIdx.x >> p.split_bits) * (4 >> __builtin_ctz(waves)) + group;
+    const Token tk(g * TPW, lane / L, TPW, p.entries, p.sp.n);
+    const int e = tk.e, i = tk.i;
     const Span sp(p.sp, p.c, e);
-    const bool on = t < tokens && i < sp.len;
+    const bool on = tk.on && i < sp.len;
     const int64_t pos = sp.pos + i;
 
     const int jobs = p.q.heads + p.k.heads + p.v.heads;
-    const int part = waves * (blockIdx.x % p.splits) + wave, parts = waves * p.splits;
-    const int j0 = (int)((int64_t)jobs * part / parts), j1 = (int)((int64_t)jobs * (part + 1) / parts);
+    const int part = waves * (int)(blockIdx.x & ((1u << p.split_bits) - 1)) + wave;
+    const int j0 = min(part * p.share, jobs), j1 = min(j0 + p.share, jobs);
 
     // the rotation of this lane's dimensions (identity past rot): a group's 256
     // angles are shared out over its lanes
@@ -232,7 +256,11 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
         float gain[8];
         const bool norm = p.norm && kind < 2;
 #pragma unroll
-        for (int k = 0; k < 8; k++) gain[k] = norm && gains ? gains[8 * l + k] : 1.0f;
+        for (int k = 0; k < 8; k++) gain[k] = 1.0f;
+        if (norm && gains) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) gain[k] = gains[8 * l + k];
+        }
         const int64_t at0 = in.at(p.sp.div, e, i, 0) + 8 * l;
         const int64_t out0 = out.p ? out.at(p.sp.div, e, i, 0) + 8 * l : 0;
         Raw8<BF16> next{};
@@ -308,12 +336,13 @@ template <bool BF16, int D> hipError_t launch_heads_d(HeadsParams p, hipStream_t
     // costs as much as a few rows (us with one, two and four waves a group: 2
     // rows, 74,046 tokens 21, 22 and 28; 6, 13,146 18, 17 and 23; 40, 32,768 -,
     // 146 and 136; but 10 waves or fewer in all, 4.6 with four and 6.6 with one).
-    int64_t splits = 1;
     p.waves = groups < 1024 || jobs > 16 ? 4 : jobs > 4 ? 2 : 1;
-    while (4 * splits < jobs && groups * splits < 512) splits *= 2;
-    p.splits = (int)splits;
+    p.split_bits = 0;
+    while ((4ll << p.split_bits) < jobs && groups << p.split_bits < 512) p.split_bits++;
+    const int parts = p.waves << p.split_bits;
+    p.share = (jobs + parts - 1) / parts;
     const int64_t per = 4 / p.waves;   // groups of a block
-    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)((groups + per - 1) / per * splits)), dim3(256), st, p);
+    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)((groups + per - 1) / per << p.split_bits)), dim3(256), st, p);
 }
 
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st)
@@ -350,11 +379,11 @@ template <bool BF16, int D> __global__ __launch_bounds__(256) void read4_kernel(
 {
     constexpr int L = D / 8, TPW = 64 / L;
     const int lane = threadIdx.x & 63, l = lane % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = p.sp.n, heads = p.c.heads;
-    const int64_t t = xcd_group(blockIdx.x, gridDim.x) * TPW + lane / L;
-    const int e = (int)(min(t, (int64_t)p.entries * n - 1) / n), i = (int)(min(t, (int64_t)p.entries * n - 1) % n);
+    const int heads = p.c.heads;
+    const Token tk(xcd_group(blockIdx.x, gridDim.x) * TPW, lane / L, TPW, p.entries, p.sp.n);
+    const int e = tk.e, i = tk.i;
     const Span sp(p.sp, p.c, e);
-    if (t >= (int64_t)p.entries * n || i >= sp.len) return;
+    if (!tk.on || i >= sp.len) return;
     const int64_t pos = sp.pos + i;
     const int64_t slot = pos < sp.sinks ? pos : p.c.sinks + (pos - sp.sinks) % p.c.ring;
     const int N = p.c.slots();
