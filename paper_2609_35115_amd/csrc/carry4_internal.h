@@ -85,6 +85,7 @@ struct Read4Params {
     Spans sp;
     HeadRows k, v;           // outputs
     int entries, wide;       // wide: every row is 16-byte aligned
+    int waves, share;   // set at the launch, as in HeadsParams
 };
 
 // The carry of (entry e, kv) in Eq. carry's logical order, widened to fp32: the

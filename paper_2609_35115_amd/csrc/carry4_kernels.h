@@ -374,26 +374,29 @@ __device__ __forceinline__ void decode8(uint32_t w, uint32_t s, float (&x)[8])
 __device__ __forceinline__ int64_t xcd_group(unsigned b, unsigned blocks) { return (int64_t)(b & 7) * (blocks >> 3) + (b >> 3); }
 inline int64_t xcd_blocks(int64_t groups) { return (groups + 7) / 8 * 8; }   // some past the last group
 
-// Lanes and tokens as in heads_kernel; a wave walks a share of the (kv, head) rows.
+// Lanes, tokens and waves as in heads_kernel; a wave walks a share of the (kv, head) rows.
 template <bool BF16, int D> __global__ __launch_bounds__(256) void read4_kernel(const Read4Params p)
 {
     constexpr int L = D / 8, TPW = 64 / L;
-    const int lane = threadIdx.x & 63, l = lane % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int heads = p.c.heads;
-    const Token tk(xcd_group(blockIdx.x, gridDim.x) * TPW, lane / L, TPW, p.entries, p.sp.n);
+    const int lane = threadIdx.x & 63, l = lane % L, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.waves;
+    const int wave = all & (waves - 1), group = all >> __builtin_ctz(waves), heads = p.c.heads;
+    const int64_t g = xcd_group(blockIdx.x, gridDim.x) * (4 >> __builtin_ctz(waves)) + group;
+    const Token tk(g * TPW, lane / L, TPW, p.entries, p.sp.n);
     const int e = tk.e, i = tk.i;
     const Span sp(p.sp, p.c, e);
     if (!tk.on || i >= sp.len) return;
     const int64_t pos = sp.pos + i;
     const int64_t slot = pos < sp.sinks ? pos : p.c.sinks + (pos - sp.sinks) % p.c.ring;
     const int N = p.c.slots();
+    const int j0 = wave * p.share, j1 = j0 + p.share;
     for (int kv = 0; kv < 2; kv++) {
         const HeadRows& o = kv ? p.v : p.k;
         const int64_t at = o.at(p.sp.div, e, i, 0) + 8 * l;
         const uint8_t* codes = p.c.base + (int64_t)e * heads * p.c.region + ((int64_t)kv * N + slot) * (D / 2) + 4 * l;
         const uint8_t* scale = p.c.base + (int64_t)e * heads * p.c.region + (int64_t)N * D + ((int64_t)kv * N + slot) * (D / 32) + (l >> 2);
+        const int h0 = max(j0 - kv * heads, 0), h1 = min(j1 - kv * heads, heads);
 #pragma unroll 2
-        for (int h = wave; h < heads; h += 4) {
+        for (int h = h0; h < h1; h++) {
             float x[8];
             decode8(*(const uint32_t*)(codes + h * p.c.region), scale[h * p.c.region], x);
             store8<BF16>(o.p, at + h * o.sh, p.wide, x);
@@ -401,11 +404,15 @@ template <bool BF16, int D> __global__ __launch_bounds__(256) void read4_kernel(
     }
 }
 
-template <bool BF16, int D> hipError_t launch_read4_d(const Read4Params& p, hipStream_t st)
+template <bool BF16, int D> hipError_t launch_read4_d(Read4Params p, hipStream_t st)
 {
     constexpr int TPW = 64 / (D / 8);
-    const unsigned blocks = (unsigned)xcd_blocks(((int64_t)p.entries * p.sp.n + TPW - 1) / TPW);
-    return launch_with(read4_kernel<BF16, D>, dim3(blocks), dim3(256), st, p);
+    const int64_t groups = ((int64_t)p.entries * p.sp.n + TPW - 1) / TPW;
+    const int jobs = 2 * p.c.heads;
+    p.waves = groups < 1024 || jobs > 16 ? 4 : jobs > 4 ? 2 : 1;
+    p.share = (jobs + p.waves - 1) / p.waves;
+    const int64_t per = 4 / p.waves;
+    return launch_with(read4_kernel<BF16, D>, dim3((unsigned)xcd_blocks((groups + per - 1) / per)), dim3(256), st, p);
 }
 
 hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
