@@ -989,12 +989,14 @@ __global__ __launch_bounds__(64 * NW, QG == 2 ? (D == 64 ? 3 : 2) : BF16 ? (D ==
 #pragma unroll
     for (int j = 0; j < 8; j++) ones[j] = (__bf16)1.0f;
 
+    const bool rows_left = row0 + 16 * QG * wave <= last;
     if (t_lo < t_hi) load(t_lo);
     for (int t = t_lo; t < t_hi; t++) {
         if (t > t_lo) __syncthreads();   // the previous tile has been read
         store();
         if (t + 1 < t_hi) load(t + 1);
         __syncthreads();
+        if (!rows_left) continue;   // the wave only decodes
         const int t0 = t * kWideTile;
         // a scale that turns the scores' order around takes the masking path too
         const bool open = ((t0 + kWideTile <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + kWideTile <= lead.hi))) & (p.scale_log2 > 0.0f);
