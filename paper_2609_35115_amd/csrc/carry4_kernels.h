@@ -1222,10 +1222,13 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     many keys in all as a block of 832 on each CU visits (40 rows, 64 regions, 540
 //     keys: 8.2 and 11.1; 128 rows, 32 regions, 828 keys of 128: 12.1 and 15.3; 36
 //     rows, 88 regions, 836 keys: 16.6 and 15.7);
-//   128 rows from 1.5 blocks a CU on, its own splits included (16,384 rows, 4
-//     regions, 4,100 keys of 128: 148, in 64-row blocks 197, in 256-row ones 146;
-//     101 rows, 215 regions, 3,230 keys: 73 and 86; 256 rows, 64 regions, 1,000
-//     keys: 27, 18 and 53);
+//   128 rows from 1.5 blocks a CU on, its own splits included, where that halves
+//     the blocks nearly (16,384 rows, 4 regions, 4,100 keys of 128: 148, in 64-row
+//     blocks 197, in 256-row ones 146; 101 rows, 215 regions, 3,230 keys: 73 and
+//     82; 256 rows, 64 regions, 1,000 keys: 27 and 18; 776 rows, 13 blocks or 7 of 84
+//     regions, 1,450 keys: 92 and 89; 192, three or two: 120 and 102); at width 64
+//     only past 256 rows (1,000, 64 regions, 2,000 keys: 52 and 57; 200, 400
+//     regions, 1,500 keys: 75 and 70);
 //   splits: the join is a launch of its own, about 2 us, which grows with them.
 //     16 rows: for a block a CU, of 128 keys or more (2,000 keys, 8 regions 8.4,
 //     of 256 9.2, unsplit 16.9; 458 keys 7.2 unsplit, 8.1 split); all of two
@@ -1255,7 +1258,7 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
     }
     const int64_t s = split(in128, 512, 1024);
-    if (rows > 96 && in128 * s >= 384) return {128, (int)s};
+    if (rows > (c.D == 64 ? 256 : 96) && 8 * in64 >= 15 * in128 && in128 * s >= 384) return {128, (int)s};
     return {64, (int)std::max(split(in64, 256, 256), split(in64, 512, 1024))};
 }
 
