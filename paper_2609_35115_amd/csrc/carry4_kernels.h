@@ -1237,9 +1237,16 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     a CU, up to eight of 1,024 in 32 splits, so that a CU always holds its four
 //     or five (17,400 keys, 200 regions 63 in ten, 85 in two, 116 unsplit; 7,600,
 //     492 regions 65 in four, 72; but 5,200 of 128, 707 regions 105 in two, 100);
-//     wider: for a block a CU of 256 keys, or two of 1,024 (836 keys of 128, 88
-//     regions 15.7 in two, 19.0 unsplit; 20,000, 32 regions 43 and 51; 56 rows, 256 blocks 16.3 unsplit, 25.5 in two; 2,100
-//     keys, 32 regions of 128 rows 20.4 and, in two a CU, 25.5).
+//     wider, 64 blocks or fewer: for a block a CU of 256 keys, or two of 1,024
+//     (2,100 keys of 128, 32 regions of 128 rows 20.4 and, in two a CU, 25.5);
+//     wider, more: by what a tile takes a CU that has k of the blocks, `fit` of them
+//     at once, fitted to calls of 80 to 1,024 blocks and 1,800 and 4,500 keys in
+//     one to four splits, all within a fifth but for a few (own: what one block
+//     alone waits for; a second costs far less than the first), and the join's
+//     bytes at 4 TB/s.  40 rows, 4,500 keys of 64: 260 regions 42 in four, 70
+//     unsplit, 400 52 in three and 71, 1,024 unsplit 107, 111 in two; of 128: 260
+//     70 and 107, 80 30 in six, 37 in three; 300 rows, 16,000 of 64, 40 regions 92
+//     in four, 133 in two; but 56 rows, 458 keys, 256 regions 16.3 unsplit, 25.5 in two.
 struct Plan4 {
     int rows;     // query rows of a block: 16 (one set for four waves), 64 or 128 (16 or 32 a wave)
     int splits;
@@ -1257,9 +1264,23 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
         const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), in16 > 512 ? 1 : std::min((int64_t)32, split(in16, 2048, 1024)));
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
     }
-    const int64_t s = split(in128, 512, 1024);
-    if (rows > (c.D == 64 ? 256 : 96) && 8 * in64 >= 15 * in128 && in128 * s >= 384) return {128, (int)s};
-    return {64, (int)std::max(split(in64, 256, 256), split(in64, 512, 1024))};
+    const bool wide = rows > (c.D == 64 ? 256 : 96) && 8 * in64 >= 15 * in128 && in128 * split(in128, 512, 1024) >= 384;
+    // a tile takes a CU with k blocks us (own ceil(k / fit) + k) microseconds
+    const double us = c.D == 64 ? (wide ? 0.40 : 0.23) : wide ? 0.62 : 0.48;
+    const double own = c.D == 64 ? (wide ? 1.2 : 2.4) : wide ? 1.5 : 1.25;
+    const int64_t fit = (c.D == 64 ? 5 : 3) - (wide ? (c.D == 64 ? 2 : 1) : 0), blocks = wide ? in128 : in64;
+    if (blocks <= 64) return {wide ? 128 : 64, (int)std::max(split(blocks, 256, 256), split(blocks, 512, 1024))};
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 8 && (s == 1 || most >= 256 * s); s++) {
+        const int64_t k = (blocks * s + 255) / 256;
+        double cost = us * (own * (double)((k + fit - 1) / fit) + (double)k) * (double)(most / 64 + 1) / s;
+        if (s > 1) cost += 2.0 + (double)(regions * rows * s) * (c.D + 2) * 2e-6;   // the join, and its 8 bytes a value
+        if (s > 1 && cost >= least) continue;
+        best = s;
+        least = cost;
+    }
+    return {wide ? 128 : 64, best};
 }
 
 int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes)
@@ -1283,8 +1304,10 @@ template <bool BF16, int D> hipError_t launch_attend4_d(const Attend4Params& p, 
     else if constexpr (BF16) e = launch_with(attend4_wide<BF16, D, 2, 4>, grid, dim3(256), st, p);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t all = (int64_t)p.entries * p.c.heads * rows;
+    // (of many rows a group takes one each: 8,000 rows in five splits 31 us with a
+    // block a row, 21 with 16)
     constexpr int per = 256 / (D / 4);   // rows of a block, or groups of one row
-    if (p.splits <= 4) return launch_with(attend4_join<BF16, D, 1>, dim3((unsigned)((all + per - 1) / per)), dim3(256), st, p);
+    if (p.splits <= 4 || all >= 2048) return launch_with(attend4_join<BF16, D, 1>, dim3((unsigned)((all + per - 1) / per)), dim3(256), st, p);
     return launch_with(attend4_join<BF16, D, per>, dim3((unsigned)all), dim3(256), st, p);
 }
 
