@@ -173,6 +173,31 @@ def test_norm_edges():
 # --------------------------------------------------------------- stored values
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,Hq,H,D,rot", [
+    (3, 3001, 1, 1, 64, 64), (700, 7, 2, 1, 128, 128),          # one wave a group of tokens
+    (9001, 1, 1, 2, 64, 32), (2100, 2, 5, 4, 128, 48),          # two
+    (5, 1700, 14, 9, 128, 128),                                 # four
+])
+def test_many_tokens_of_few_heads(B, n, Hq, H, D, rot, dtype):
+    """Each sharing of a block's waves: norms as of the entries by themselves, and
+    the held values, of entries of different lengths."""
+    m = carry4()
+    q, k, v = (rand((B, n, h, D), dtype, s) for h, s in ((Hq, 1), (H, 2), (H, 3)))
+    freqs = torch.rand(rot // 2, generator=torch.Generator().manual_seed(4)).cuda()
+    lens = [n - b % 3 * (n // 3) for b in range(B)]
+    pos, li = index([17 * b for b in range(B)]), index(lens, torch.int32)
+    q1, k1 = m.qk_norm_rope(q, k, pos, freqs, lens=li)
+    for b in (0, 1, B // 2, B - 1):
+        q2, k2 = m.qk_norm_rope(q[b:b + 1, :lens[b]], k[b:b + 1, :lens[b]], pos[b:b + 1], freqs)
+        assert torch.equal(q1[b, :lens[b]], q2[0]) and torch.equal(k1[b, :lens[b]], k2[0])
+    c = m.Carry4(B, H, D, sinks=2, ring=n)
+    c.append(k, v, pos, lens=li)
+    a, b = c.read(pos, n, lens=li)
+    live = (torch.arange(n)[None] < torch.tensor(lens)[:, None])[..., None, None]
+    assert torch.equal(a.double().cpu(), held(k).double().cpu() * live) and torch.equal(b.double().cpu(), held(v).double().cpu() * live)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_stored_values_are_exact(dtype, D):
     """Every border between codes and its neighbours, at several scales, and random rows."""
@@ -470,6 +495,98 @@ def test_attend_masked_nan_and_infinity(dtype):
     bad = torch.isnan(got).cpu()
     assert bad[0, 10:16, :2].all() and not bad[0, :10].any() and not bad[0, 16:20].any()
     assert bad[0, 20:24, 2:, 32:].all() and not bad[0, 20:24, 2:, :32].any() and not bad[0, 20:24, :2].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,Hq,H,D,sinks,window,causal,ring", [
+    (10, 42, 5, 5, 64, 0, 1400, True, 1442),      # 64 rows, five splits, many rows to join
+    (2, 42, 5, 5, 64, 0, 8000, True, 8042),       # 25 splits, few rows to join
+    (17, 40, 4, 4, 64, 3, 1800, False, 1900),     # a few splits; the last wave without rows
+    (5, 100, 3, 3, 128, 0, 3000, True, 3100),
+    (26, 100, 5, 5, 128, 0, 3100, True, 3200),    # 128 rows, splits
+    (16, 380, 8, 8, 64, 5, 70, True, 500),        # 128 rows at width 64
+    (16, 380, 8, 8, 64, 70, 150, False, 600),
+])
+def test_attend_wide_block_shapes(B, n, Hq, H, D, sinks, window, causal, ring, dtype):
+    test_attend_block_shapes(B, n, Hq, H, D, sinks, window, causal, ring, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,H,D,sinks,window,causal", [
+    (40, 200, 2, 64, 3, 40, True), (40, 200, 2, 128, 3, 40, False),     # 64 rows a block
+    (17, 40, 4, 64, 3, 1800, True),                                     # split
+    (16, 380, 8, 64, 0, 70, True), (48, 100, 8, 128, 3, 60, True),      # 128 rows
+])
+def test_attend_nan_of_a_batch(B, n, H, D, sinks, window, causal, dtype):
+    """NaN keys and values in wide blocks: an entry's rows and dimensions that are
+    NaN are those of the entry's own call (16-row blocks), the others as near as
+    both are to the formula."""
+    m = carry4()
+    ring, T = window + n, sinks + window + n + 20
+    k, v = rand((B, T + n, H, D), dtype, 1), rand((B, T + n, H, D), dtype, 2)
+    q = rand((B, n, H, D), dtype, 3)
+    picked = [0, 1, B - 1]
+    clean = {b: [x[b].clone() for x in (k, v)] for b in picked}
+    k[0, T + 15, 0, 5] = math.nan
+    v[0, T + n - 1, H - 1, D - 1] = math.inf
+    v[1, T + 1, 0, 33] = math.nan
+    k[1, T - 3, H - 1, 0] = -math.inf
+    v[B - 1, 0 if sinks else T, 0, 0] = math.nan
+
+    def run(b):
+        c = m.Carry4(len(b), H, D, sinks=sinks, ring=ring)
+        c.memory.fill_(255)
+        c.append(k[b, :T], v[b, :T], index([0] * len(b)))
+        c.append(k[b, T:], v[b, T:], index([T] * len(b)))
+        return c.attend(q[b], index([T] * len(b)), window, causal=causal)
+    got = run(list(range(B)))
+    for b in picked:
+        alone = run([b])[0]
+        bad = torch.isnan(alone)
+        assert bad.any() and not bad.all() and torch.equal(bad, torch.isnan(got[b]))
+        _, bound, top = dense([held(x) for x in clean[b]], q[b], range(T, T + n), 0, window, causal, sinks)
+        rel = 2.0 ** -8 if dtype == "bf16" else 0.0
+        limit = 2 * (rel * top + (bound + rel * top * (1 + rel)) * (1 + rel)).expand(n, H, D)
+        far = (got[b].double() - alone.double()).abs().cpu() > limit.cpu()
+        assert not (far & ~bad.cpu()).any()
+    for b in range(2, B - 1):
+        assert not torch.isnan(got[b]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_nan_of_a_few_rows(D, dtype):
+    """As of a wide block, for the four rows of two tokens."""
+    shape = (2, 2, 4, 2, D, 0, 6, True, [0, 30])
+    m = carry4()
+
+    def plant(k, v):
+        k[0, 1, 0, 5] = math.nan
+        v[1, 0, 1, 40] = math.inf
+        v[1, 1, 0, 33] = math.nan
+    c, model, lens = turn(m, shape, dtype, 52, before=plant)
+    q = rand((2, 2, 4, D), dtype, 80)
+    got = c.attend(q, index(shape[8]), shape[6])
+    check(got, model, q, shape, dtype, lens)
+    bad = torch.isnan(got).cpu()
+    assert bad[0, 1, :2].all() and not bad[0, 0].any() and not bad[0, 1, 2:].any()
+    assert bad[1, :, 2:, 32:64].all() and bad[1, 1, :2, 32:64].all() and not bad[1, :, :, :32].any() and not bad[1, 0, :2].any()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1.0, 1e30])
+def test_attend_fp32_rows_of_any_size(scale):
+    """The planes of queries from 1e-30 to 1e30 (scaled back by the score scale):
+    one to four rows, and more."""
+    m = carry4()
+    for n, D in ((1, 64), (2, 128), (4, 64), (9, 128)):
+        k, v, q = (rand((1, 50, 1, D), "f32", s) for s in (1, 2, 3))
+        c = m.Carry4(1, 1, D, sinks=0, ring=60)
+        c.append(k, v, index([0]))
+        q = q[:, :n]
+        got = c.attend(q * scale, index([50 - n]), 50, scale=D ** -0.5 / scale)
+        exact = (q * scale).double() / scale   # what the rounded queries are
+        want, bound, _ = dense((held(k[0]), held(v[0])), exact[0], range(50 - n, 50), 0, 50, True, 0)
+        near(got[0], want, 0.0, bound * (1 + 2.0 ** -20))
 
 
 def test_attend_scores_far_apart():
