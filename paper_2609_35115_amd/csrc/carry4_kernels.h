@@ -175,10 +175,12 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 // precision they are computed in.  A group with a NaN or an infinity is NaN.
 //
 // What bounds it: HBM.  Norm and rotation of 32,768 tokens of 40 heads of 128 (671 MB)
-// 139 us, 4.8 TB/s; of 14,336 of 16 heads of 64 16 us.  A load of the next row
+// 129 us, 5.2 TB/s; of 14,336 of 16 heads of 64 14.3 us.  A load of the next row
 // before this one is worked on, partners by DPP instead of LDS and one reciprocal
-// root took the first from 315 to 161, the block's shared sines to 139.  The store
-// of 16,384 tokens of 8 heads of 128 (85 MB) 23 us.
+// root took the first from 315 to 161, the block's shared sines to 139, 32-bit
+// divisions to 129.  The store of 16,384 tokens of 8 heads of 128 (85 MB) 23.8 us,
+// two thirds of its time the codes' stores (stores past the caches take 21.9, but
+// the attention that follows reads 3% slower).
 // The value of the lane whose number differs by half a row's lanes (D = 64:
 // lane ^ 4; 128: lane ^ 8), without an LDS round trip.
 template <int L> __device__ __forceinline__ float half_row(float v)
@@ -876,7 +878,8 @@ __global__ __launch_bounds__(256, !BF16 && !FOLD ? 1 : D == 128 ? 4 : 5) void at
 // queries, 4 to a key head of 128, window 4,096: 289 us, 966 TFLOP/s; two waves a
 // SIMD whose vector (46%) and matrix work (39%) overlap only in part.
 // Queries scaled in two bf16 planes, so that scores come ready for the exponential,
-// were slower (38 us); so were waves of 32 rows for the short lists (44).
+// were slower (38 us); so were waves of 32 rows for the short lists (44), and two
+// tiles in LDS, one decoded while the other is worked on (42: fewer waves a SIMD).
 constexpr int kWideTile = 64;
 constexpr float kSlack = 8.0f;
 
