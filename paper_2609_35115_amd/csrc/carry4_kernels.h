@@ -1220,11 +1220,11 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 
 // Which kernel an attention call takes, and over how many blocks its keys are
 // split.  Us of a call in a graph, bf16, both sides of each border:
-//   16 rows a block up to 32 rows (20 rows, 256 regions, 3,025 keys of 128: 50,
-//     in 64-row blocks 103; 60 rows, 256 regions, 560 keys 25 and 17), and for as
-//     many keys in all as a block of 832 on each CU visits (40 rows, 64 regions, 540
-//     keys: 8.2 and 11.1; 128 rows, 32 regions, 828 keys of 128: 12.1 and 15.3; 36
-//     rows, 88 regions, 836 keys: 16.6 and 15.7);
+//   16 rows a block up to 16 rows, and for as many keys in all as a block of 832
+//     on each CU visits, 1,500 up to 32 rows (40 rows, 64 regions, 540 keys: 8.2 and
+//     11.1; 128 rows, 32 regions, 828 keys of 128: 12.1 and 15.3; 36 rows, 88
+//     regions, 836 keys: 16.6 and 15.7; 24 rows, 256 regions, 724 keys 11.8 and
+//     12.4, 6,024 keys 55 and 38; 20 rows, 600 regions, 6,020 keys of 128: 171 and 146);
 //   128 rows from 1.5 blocks a CU on, its own splits included, where that halves
 //     the blocks nearly (16,384 rows, 4 regions, 4,100 keys of 128: 148, in 64-row
 //     blocks 197, in 256-row ones 146; 101 rows, 215 regions, 3,230 keys: 73 and
@@ -1262,7 +1262,7 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
                   in128 = regions * ((rows + 127) / 128);
     // the most splits that make up to `blocks` blocks of `of` and leave each `keys` keys or more
     auto split = [&](int64_t of, int64_t blocks, int64_t keys) { return std::max((int64_t)1, std::min(blocks / of, most / keys)); };
-    if (rows <= 32 || in16 * most <= 256 * 832) {
+    if (rows <= 16 || in16 * most <= 256 * (rows <= 32 ? 1500 : 832)) {
         const int64_t two = 512 / in16;
         const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), in16 > 512 ? 1 : std::min((int64_t)32, split(in16, 2048, 1024)));
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
