@@ -95,7 +95,7 @@ hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv,
                                 float* out, hipStream_t st);
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st);
 // Key splits of an attention call, and the bytes of workspace they take.
-int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes);
+int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int bf16, int64_t* ws_bytes);
 hipError_t launch_attend4(const Attend4Params& p, int bf16, hipStream_t st);
 hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st);
 

@@ -1224,7 +1224,9 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
 //     on each CU visits, 1,500 up to 32 rows (40 rows, 64 regions, 540 keys: 8.2 and
 //     11.1; 128 rows, 32 regions, 828 keys of 128: 12.1 and 15.3; 36 rows, 88
 //     regions, 836 keys: 16.6 and 15.7; 24 rows, 256 regions, 724 keys 11.8 and
-//     12.4, 6,024 keys 55 and 38; 20 rows, 600 regions, 6,020 keys of 128: 171 and 146);
+//     12.4, 6,024 keys 55 and 38; 20 rows, 600 regions, 6,020 keys of 128: 171 and 146); bf16 rows
+//     of 64 up to 4,000,000 keys in all (one token, 1,500 keys, 2,048 regions: 51 and
+//     51; 6,350, 840 regions 104 and 89; 10,000, 800 regions 158 and 136);
 //   128 rows from 1.5 blocks a CU on, its own splits included, where that halves
 //     the blocks nearly (16,384 rows, 4 regions, 4,100 keys of 128: 148, in 64-row
 //     blocks 197, in 256-row ones 146; 101 rows, 215 regions, 3,230 keys: 73 and
@@ -1254,7 +1256,7 @@ struct Plan4 {
     int rows;     // query rows of a block: 16 (one set for four waves), 64 or 128 (16 or 32 a wave)
     int splits;
 };
-static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
+static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window, bool bf16)
 {
     const int64_t rows = (int64_t)n * group, regions = (int64_t)entries * c.heads;
     const int64_t most = (int64_t)c.sinks + (window < c.ring ? window : c.ring) + n;   // keys of a list
@@ -1262,12 +1264,14 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
                   in128 = regions * ((rows + 127) / 128);
     // the most splits that make up to `blocks` blocks of `of` and leave each `keys` keys or more
     auto split = [&](int64_t of, int64_t blocks, int64_t keys) { return std::max((int64_t)1, std::min(blocks / of, most / keys)); };
-    if (rows <= 16 || in16 * most <= 256 * (rows <= 32 ? 1500 : 832)) {
+    const bool few = rows <= 16 && (!bf16 || c.D == 128 || in16 * most <= 4000000);
+    if (few || in16 * most <= 256 * (rows <= 32 ? 1500 : 832)) {
         const int64_t two = 512 / in16;
         const int64_t s = std::max(most < 640 ? 1 : split(in16, 256, 128), in16 > 512 ? 1 : std::min((int64_t)32, split(in16, 2048, 1024)));
         return {16, (int)(two * 448 <= most ? std::max(two, s) : s)};
     }
-    const bool wide = rows > (c.D == 64 ? 256 : 96) && 8 * in64 >= 15 * in128 && in128 * split(in128, 512, 1024) >= 384;
+    // (three planes of 32 rows do not fit the registers)
+    const bool wide = bf16 && rows > (c.D == 64 ? 256 : 96) && 8 * in64 >= 15 * in128 && in128 * split(in128, 512, 1024) >= 384;
     // a tile takes a CU with k blocks us (own ceil(k / fit) + k) microseconds
     const double us = c.D == 64 ? (wide ? 0.40 : 0.23) : wide ? 0.62 : 0.48;
     const double own = c.D == 64 ? (wide ? 1.2 : 2.4) : wide ? 1.5 : 1.25;
@@ -1286,9 +1290,9 @@ static Plan4 plan4(const Carry4& c, int entries, int n, int group, int window)
     return {wide ? 128 : 64, best};
 }
 
-int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int64_t* ws_bytes)
+int attend4_splits(const Carry4& c, int entries, int n, int group, int window, int bf16, int64_t* ws_bytes)
 {
-    const Plan4 pl = plan4(c, entries, n, group, window);
+    const Plan4 pl = plan4(c, entries, n, group, window, bf16 != 0);
     if (ws_bytes)
         *ws_bytes = pl.splits > 1 ? (int64_t)entries * c.heads * n * group * pl.splits * (c.D + 2) * 4 : 0;
     return pl.splits;
@@ -1297,8 +1301,7 @@ int attend4_splits(const Carry4& c, int entries, int n, int group, int window, i
 template <bool BF16, int D> hipError_t launch_attend4_d(const Attend4Params& p, hipStream_t st)
 {
     const int64_t rows = (int64_t)p.sp.n * p.group;
-    int rb = plan4(p.c, p.entries, p.sp.n, p.group, p.window).rows;
-    if (!BF16 && rb == 128) rb = 64;   // (three planes of 32 rows do not fit the registers)
+    const int rb = plan4(p.c, p.entries, p.sp.n, p.group, p.window, BF16).rows;
     const dim3 grid((unsigned)((int64_t)p.splits * p.entries * p.c.heads * ((rows + rb - 1) / rb)));
     hipError_t e = hipErrorInvalidValue;
     if (rb == 16 && !BF16 && rows <= 4) e = launch_with(attend4_kernel<BF16, D, !BF16>, grid, dim3(256), st, p);

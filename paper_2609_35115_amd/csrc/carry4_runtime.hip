@@ -2,6 +2,7 @@
 // launches of carry4_kernels.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 
@@ -209,9 +210,9 @@ dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_
 int64_t dc_carry4_workspace(const dc_carry4* c, int32_t q_heads, int32_t n, int32_t window)
 {
     if (check_shape(c) != DC_OK || q_heads < 1 || q_heads % c->heads != 0 || n < 1 || window < 0) return 0;
-    int64_t bytes = 0;
-    attend4_splits(carry(c), c->batch, n, q_heads / c->heads, window, &bytes);
-    return bytes;
+    int64_t bytes[2] = {0, 0};   // of fp32 and of bf16 rows
+    for (int bf16 = 0; bf16 < 2; bf16++) attend4_splits(carry(c), c->batch, n, q_heads / c->heads, window, bf16, bytes + bf16);
+    return std::max(bytes[0], bytes[1]);
 }
 
 dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtype, const dc_head_rows* q,
@@ -246,7 +247,7 @@ dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtyp
     p.wide_in = wide(q, dtype);
     p.wide_out = wide(out, dtype);
     int64_t need = 0;
-    p.splits = attend4_splits(p.c, p.entries, span->n, p.group, window, &need);
+    p.splits = attend4_splits(p.c, p.entries, span->n, p.group, window, dtype == DC_BF16, &need);
     CHECK(need == 0 || (workspace && workspace_bytes >= need && (uintptr_t)workspace % 16 == 0), DC_EINVAL,
           "workspace is NULL, too small or not 16-byte aligned");
     p.ws = (float*)workspace;

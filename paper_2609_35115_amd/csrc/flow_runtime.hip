@@ -266,7 +266,7 @@ hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc,
     p.scale_log2 = 0.125f * 1.4426950408889634f;
     p.wide_in = p.wide_out = 1;
     int64_t need = 0;
-    p.splits = attend4_splits(p.c, p.entries, n, 1, p.window, &need);
+    p.splits = attend4_splits(p.c, p.entries, n, 1, p.window, s->bf ? 1 : 0, &need);
     if (need > s->ws_bytes) return hipErrorInvalidValue;
     *launches = p.splits > 1 ? 2 : 1;   // the join
     p.ws = s->ws;
@@ -587,7 +587,7 @@ dc_status dc_flow_init_opt(const void* weights_blob, size_t blob_bytes, const dc
     auto ws_most = [&](int entries, int frames) {
         for (int n = 1; four && n <= frames; n++) {
             int64_t b = 0;
-            attend4_splits(s->carry4, entries, n, 1, c.f_retained, &b);
+            attend4_splits(s->carry4, entries, n, 1, c.f_retained, s->bf ? 1 : 0, &b);
             s->ws_bytes = std::max(s->ws_bytes, b);
         }
     };

@@ -506,6 +506,7 @@ def test_attend_masked_nan_and_infinity(dtype):
     (26, 100, 5, 5, 128, 0, 3100, True, 3200),    # 128 rows, splits
     (16, 380, 8, 8, 64, 5, 70, True, 500),        # 128 rows at width 64
     (16, 380, 8, 8, 64, 70, 150, False, 600),
+    (75, 1, 80, 10, 64, 3, 5400, True, 5400),     # few rows of many keys
 ])
 def test_attend_wide_block_shapes(B, n, Hq, H, D, sinks, window, causal, ring, dtype):
     test_attend_block_shapes(B, n, Hq, H, D, sinks, window, causal, ring, dtype)
