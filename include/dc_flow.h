@@ -216,8 +216,8 @@ void dc_flow_free(dc_flow_state* s);
  * negatives) with one scale for 32 consecutive dimensions: 2^e, e the least
  * integer in [-126, 126] for which 6 * 2^e is at least the group's largest
  * magnitude; ties to the even code.  4.25 bits a value.  A group with a NaN
- * or an infinity is held as NaN (and a magnitude of 3.5 * 2^126 and more, which
- * rounds to 2^128, as an infinity).
+ * or an infinity is held as NaN, and one with a magnitude of 3.5 * 2^126 and
+ * more, which rounds to 2^128, as well.
  *
  * Every call is launched on hip_stream, a stream of the current device, and
  * returns without waiting; nothing is allocated, so calls can be captured.

@@ -203,14 +203,23 @@ void ocf_qk(int hd, double* x, const double* gain, double eps, int rope_dims, do
  * The values that n values (n a multiple of 32) are held as in 4 bits: per
  * group of 32, scale 2^e with the least e in [-126, 126] for which 6 * 2^e is at
  * least the largest magnitude; every value the nearest of +-{0, 0.5, 1, 1.5, 2,
- * 3, 4, 6} * 2^e, ties to the even place in that list.
+ * 3, 4, 6} * 2^e, ties to the even place in that list.  A group with a NaN, an
+ * infinity or an element that rounds to 2^128 is NaN.
  */
 void ocf_hold4(int n, double* x)
 {
     static const double grid[8] = {0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0};
     for (int g = 0; g < n; g += 32) {
         double top = 0.0;
-        for (int i = 0; i < 32; i++) top = fmax(top, fabs(x[g + i]));
+        int nan = 0;
+        for (int i = 0; i < 32; i++) {
+            top = fmax(top, fabs(x[g + i]));
+            nan |= isnan(x[g + i]);
+        }
+        if (nan || top >= ldexp(3.5, 126)) {
+            for (int i = 0; i < 32; i++) x[g + i] = NAN;
+            continue;
+        }
         int e = -126;
         while (e < 126 && ldexp(6.0, e) < top) e++;
         for (int i = 0; i < 32; i++) {

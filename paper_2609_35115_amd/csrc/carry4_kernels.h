@@ -172,7 +172,9 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 // [-126, 126] for which 6 * 2^e is at least its largest magnitude (so none is
 // cut), and an element is the nearest E2M1 value of x 2^-e, ties to even.
 // Scaling by a power of two is exact, so the codes do not depend on the
-// precision they are computed in.  A group with a NaN or an infinity is NaN.
+// precision they are computed in.  A group with a NaN or an infinity is NaN, and so
+// is one with an element that would be 2^128 (3.5 * 2^126 and more): held as an
+// infinity it would turn a masked probability of zero into NaN.
 //
 // What bounds it: HBM.  Norm and rotation of 32,768 tokens of 40 heads of 128 (671 MB)
 // 129 us, 5.2 TB/s; of 14,336 of 16 heads of 64 14.3 us.  A load of the next row
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
             w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
             w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
             w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
-            if (top >= 0x7f800000u) {
+            if (top >= 0x7f600000u) {   // 3.5 * 2^126
                 s = 255;
                 w = 0;
             }

@@ -1,0 +1,79 @@
+"""The attention over the 4-bit carry at the edges of its numbers, in every
+block shape."""
+import pytest
+import torch
+
+from tests.test_gpu_carry4 import DT, carry4, index, rand
+
+pytestmark = pytest.mark.gpu
+
+# B, n, heads of queries and keys, width, first tokens, window; the shape that each type's rows take:
+# rows of a block and splits, of fp32 and bf16
+SHAPES = [
+    ((2, 24, 4, 2, 64, 0, 6), (16, 1), (16, 1)),
+    ((2, 2, 4, 2, 128, 0, 6), (16, 1), (16, 1)),          # four rows
+    ((1, 2, 4, 2, 64, 0, 3000), (16, 23), (16, 23)),      # four rows, split
+    ((1, 6, 4, 2, 128, 0, 3000), (16, 23), (16, 23)),
+    ((40, 200, 2, 2, 64, 3, 40), (64, 1), (64, 1)),
+    ((40, 200, 2, 2, 128, 3, 40), (64, 1), (64, 1)),
+    ((17, 40, 4, 4, 64, 3, 1800), (64, 7), (64, 7)),
+    ((5, 100, 3, 3, 128, 0, 3000), (64, 8), (64, 8)),
+    ((16, 380, 8, 8, 64, 0, 70), (64, 1), (128, 1)),
+    ((48, 100, 8, 8, 128, 3, 60), (64, 1), (128, 1)),
+    ((66, 380, 1, 1, 64, 0, 3000), (64, 3), (128, 3)),
+    ((26, 100, 5, 5, 128, 0, 3100), (64, 5), (128, 3)),
+]
+each_shape = pytest.mark.parametrize("shape", [s for s, _, _ in SHAPES], ids=["x".join(map(str, s)) for s, _, _ in SHAPES])
+each_type = pytest.mark.parametrize("dtype", ["f32", "bf16"])
+
+
+def turn(shape, dtype):
+    """A causal call's tensors: tokens before it, its own, its queries; and what runs it."""
+    B, n, Hq, H, D, sinks, w = shape
+    T = sinks + w + 9
+    k, v, q = rand((B, T + n, H, D), dtype, 1), rand((B, T + n, H, D), dtype, 2), rand((B, n, Hq, D), dtype, 3)
+
+    def run(k, v, q):
+        c = carry4().Carry4(B, H, D, sinks=sinks, ring=w + n)
+        c.memory.fill_(255)
+        c.append(k[:, :T], v[:, :T], index([0] * B))
+        c.append(k[:, T:], v[:, T:], index([T] * B))
+        return c.attend(q, index([T] * B), w)
+    return T, k, v, q, run
+
+
+@each_type
+@pytest.mark.parametrize("D", [64, 128])
+def test_largest_magnitudes(D, dtype):
+    """3.5 * 2^126 and more would round to 2^128: such a group is held as NaN; what is
+    just below is held as 3 * 2^126."""
+    m = carry4()
+    below = 3.5 * 2.0 ** 126 * (1 - 2.0 ** (-24 if dtype == "f32" else -8))
+    tops = [below, -below, 3.5 * 2.0 ** 126, -3.5 * 2.0 ** 126, 3.75 * 2.0 ** 126, torch.finfo(DT[dtype]).max]
+    k = rand((1, len(tops), 1, D), dtype, 5)
+    k[0, :, 0, 7] = torch.tensor(tops, dtype=torch.float64).to(k.dtype).cuda()
+    c = m.Carry4(1, 1, D, sinks=0, ring=len(tops))
+    c.append(k, k.flip(1), index([0]))
+    for out in (torch.float32, torch.bfloat16):
+        a, b = c.read(index([0]), len(tops), dtype=out)
+        assert torch.equal(torch.isnan(a), torch.isnan(b.flip(1)))
+        assert torch.isnan(a[0, 2:, 0, :32]).all() and not torch.isnan(a[0, :2]).any() and not torch.isnan(a[0, :, 0, 32:]).any()
+        assert (a[0, :2, 0, 7].double().cpu() == torch.tensor([3.0, -3.0], dtype=torch.float64) * 2.0 ** 126).all()
+        assert (a[0, :2, 0, :7] == 0).all() and (a[0, :2, 0, 8:32] == 0).all()
+
+
+@each_type
+@each_shape
+def test_largest_magnitudes_in_masked_places(shape, dtype):
+    """A value near the type's largest among the call's tokens: NaN in its 32
+    dimensions of the rows that see it, no other row's bits touched."""
+    B, n, Hq, H, D, _, w = shape
+    T, k, v, q, run = turn(shape, dtype)
+    want = run(k, v, q)
+    b, t, at = B - 1, n // 2, D - 1
+    v[b, T + t, H - 1, at] = 2.0 ** 127 * 1.9
+    got = run(k, v, q)
+    seen = torch.zeros(B, n, Hq, D, dtype=torch.bool)
+    seen[b, t:t + w, Hq - Hq // H:, D - 32:] = True
+    assert torch.equal(torch.isnan(got).cpu(), seen)
+    assert torch.equal(got.cpu()[~seen], want.cpu()[~seen])
