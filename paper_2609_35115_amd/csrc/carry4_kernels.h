@@ -1072,7 +1072,8 @@ __global__ __launch_bounds__(64 * NW, QG == 2 ? (D == 64 ? 3 : 2) : BF16 ? (D ==
             if (__any(top * mul > limit[u])) {
                 top = max_xor16_32(top) * mul;
                 const bool move = top > limit[u];
-                const float f = move ? __builtin_amdgcn_exp2f((limit[u] - kSlack) - top) : 1.0f;
+                // (from base itself: limit - kSlack is off by up to 2^-21 of a power of two)
+                const float f = move ? __builtin_amdgcn_exp2f((limit[u] == -INFINITY ? -INFINITY : base[u]) - top) : 1.0f;
                 if (move) {
                     limit[u] = top + kSlack;
                     base[u] = top;
@@ -1147,7 +1148,7 @@ __global__ __launch_bounds__(64 * NW, QG == 2 ? (D == 64 ? 3 : 2) : BF16 ? (D ==
             }
         }
         if (p.splits > 1 && g == 0) {
-            p.ws[parts * D + 2 * part] = limit[u] - kSlack;
+            p.ws[parts * D + 2 * part] = limit[u] == -INFINITY ? -INFINITY : base[u];
             p.ws[parts * D + 2 * part + 1] = l;
         }
     }

@@ -1,8 +1,11 @@
 """The attention over the 4-bit carry at the edges of its numbers, in every
 block shape."""
+import math
+
 import pytest
 import torch
 
+from paper_2609_35115_amd import flow
 from tests.test_gpu_carry4 import DT, carry4, index, rand
 
 pytestmark = pytest.mark.gpu
@@ -77,3 +80,35 @@ def test_largest_magnitudes_in_masked_places(shape, dtype):
     seen[b, t:t + w, Hq - Hq // H:, D - 32:] = True
     assert torch.equal(torch.isnan(got).cpu(), seen)
     assert torch.equal(got.cpu()[~seen], want.cpu()[~seen])
+
+
+@each_shape
+def test_splits_meet_with_exact_weights(shape):
+    """fp32 rows whose splits' largest scores differ by about 2^-22: a split's
+    weight is its keys' number times 2^(its score).  Each dimension's values are
+    ones in one split alone, so results' ratios are the weights'.  Against 2 to the
+    difference a ratio is off by one exponential's last place (2^-23 at most) and the
+    product with it in each of two stages of the join, and by two products with the
+    sum's reciprocal: 2 (2 + 1) + 2 halves of a last place."""
+    B, n, Hq, H, D, _, w = shape
+    m = carry4()
+    c = m.Carry4(B, H, D, sinks=0, ring=w + n)
+    rows, keys = B * n * Hq * (D + 2) * 4, w + n
+    size = flow.flib().dc_carry4_workspace(c._ref, Hq, n, w)
+    splits = size // rows if size else 1
+    tile = 64 if n * (Hq // H) > 16 or splits == 1 else 32
+    tiles = -(-keys // tile)
+    of = torch.tensor([next(s for s in range(splits) if tiles * (s + 1) // splits > t // tile) for t in range(keys)])
+    k, v = torch.zeros(B, keys, H, D), torch.zeros(B, keys, H, D)
+    k[..., 0] = torch.where(of % 2 == 0, 3.0, 4.0)[None, :, None]
+    v[:, torch.arange(keys), :, of] = 1.0
+    q = torch.zeros(B, n, Hq, D)
+    q[..., 0] = 0.157 * 2.0 ** -20
+    c.append(k.cuda(), v.cuda(), index([0] * B))
+    out = c.attend(q.cuda(), index([w] * B), w, causal=False, scale=math.log(2.0)).double().cpu()   # log2 scores: 3 q, 4 q
+    weight = out[..., :splits] / torch.bincount(of, minlength=splits).double()
+    assert not out[..., splits:].any()
+    for s in range(splits):
+        want = 2.0 ** ((s % 2) * float(q[0, 0, 0, 0]))
+        off = (weight[..., s] / weight[..., 0] / want - 1).abs().max().item()
+        assert off <= 8 * 2.0 ** -24, f"split {s}: {off * 2 ** 24:.1f} halves of a last place"
