@@ -298,7 +298,8 @@ dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_
  * as far as the ring still holds them after the call's last token: size it for
  * window + n tokens (causal: one less).  A call that begins among the first
  * tokens needs as many slots less as it stores there, so windows and calls of
- * up to ring + sinks are taken; longer ones are refused (DC_ERANGE).
+ * up to ring + sinks are taken; longer ones are refused (DC_ERANGE).  A query
+ * that sees nothing gives 0, one whose scores are infinite NaN.
  * out's rows may be q's.
  * workspace: dc_carry4_workspace() device bytes, 16-byte aligned (NULL where
  * that is 0), not shared with a call that may run at the same time.  Sums and

@@ -568,6 +568,16 @@ struct KeyList {
     }
 };
 
+// 1 / l for the result of token i's row.  l = 0: the row sees nothing and its
+// result is 0, or every score that it sees is -infinity (an infinite query) and
+// there is no softmax: NaN, as for the other infinities.
+__device__ __forceinline__ float inverse_sum(const Attend4Params& p, const Span& sp, int i, float l)
+{
+    if (__builtin_expect(l != 0.0f, 1)) return 1.0f / l;
+    const RowSpan r = KeyList(p, sp, i, i).row(p, sp, i);
+    return r.sink_hi > 0 || r.hi > r.lo ? NAN : 0.0f;
+}
+
 template <int D> struct Tile4 {   // a lane's part of 32 keys' and values' codes and scales
     static constexpr int W = D / 32;   // words
     uint32_t k[2][W], v[2][W], ks[2], vs[2];
@@ -845,7 +855,7 @@ __global__ __launch_bounds__(256, !BF16 && !FOLD ? 1 : D == 128 ? 4 : 5) void at
         const int row = row0 + q;
         if (p.splits == 1) {
             const int i = row / p.group, hq = h * p.group + row % p.group;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const float inv = inverse_sum(p, sp, i, l);
             const int64_t at = p.o.at(p.sp.div, e, i, hq) + d;
             if (p.wide_out) {
                 store4<BF16>(p.o.p, at, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
@@ -1132,7 +1142,7 @@ __global__ __launch_bounds__(64 * NW, QG == 2 ? (D == 64 ? 3 : 2) : BF16 ? (D ==
         const int64_t at = p.o.at(p.sp.div, e, i, hq);
         const int64_t part = ((int64_t)eh * p.sp.n * p.group + row) * p.splits + split;
         const int64_t parts = (int64_t)regions * p.sp.n * p.group * p.splits;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = p.splits > 1 ? 0.0f : inverse_sum(p, sp, i, l);
 #pragma unroll
         for (int b = 0; b < DB; b++) {
             f32x4 x = o[u][b];
@@ -1210,8 +1220,8 @@ template <bool BF16, int D, int NG> __global__ __launch_bounds__(256) void atten
         }
     }
     if (!on) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int i = row / p.group, hq = h * p.group + row % p.group;
+    const float inv = inverse_sum(p, sp, i, l);
     const int64_t at = p.o.at(p.sp.div, e, i, hq) + d;
     if (p.wide_out) {
         store4<BF16>(p.o.p, at, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});

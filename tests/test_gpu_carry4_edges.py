@@ -112,3 +112,37 @@ def test_splits_meet_with_exact_weights(shape):
         want = 2.0 ** ((s % 2) * float(q[0, 0, 0, 0]))
         off = (weight[..., s] / weight[..., 0] / want - 1).abs().max().item()
         assert off <= 8 * 2.0 ** -24, f"split {s}: {off * 2 ** 24:.1f} halves of a last place"
+
+
+@each_type
+@each_shape
+def test_infinite_queries(shape, dtype):
+    """A query whose score is infinite for every key has no softmax: NaN, as
+    elsewhere, not the zeros of a query that sees nothing; no other row's bits touched."""
+    B, n, Hq, H, D, _, w = shape
+    T, k, v, q, run = turn(shape, dtype)
+    k[..., 5] = k[..., 5].abs() + 3   # (held as it is or rounded, never as zero)
+    want = run(k, v, q)
+    bad = torch.zeros(B, n, Hq, dtype=torch.bool)
+    for b, i, h, x in ((0, 0, 0, -math.inf), (B - 1, n - 1, Hq - 1, -math.inf), (B - 1, n // 2, 0, math.inf)):
+        q[b, i, h, 5] = x
+        bad[b, i, h] = True
+    got = run(k, v, q)
+    assert torch.equal(torch.isnan(got).cpu(), bad[..., None].expand_as(got))
+    assert torch.equal(got.cpu()[~bad], want.cpu()[~bad])
+
+
+@each_type
+@pytest.mark.parametrize("B,n,Hq,D", [(2, 20, 2, 64), (1, 4, 1, 128), (60, 200, 4, 64), (60, 200, 4, 128), (16, 2000, 1, 64), (48, 300, 4, 128)])
+def test_queries_that_see_nothing(B, n, Hq, D, dtype):
+    """A call longer than the ring, of entries past their first tokens that keep
+    none of them: early queries see no token at all and give 0."""
+    m = carry4()
+    ring, w = n // 2 + 1, n // 4
+    c = m.Carry4(B, 1, D, sinks=n, ring=ring)
+    c.memory.fill_(255)
+    k, v, q = rand((B, n, 1, D), dtype, 1), rand((B, n, 1, D), dtype, 2), rand((B, n, Hq, D), dtype, 3)
+    pos, keep = index([5 * n] * B), index([0] * B, torch.int32)
+    c.append(k, v, pos, sinks=keep)
+    out = c.attend(q, pos, w, sinks=keep, out=torch.full_like(q, 7.0))
+    assert not out[:, :n - ring].any() and out[:, n - ring:].any(-1).all() and not torch.isnan(out).any()
