@@ -277,13 +277,13 @@ hipError_t enqueue_attend4(const dc_flow_state* s, int i, int l, int b0, int Bc,
 struct Recorder {
     std::vector<std::string> role;
     std::vector<double> flops, bytes;
-    std::vector<int> mfma;
-    std::vector<hipEvent_t> ev;   // two per launch
+    std::vector<int> mfma, launches;
+    std::vector<hipEvent_t> ev;   // two per step: one launch, or a split attention's two
     size_t at = 0;
 };
 
 // The launches of one call over Bc streams from b0 with n frames per stream.
-// With a recorder, each launch is bracketed by events and described (role,
+// With a recorder, each step is bracketed by events and described (role,
 // algorithmic flops and bytes), and the state advance is left out.
 hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, const float* mu, const float* cond,
                         float* mel, hipStream_t st, int* count, Recorder* rec = nullptr)
@@ -305,7 +305,7 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
     }();
     std::string role;
     double fl = 0, by = 0;
-    int mf = 0;
+    int mf = 0, launches = 1;   // of the next step
     auto describe = [&](const char* r, double f, double b, int m) {
         role = r;
         fl = f;
@@ -331,9 +331,11 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
             rec->flops[rec->at] = fl;                                        \
             rec->bytes[rec->at] = by;                                        \
             rec->mfma[rec->at] = mf;                                         \
+            rec->launches[rec->at] = launches;                               \
             rec->at++;                                                       \
         }                                                                    \
-        k++;                                                                 \
+        k += launches;                                                       \
+        launches = 1;                                                        \
     } while (0)
 
     AssembleParams ap{mu, cond, s->spk, s->x, s->xin, s->pos, s->keys, c.rng_seed, c.temperature, n, b0, Bc, M};
@@ -401,9 +403,7 @@ hipError_t enqueue_call(dc_flow_state* s, int b0, int Bc, int n, int prompt, con
             describe("attn", 4.0 * 2 * c.heads * 64 * (double)n * ext_keys,
                      2.0 * 2 * c.heads * (double)ext_keys * kv_bytes + 2.0 * rows * D * es, 1);
             if (four) {
-                int launches = 1;
                 DCF_TRY(enqueue_attend4(s, i, l, b0, Bc, n, prompt, st, &launches));
-                k += launches - 1;
             } else {
                 DCF_TRY(launch_attn(at, Bc, bf, st));
             }
@@ -879,6 +879,7 @@ dc_status dc_flow_profile(dc_flow_state* s, int32_t reps, dc_flow_kernel_stat* o
     rec.flops.assign(nl, 0.0);
     rec.bytes.assign(nl, 0.0);
     rec.mfma.assign(nl, 0);
+    rec.launches.assign(nl, 0);
     rec.ev.assign(2 * (size_t)nl, nullptr);
     hipError_t e = hipSuccess;
     for (auto& ev : rec.ev)
@@ -909,7 +910,7 @@ dc_status dc_flow_profile(dc_flow_state* s, int32_t reps, dc_flow_kernel_stat* o
             groups.push_back(g);
             it = groups.end() - 1;
         }
-        it->launches++;
+        it->launches += rec.launches[i];
         it->us += us[i];
         it->flops += rec.flops[i];
         it->bytes += rec.bytes[i];
