@@ -302,11 +302,12 @@ dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_
  * that sees nothing gives 0, one whose scores are infinite NaN.
  * out's rows may be q's.
  * workspace: dc_carry4_workspace() device bytes, 16-byte aligned (NULL where
- * that is 0), not shared with a call that may run at the same time.  Sums and
- * statistics in fp32; with DC_BF16 the probabilities are rounded to bf16 for
- * the product with the values, with DC_F32 they are not.  The order of the sums
- * is fixed by the call's sizes (batch, heads, n, window, the carry's slots) and
- * type: the same call gives the same bits, whatever the other entries hold. */
+ * that is 0, as for sizes that the call refuses), not shared with a call that
+ * may run at the same time.  Sums and statistics in fp32; with DC_BF16 the
+ * probabilities are rounded to bf16 for the product with the values, with
+ * DC_F32 they are not.  The order of the sums is fixed by the call's sizes
+ * (batch, heads, n, window, the carry's slots) and type: the same call gives
+ * the same bits, whatever the other entries hold. */
 int64_t dc_carry4_workspace(const dc_carry4* c, int32_t q_heads, int32_t n, int32_t window);
 dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtype, const dc_head_rows* q,
                            const dc_head_rows* out, int32_t window, int32_t causal, float scale, void* workspace,

@@ -120,9 +120,11 @@ void set_norm(HeadsParams& p, const dc_qk_norm* m)
     p.eps = m->eps;
 }
 
-dc_status check_size(int64_t rows, int32_t head_dim)
+// Rows of a call: heads * batch * n.  (Quotients: the product may not fit 64 bits.)
+dc_status check_size(int64_t heads, int32_t batch, int32_t n, int32_t head_dim)
 {
-    CHECK(rows <= kMaxThreads / (head_dim / 4), DC_ERANGE, "the call has too many rows");
+    const int64_t most = kMaxThreads / (head_dim / 4);
+    CHECK(heads <= most / batch && (n == 0 || heads * batch <= most / n), DC_ERANGE, "the call has too many rows");
     return DC_OK;
 }
 
@@ -145,7 +147,7 @@ dc_status dc_qk_norm_rope(const dc_qk_norm* norm, const dc_span* span, int32_t h
     PASS(check_rows(q_out, span->n, dtype, "q_out"));
     PASS(check_rows(k_out, span->n, dtype, "k_out"));
     CHECK(q_out->heads == q->heads && k_out->heads == k->heads, DC_EINVAL, "outputs need as many heads as their inputs");
-    PASS(check_size(((int64_t)q->heads + k->heads) * span->batch * span->n, head_dim));
+    PASS(check_size((int64_t)q->heads + k->heads, span->batch, span->n, head_dim));
     if (span->n == 0) return DC_OK;
     HeadsParams p{};
     p.q = rows(q);
@@ -188,7 +190,7 @@ dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_
     } else {
         CHECK(!q && !q_out, DC_EINVAL, "q and q_out go with norm");
     }
-    PASS(check_size(heads * span->batch * span->n, c->head_dim));
+    PASS(check_size(heads, span->batch, span->n, c->head_dim));
     if (span->n == 0) return DC_OK;
     HeadsParams p{};
     p.k = rows(k);
@@ -210,6 +212,7 @@ dc_status dc_carry4_append(const dc_carry4* c, const dc_qk_norm* norm, const dc_
 int64_t dc_carry4_workspace(const dc_carry4* c, int32_t q_heads, int32_t n, int32_t window)
 {
     if (check_shape(c) != DC_OK || q_heads < 1 || q_heads % c->heads != 0 || n < 1 || window < 0) return 0;
+    if (check_size(q_heads, c->batch, n, c->head_dim) != DC_OK) return 0;
     int64_t bytes[2] = {0, 0};   // of fp32 and of bf16 rows
     for (int bf16 = 0; bf16 < 2; bf16++) attend4_splits(carry(c), c->batch, n, q_heads / c->heads, window, bf16, bytes + bf16);
     return std::max(bytes[0], bytes[1]);
@@ -232,7 +235,7 @@ dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtyp
     CHECK((int64_t)window + span->n - (causal ? 1 : 0) <= (int64_t)c->ring + c->sinks, DC_ERANGE,
           "the window and the call's tokens do not fit the carry");
     CHECK(std::isfinite(scale), DC_EINVAL, "scale must be finite");
-    PASS(check_size((int64_t)q->heads * span->batch * span->n, c->head_dim));
+    PASS(check_size(q->heads, span->batch, span->n, c->head_dim));
     if (span->n == 0) return DC_OK;
     Attend4Params p{};
     p.q = rows(q);
@@ -264,7 +267,7 @@ dc_status dc_carry4_read(const dc_carry4* c, const dc_span* span, int32_t dtype,
     PASS(check_rows(k, span->n, dtype, "k"));
     PASS(check_rows(v, span->n, dtype, "v"));
     CHECK(k->heads == c->heads && v->heads == c->heads, DC_EINVAL, "k and v need the carry's heads");
-    PASS(check_size(2 * (int64_t)c->heads * span->batch * span->n, c->head_dim));
+    PASS(check_size(2 * (int64_t)c->heads, span->batch, span->n, c->head_dim));
     if (span->n == 0) return DC_OK;
     Read4Params p{};
     p.c = carry(c);
