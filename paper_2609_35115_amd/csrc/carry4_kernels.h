@@ -8,10 +8,13 @@
 
 namespace dcf {
 
-template <class P> hipError_t launch_with(void (*kernel)(P), dim3 grid, dim3 block, hipStream_t st, P p)
+// A launch has fewer than 2^32 threads: more are refused here, since a launch that
+// fails leaves its error for the thread's next runtime call.
+template <class P> hipError_t launch_with(void (*kernel)(P), int64_t blocks, hipStream_t st, P p)
 {
+    if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
     void* args[] = {&p};
-    return hipLaunchKernel((const void*)kernel, grid, block, args, 0, st);
+    return hipLaunchKernel((const void*)kernel, dim3((unsigned)blocks), dim3(256), args, 0, st);
 }
 
 // An entry's span of a call.  Values that no caller may pass (a negative
@@ -346,7 +349,7 @@ template <bool BF16, int D> hipError_t launch_heads_d(HeadsParams p, hipStream_t
     const int parts = p.waves << p.split_bits;
     p.share = (jobs + parts - 1) / parts;
     const int64_t per = 4 / p.waves;   // groups of a block
-    return launch_with(heads_kernel<BF16, D>, dim3((unsigned)((groups + per - 1) / per << p.split_bits)), dim3(256), st, p);
+    return launch_with(heads_kernel<BF16, D>, (groups + per - 1) / per << p.split_bits, st, p);
 }
 
 hipError_t launch_heads(HeadsParams p, int D, int bf16, hipStream_t st)
@@ -416,7 +419,7 @@ template <bool BF16, int D> hipError_t launch_read4_d(Read4Params p, hipStream_t
     p.waves = groups < 1024 || jobs > 16 ? 4 : jobs > 4 ? 2 : 1;
     p.share = (jobs + p.waves - 1) / p.waves;
     const int64_t per = 4 / p.waves;
-    return launch_with(read4_kernel<BF16, D>, dim3((unsigned)xcd_blocks((groups + per - 1) / per)), dim3(256), st, p);
+    return launch_with(read4_kernel<BF16, D>, xcd_blocks((groups + per - 1) / per), st, p);
 }
 
 hipError_t launch_read4(const Read4Params& p, int bf16, hipStream_t st)
@@ -1315,19 +1318,19 @@ template <bool BF16, int D> hipError_t launch_attend4_d(const Attend4Params& p, 
 {
     const int64_t rows = (int64_t)p.sp.n * p.group;
     const int rb = plan4(p.c, p.entries, p.sp.n, p.group, p.window, BF16).rows;
-    const dim3 grid((unsigned)((int64_t)p.splits * p.entries * p.c.heads * ((rows + rb - 1) / rb)));
+    const int64_t blocks = (int64_t)p.splits * p.entries * p.c.heads * ((rows + rb - 1) / rb);
     hipError_t e = hipErrorInvalidValue;
-    if (rb == 16 && !BF16 && rows <= 4) e = launch_with(attend4_kernel<BF16, D, !BF16>, grid, dim3(256), st, p);
-    else if (rb == 16) e = launch_with(attend4_kernel<BF16, D, false>, grid, dim3(256), st, p);
-    else if (rb == 64 || !BF16) e = launch_with(attend4_wide<BF16, D, 1, 4>, grid, dim3(256), st, p);
-    else if constexpr (BF16) e = launch_with(attend4_wide<BF16, D, 2, 4>, grid, dim3(256), st, p);
+    if (rb == 16 && !BF16 && rows <= 4) e = launch_with(attend4_kernel<BF16, D, !BF16>, blocks, st, p);
+    else if (rb == 16) e = launch_with(attend4_kernel<BF16, D, false>, blocks, st, p);
+    else if (rb == 64 || !BF16) e = launch_with(attend4_wide<BF16, D, 1, 4>, blocks, st, p);
+    else if constexpr (BF16) e = launch_with(attend4_wide<BF16, D, 2, 4>, blocks, st, p);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t all = (int64_t)p.entries * p.c.heads * rows;
     // (of many rows a group takes one each: 8,000 rows in five splits 31 us with a
     // block a row, 21 with 16)
     constexpr int per = 256 / (D / 4);   // rows of a block, or groups of one row
-    if (p.splits <= 4 || all >= 2048) return launch_with(attend4_join<BF16, D, 1>, dim3((unsigned)((all + per - 1) / per)), dim3(256), st, p);
-    return launch_with(attend4_join<BF16, D, per>, dim3((unsigned)all), dim3(256), st, p);
+    if (p.splits <= 4 || all >= 2048) return launch_with(attend4_join<BF16, D, 1>, (all + per - 1) / per, st, p);
+    return launch_with(attend4_join<BF16, D, per>, all, st, p);
 }
 
 hipError_t launch_attend4(const Attend4Params& p, int bf16, hipStream_t st)

@@ -24,12 +24,13 @@ dc_status fail(dc_status code, const char* why)
 dc_status done(hipError_t e, const char* where)
 {
     if (e == hipSuccess) return DC_OK;
+    if (e == hipErrorInvalidConfiguration) return fail(DC_ERANGE, "the call has too many rows for a launch");
     std::snprintf(g_error, sizeof(g_error), "%s: %s", where, hipGetErrorString(e));
     return DC_EDEVICE;
 }
 
 constexpr int64_t kMaxSlots = 1 << 24;             // byte offsets inside a region fit 32 bits
-constexpr int64_t kMaxThreads = (int64_t)1 << 34;   // of a launch: rows and blocks fit 31 bits
+constexpr int64_t kMaxThreads = (int64_t)1 << 34;   // of a call's rows: rows and blocks fit 31 bits
 
 #define CHECK(cond, code, why) \
     do {                       \

@@ -42,3 +42,22 @@ def test_stores_and_reads_past_the_limit(k, n):
 @pytest.mark.parametrize("c", [carry(ring=(1 << 24) - 3), carry(batch=1 << 20, heads=1 << 1, head_dim=128)])
 def test_no_workspace_for_a_call_past_the_limit(c, q_heads, n):
     assert L.dc_carry4_workspace(byref(c), q_heads, n, 1 << 20) == 0
+
+
+# A launch has fewer than 2^24 blocks of 256 threads.
+
+@pytest.mark.parametrize("batch,heads,q", [(1 << 21, 8, 8), (1 << 23, 8, 16), (1 << 24, 4, 4)])
+def test_attention_of_more_regions_than_a_launch_has_blocks(batch, heads, q):
+    c = carry(batch=batch, heads=heads, sinks=0)
+    assert attend(c=c, s=span(batch=batch, n=1), q=rows(q), o=rows(q)) == dc.DC_ERANGE
+    assert b"too many rows" in L.dc_carry4_last_error()
+
+
+@pytest.mark.parametrize("D,n", [(64, 1 << 15), (128, 1 << 14)])
+def test_norms_and_stores_of_more_tokens_than_a_launch_has_blocks(D, n):
+    one, s = rows(1), span(batch=1 << 14, n=n)
+    assert rotate(s=s, D=D, q=one, k=one, qo=one, ko=one) == dc.DC_ERANGE
+    c = carry(batch=1 << 14, heads=1, head_dim=D)
+    assert append(c=c, s=s, k=one, v=one) == dc.DC_ERANGE
+    assert read(c=c, s=s, k=one, v=one) == dc.DC_ERANGE
+    assert b"too many rows" in L.dc_carry4_last_error()

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paper_2609_35115_amd import flow
+from paper_2609_35115_amd import DcError, flow
 from tests.test_gpu_carry4 import DT, carry4, index, rand
 
 pytestmark = pytest.mark.gpu
@@ -146,3 +146,16 @@ def test_queries_that_see_nothing(B, n, Hq, D, dtype):
     c.append(k, v, pos, sinks=keep)
     out = c.attend(q, pos, w, sinks=keep, out=torch.full_like(q, 7.0))
     assert not out[:, :n - ring].any() and out[:, n - ring:].any(-1).all() and not torch.isnan(out).any()
+
+
+def test_a_call_past_the_launch_limit_leaves_no_error():
+    """2^24 regions: refused, and the next runtime call finds no error of it."""
+    m = carry4()
+    B, H, D = 1 << 21, 8, 64
+    c = m.Carry4(B, H, D, sinks=0, ring=1)
+    k, pos = rand((1, 1, H, D), "bf16", 1).expand(B, 1, H, D), index([0]).expand(B).contiguous()
+    c.append(k, k, pos)
+    with pytest.raises(DcError, match="too many rows"):
+        c.attend(k, pos, 1, out=torch.empty_like(k).contiguous())
+    torch.cuda.synchronize()
+    assert torch.zeros(3, device="cuda").add_(1).sum().item() == 3
