@@ -72,6 +72,8 @@ def _rows(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int)
     b, t, h, d = shape
     if b != batch or t != n or d != head_dim or (heads and h != heads):
         _refuse(f"{name} must be [{batch}][{n}][{heads or 'heads'}][{head_dim}], not {list(shape)}")
+    if t > _INT32 or h > _INT32:
+        _refuse(f"{name}: tokens and heads must be below 2^31, not {t} and {h}")
     sb, st, sh, sd = x.stride()
     if sd != 1:
         _refuse(f"{name}: a head's elements must be consecutive")
@@ -106,8 +108,12 @@ def _vector(x, name: str, device, size) -> int:
 
 
 def _norm(device, head_dim: int, freqs, q_gain, k_gain, eps: float, interleaved: bool):
-    _pack_norm(_frame.norm_, 0, _vector(q_gain, "q_gain", device, head_dim), _vector(k_gain, "k_gain", device, head_dim),
-               _vector(freqs, "freqs", device, None), 0 if freqs is None else freqs.shape[0], int(interleaved), eps)
+    a, b = _vector(q_gain, "q_gain", device, head_dim), _vector(k_gain, "k_gain", device, head_dim)
+    f, nf = _vector(freqs, "freqs", device, None), 0 if freqs is None else freqs.shape[0]
+    try:
+        _pack_norm(_frame.norm_, 0, a, b, f, nf, int(interleaved), eps)
+    except (struct.error, OverflowError):
+        _refuse(f"eps or the number of frequencies does not fit its field: {eps}, {nf}")
     return _frame.norm
 
 
