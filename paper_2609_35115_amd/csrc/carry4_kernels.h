@@ -36,23 +36,19 @@ struct Span {
 };
 
 // Token `off` of the `per` that start at token t0 (of entries of n tokens each;
-// t0, n uniform): a 64-bit division a lane costs as much as a head's row.
+// t0, n uniform): a 64-bit division a lane costs as much as a head's row.  A call
+// has at most 2^30 rows, so its tokens' numbers fit 31 bits.
 struct Token {
     int e, i;   // of the last token, past the end
     bool on;
     __device__ __forceinline__ Token(int64_t t0, int off, int per, int entries, int n)
     {
-        const int64_t tokens = (int64_t)entries * n, t = t0 + off;
-        on = t < tokens;
-        if (tokens <= INT32_MAX) {
-            const uint32_t u = (uint32_t)min(t0, tokens - 1), e0 = u / (uint32_t)n, x = u - e0 * (uint32_t)n + off;
-            const uint32_t q = n >= per ? (x >= (uint32_t)n ? 1 : 0) : x / (uint32_t)n;
-            e = (int)(e0 + q);
-            i = (int)(x - q * (uint32_t)n);
-        } else {
-            e = (int)(min(t, tokens - 1) / n);
-            i = (int)(min(t, tokens - 1) % n);
-        }
+        const int64_t tokens = (int64_t)entries * n;
+        on = t0 + off < tokens;
+        const uint32_t u = (uint32_t)min(t0, tokens - 1), e0 = u / (uint32_t)n, x = u - e0 * (uint32_t)n + off;
+        const uint32_t q = n >= per ? (x >= (uint32_t)n ? 1 : 0) : x / (uint32_t)n;
+        e = (int)(e0 + q);
+        i = (int)(x - q * (uint32_t)n);
         if (!on) {
             e = entries - 1;
             i = n - 1;
@@ -60,8 +56,8 @@ struct Token {
     }
 };
 
-// Sum and maximum over aligned groups of LANES lanes (4, 8, 16 or 32), in
-// every lane, one fixed order.
+// Sum and maximum over aligned groups of LANES lanes (4, 8 or 16), in every
+// lane, one fixed order.
 template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v)
 {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
@@ -72,11 +68,6 @@ template <int LANES, class F> __device__ __forceinline__ uint32_t lanes_reduce(u
     v = f(v, dpp<0x4E>(v));                           // quad_perm 2 3 0 1
     if constexpr (LANES >= 8) v = f(v, dpp<0x141>(v));   // row_half_mirror: the other quad of eight lanes
     if constexpr (LANES >= 16) v = f(v, dpp<0x140>(v));  // row_mirror: the other eight of sixteen
-    if constexpr (LANES >= 32) {
-        const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        const uint32_t a0 = a[0], a1 = a[1];
-        v = f(a0, a1);
-    }
     return v;
 }
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
