@@ -5,7 +5,7 @@ from ctypes import byref
 import pytest
 
 from paper_2609_35115_amd import flow
-from tests import test_gpu_carry4_edges as edges, test_gpu_carry4_wide as wide
+from tests import test_gpu_carry4_edges as edges, test_gpu_carry4_wide as wide, test_gpu_flow_wide as flow_wide
 from tests.carry4_plan import plan
 from tests.test_carry4_args import carry
 
@@ -39,3 +39,13 @@ def test_block_calls(call, f32, bf16):
 @pytest.mark.parametrize("call,f32,bf16", wide.FAR)
 def test_far_calls(call, f32, bf16):
     assert plan(*call, "f32") == f32 and plan(*call, "bf16") == bf16
+
+
+@pytest.mark.parametrize("name", list(flow_wide.ARCHS))
+def test_flow_calls(name):
+    """Entries are streams times guidance branches; every call's carry has the same slots."""
+    a, chunk, prompt = flow_wide.ARCHS[name]
+    h, slots = a["heads"], (a["f_prompt"], a["f_retained"], a["f_retained"] + a["f_call"])
+    for dtype in ("f32", "bf16"):
+        assert plan(2 * flow_wide.B, a["f_call"], h, h, 64, *slots, dtype) == chunk
+        assert plan(2, a["f_prompt"], h, h, 64, *slots, dtype) == prompt
