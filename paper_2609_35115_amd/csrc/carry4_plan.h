@@ -71,7 +71,8 @@ inline Plan4 plan4(int D, int sinks, int ring, int64_t regions, int n, int group
     if (blocks <= 64) return {wide ? 128 : 64, (int)std::max(split(blocks, 256, 256), split(blocks, 512, 1024))};
     int best = 1;
     double least = 0.0;
-    for (int s = 1; s <= 8 && (s == 1 || most >= 256 * s); s++) {
+    // (of very many blocks, splits balance the last few only, and could pass a launch's 2^24)
+    for (int s = 1; s <= 8 && (s == 1 || (most >= 256 * s && blocks * s <= 1 << 20)); s++) {
         const int64_t k = (blocks * s + 255) / 256;
         double cost = us * (own * (double)((k + fit - 1) / fit) + (double)k) * (double)(most / 64 + 1) / s;
         if (s > 1) cost += 2.0 + (double)(regions * rows * s) * (D + 2) * 2e-6;   // the join, and its 8 bytes a value

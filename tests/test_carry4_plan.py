@@ -49,3 +49,22 @@ def test_flow_calls(name):
     for dtype in ("f32", "bf16"):
         assert plan(2 * flow_wide.B, a["f_call"], h, h, 64, *slots, dtype) == chunk
         assert plan(2, a["f_prompt"], h, h, 64, *slots, dtype) == prompt
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_splits_do_not_take_a_call_past_the_launch(D, dtype):
+    """Few or many regions of few or many rows over up to 2^24 slots: no more than 2^20
+    blocks by splitting (a launch has fewer than 2^24; from thousands of blocks a CU on
+    splits balance nothing)."""
+    split = 0
+    for regions in (1, 7, 300, 5000, 300_000, 1 << 22, 1 << 24):
+        for n in (1, 17, 56, 1000, 50_000, 1 << 26):
+            for slots in (458, 100_000, 1 << 24):
+                if regions * n > 1 << 28:
+                    continue
+                rows, splits = plan(regions, n, 1, 1, D, 0, slots, slots, dtype)
+                blocks = regions * -(-n // rows)
+                assert splits == 1 or blocks * splits <= 1 << 20, (regions, n, slots, blocks, splits)
+                split += splits > 1
+    assert split > 10
