@@ -89,8 +89,8 @@ HeadRows rows(const dc_head_rows* r) { return HeadRows{r->data, r->stride_b, r->
 
 bool wide(const dc_head_rows* r, int32_t dtype)
 {
-    const int64_t es = dtype == DC_BF16 ? 2 : 4;
-    return (uintptr_t)r->data % 16 == 0 && r->stride_b * es % 16 == 0 && r->stride_t * es % 16 == 0 && r->stride_h * es % 16 == 0;
+    const int64_t per = dtype == DC_BF16 ? 8 : 4;   // elements of 16 bytes
+    return (uintptr_t)r->data % 16 == 0 && r->stride_b % per == 0 && r->stride_t % per == 0 && r->stride_h % per == 0;
 }
 
 Carry4 carry(const dc_carry4* c)
