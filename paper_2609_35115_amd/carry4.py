@@ -80,6 +80,15 @@ def _rows(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int)
     return x.data_ptr(), sb, st, sh, h
 
 
+def _out(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int, *others):
+    """_rows of a result, whose rows have places of their own: none shared with
+    each other, nor with the row sets `others` (by their first element)."""
+    r = _rows(x, name, device, dtype, batch, n, heads, head_dim)
+    if (r[1] == 0 and batch > 1) or (r[2] == 0 and n > 1) or (r[3] == 0 and r[4] > 1) or (r[0] and r[0] in others):
+        _refuse(f"{name}: rows that overlap each other's, or those of another argument")
+    return r
+
+
 def _index(x, name: str, device, dtype, batch: int) -> int:
     """Address of a device array [batch] (None: NULL)."""
     if x is None:
@@ -144,7 +153,8 @@ def qk_norm_rope(q, k, pos, freqs, q_gain=None, k_gain=None, eps: float = 1e-6, 
     RMS norm per head with the gains [head_dim], then the rotation by
     (pos[b] + i) * freqs [n_freqs] of the first 2 n_freqs dimensions (freqs
     None: no rotation).  pos int64 [batch], lens int32 [batch] or None.  out:
-    the two results' tensors, which may be q and k themselves; rows behind
+    the two results' tensors, which may be q and k themselves (in that order)
+    and share no memory with another argument otherwise; rows behind
     lens are left as they are (zeros where out is None)."""
     dt = _dtype(q, "q")
     device, dtype = q.device, q.dtype
@@ -154,7 +164,8 @@ def qk_norm_rope(q, k, pos, freqs, q_gain=None, k_gain=None, eps: float = 1e-6, 
         new = _torch.empty if lens is None else _torch.zeros
         out = (new(q.shape, dtype=dtype, device=device), new(k.shape, dtype=dtype, device=device))
     qo, ko = out
-    c, d = _rows(qo, "out[0]", device, dtype, B, n, Hq, D), _rows(ko, "out[1]", device, dtype, B, n, b[4], D)
+    c = _out(qo, "out[0]", device, dtype, B, n, Hq, D, b[0])
+    d = _out(ko, "out[1]", device, dtype, B, n, b[4], D, a[0], c[0])
     m, s = _norm(device, D, freqs, q_gain, k_gain, eps, interleaved), _span(device, B, n, pos, lens, None)
     _pack_rows[4](_frame.rows_, 0, *a, *b, *c, *d)
     _launch(device, flib().dc_qk_norm_rope, m, s, D, dt, *_frame.rows)
@@ -206,7 +217,7 @@ class Carry4:
         r = _rows(q, "q", self.device, k.dtype, self.batch, n, None, self.head_dim)
         if out is None:
             out = (_torch.empty if lens is None else _torch.zeros)(q.shape, dtype=q.dtype, device=self.device)
-        o = _rows(out, "out", self.device, k.dtype, self.batch, n, r[4], self.head_dim)
+        o = _out(out, "out", self.device, k.dtype, self.batch, n, r[4], self.head_dim, a[0], b[0])
         m = _norm(self.device, self.head_dim, freqs, q_gain, k_gain, eps, interleaved)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
         _pack_rows[4](_frame.rows_, 0, *r, *a, *b, *o)
@@ -226,7 +237,7 @@ class Carry4:
         a = _rows(q, "q", self.device, dtype, self.batch, n, None, self.head_dim)
         if out is None:
             out = (_torch.empty if lens is None else _torch.zeros)(q.shape, dtype=dtype, device=self.device)
-        o = _rows(out, "out", self.device, dtype, self.batch, n, a[4], self.head_dim)
+        o = _out(out, "out", self.device, dtype, self.batch, n, a[4], self.head_dim)
         s = _span(self.device, self.batch, n, pos, lens, sinks)
         L = flib()
         size = L.dc_carry4_workspace(self._ref, a[4], n, window)
