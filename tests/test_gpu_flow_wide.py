@@ -13,6 +13,7 @@ import numpy as np
 import pytest
 
 from paper_2609_35115_amd import synth
+from tests.carry4_plan import plan
 from tests.gpu_common import TOL, err_stats, say
 from tests.test_gpu_flow import _prompts, _run_gpu, _run_oracle
 from tests.test_gpu_flow_options import QK, _audit
@@ -56,4 +57,21 @@ def test_chunk_calls_match_oracle(name, dtype):
             say(f"  {name} {dtype} stream {b} call {k}: max-abs/RMS {e:.3e} of {tol:.3e}, RMS {rms:.3e}")
             assert np.isfinite(g[b]).all() and e <= tol
         _audit(dec, s, a, dtype, b, [(0, 0, 0, 0), (0, 0, 1, 1)])
+    dec.close()
+
+
+@pytest.mark.parametrize("B", [1, 2, 16])
+def test_every_length_has_its_workspace(B):
+    """Prompt passes and chunk calls of lengths whose keys are split differently:
+    none needs more than the state has placed (such a call is refused), and a split
+    result is finite."""
+    a = dict(SPLIT, depth=1, n_steps=1)
+    plans = {plan(e, n, 2, 2, 64, 500, 420, 495, "bf16") for e, most in ((2 * B, 75), (2, 500)) for n in range(1, most + 1)}
+    assert len(plans) > 1 and max(s for _, s in plans) > 1
+    dec, _, mu, _ = _run_gpu(a, "bf16", synth.make_flow_weights(a, 1), B, a["f_prompt"], [])
+    for n in list(range(1, 76)):
+        assert np.isfinite(dec.decode(mu[:, :n]).cpu().numpy()).all(), n
+    for frames in (1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 128, 129, 250, 499, 500):
+        dec.prompt(B - 1, *synth.make_flow_prompt(a, frames, seed=frames))
+        assert np.isfinite(dec.decode(mu[:, :75]).cpu().numpy()).all(), frames
     dec.close()
