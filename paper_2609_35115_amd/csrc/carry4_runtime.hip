@@ -235,7 +235,8 @@ dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtyp
     // (a call that begins among the first tokens puts up to `sinks` of its own there)
     CHECK((int64_t)window + span->n - (causal ? 1 : 0) <= (int64_t)c->ring + c->sinks, DC_ERANGE,
           "the window and the call's tokens do not fit the carry");
-    CHECK(std::isfinite(scale), DC_EINVAL, "scale must be finite");
+    const float scale_log2 = scale * 1.4426950408889634f;
+    CHECK(std::isfinite(scale_log2), DC_EINVAL, "scale and scale * log2(e) must be finite");
     PASS(check_size(q->heads, span->batch, span->n, c->head_dim));
     if (span->n == 0) return DC_OK;
     Attend4Params p{};
@@ -247,7 +248,7 @@ dc_status dc_carry4_attend(const dc_carry4* c, const dc_span* span, int32_t dtyp
     p.group = q->heads / c->heads;
     p.window = window;
     p.causal = causal ? 1 : 0;
-    p.scale_log2 = scale * 1.4426950408889634f;
+    p.scale_log2 = scale_log2;
     p.wide_in = wide(q, dtype);
     p.wide_out = wide(out, dtype);
     int64_t need = 0;

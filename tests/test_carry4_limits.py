@@ -61,3 +61,12 @@ def test_norms_and_stores_of_more_tokens_than_a_launch_has_blocks(D, n):
     assert append(c=c, s=s, k=one, v=one) == dc.DC_ERANGE
     assert read(c=c, s=s, k=one, v=one) == dc.DC_ERANGE
     assert b"too many rows" in L.dc_carry4_last_error()
+
+
+def test_scales_whose_product_with_log2_e_is_infinite():
+    """(A score of zero times it would be NaN.)"""
+    for scale in (3e38, -3e38, 2.3588e38):
+        assert attend(scale=scale) == dc.DC_EINVAL
+        assert b"scale" in L.dc_carry4_last_error()
+    none = rows(4, None)
+    assert attend(s=span(n=0), q=none, o=none, scale=2.3586e38) == dc.DC_OK
