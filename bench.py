@@ -95,7 +95,7 @@ def cpu_baseline(arch, dtype, blob, tokens, budget_s: float, f0=None, streams=(0
 
 
 FLOW_FRAME_RATE = 50.0   # frames per second of audio: 2 frames per 25 Hz token
-FLOW_SOURCES = ("flow_kernels.hip", "flow_internal.h")
+FLOW_SOURCES = ("flow_kernels.hip", "flow_internal.h", "dc_philox.h", "carry4_kernels.h", "carry4_internal.h", "carry4_plan.h")
 
 
 def kernel_source_hash(files=("dc_kernels.hip", "dc_internal.h")) -> str:

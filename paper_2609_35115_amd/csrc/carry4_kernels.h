@@ -172,12 +172,16 @@ __device__ __forceinline__ float turn_fraction(int64_t pos, float freq)
 // infinity it would turn a masked probability of zero into NaN.
 //
 // What bounds it: HBM.  Norm and rotation of 32,768 tokens of 40 heads of 128 (671 MB)
-// 129 us, 5.2 TB/s; of 14,336 of 16 heads of 64 14.3 us.  A load of the next row
+// 129 us, 5.2 TB/s; of 14,336 of 16 heads of 64 (59 MB) 13.3 us, 17.6 where the 256 MB
+// last-level cache holds neither side.  A load of the next row
 // before this one is worked on, partners by DPP instead of LDS and one reciprocal
 // root took the first from 315 to 161, the block's shared sines to 139, 32-bit
-// divisions to 129.  The store of 16,384 tokens of 8 heads of 128 (85 MB) 23.8 us,
-// two thirds of its time the codes' stores (stores past the caches take 21.9, but
-// the attention that follows reads 3% slower).
+// divisions to 129.  The store of 16,384 tokens of 8 heads of 128 (85 MB) 22.9 us, 3.7
+// TB/s, and 16.9 over buffers that stay in the cache; two thirds of its time are the
+// codes' stores (stores past the caches took 8% less, but the attention that follows
+// read 3% slower).  Norm, rotation and store in one pass of 16,384 tokens of 32 and
+// twice 8 heads (353 MB) 72.7 us, 4.9 TB/s; of 14,336 of three times 8 of 64 (66 MB)
+// 23.0 us.
 // The value of the lane whose number differs by half a row's lanes (D = 64:
 // lane ^ 4; 128: lane ^ 8), without an LDS round trip.
 template <int L> __device__ __forceinline__ float half_row(float v)
@@ -473,9 +477,9 @@ hipError_t launch_carry4_gather(const Carry4& c, const Spans& sp, int e, int kv,
 // rows: a probability is rounded to bf16 for the product, half a step of the
 // result's own type; its sum is not.
 //
-// What bounds it: long lists HBM (131,004 keys of 128, 64 regions, 1.14 GB: 224 us,
-// 5.1 TB/s, the rate of a large copy; 242 at three waves a SIMD, the compiler's
-// choice without a bound), short ones latency (458 keys of 64: 7.2 us in a graph).
+// What bounds it: long lists HBM (131,004 keys of 128, 64 regions, 1.14 GB: 215 us,
+// 5.3 TB/s, the rate of a large copy; 8% more at three waves a SIMD, the compiler's
+// choice without a bound), short ones latency (458 keys of 64: 7.0 us in a graph).
 constexpr int kKeyTile = 32;
 
 template <int PL> struct Planes { bf16x8_t f[PL]; };
@@ -879,11 +883,11 @@ __global__ __launch_bounds__(256, !BF16 && !FOLD ? 1 : D == 128 ? 4 : 5) void at
 // is rarely rescaled; in bf16 the probabilities' sum is one more row of the
 // second product (ones, so the sum is of the rounded ones), not vector work.
 //
-// What bounds it: the vector unit.  56 queries over 458 keys of 64, 2,048 regions: 35 us
-// (67% of the cycles issue vector work, an exponential taking four; the matrix unit
-// 23%, LDS 49%); 80 where every 16 rows decoded the keys.  A causal prompt of 8,192
-// queries, 4 to a key head of 128, window 4,096: 289 us, 966 TFLOP/s; two waves a
-// SIMD whose vector (46%) and matrix work (39%) overlap only in part.
+// What bounds it: the vector unit.  56 queries over 458 keys of 64, 2,048 regions: 33 us
+// (65% of the cycles issue vector work, an exponential taking four; the matrix unit
+// 24%, LDS 52%); 80 where every 16 rows decoded the keys.  A causal prompt of 8,192
+// queries, 4 to a key head of 128, window 4,096: 290 us, 963 TFLOP/s; two waves a
+// SIMD whose vector (46%) and matrix work (42%) overlap only in part.
 // Queries scaled in two bf16 planes, so that scores come ready for the exponential,
 // were slower (38 us); so were waves of 32 rows for the short lists (44), and two
 // tiles in LDS, one decoded while the other is worked on (42: fewer waves a SIMD).
