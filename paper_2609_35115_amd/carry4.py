@@ -229,7 +229,12 @@ class Carry4:
         carry (which holds the call's own tokens already): the first tokens
         and, causal, the positions in (p - window, p] of a query at p; else
         those in [pos - window, pos + len) for all of an entry's queries.
-        scale: head_dim ** -0.5 by default.  out may be q itself."""
+        Only as far as the ring still holds them after the call's last token:
+        it needs window + n slots (causal: one less) for early queries to see
+        their whole window; calls of up to ring + sinks are taken, for entries
+        that begin among their first tokens, and past those an early query sees
+        fewer keys, or none (0).  scale: head_dim ** -0.5 by default.  out may
+        be q itself."""
         dt, dtype = _dtype(q, "q"), q.dtype
         if not 0 <= window <= _INT32:
             _refuse(f"window must be in [0, 2^31), not {window}")
