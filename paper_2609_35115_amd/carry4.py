@@ -84,7 +84,7 @@ def _out(x, name: str, device, dtype, batch: int, n: int, heads, head_dim: int, 
     """_rows of a result, whose rows have places of their own: none shared with
     each other, nor with the row sets `others` (by their first element)."""
     r = _rows(x, name, device, dtype, batch, n, heads, head_dim)
-    if (r[1] == 0 and batch > 1) or (r[2] == 0 and n > 1) or (r[3] == 0 and r[4] > 1) or (r[0] and r[0] in others):
+    if (r[1] == 0 and batch > 1) or (r[2] == 0 and n > 1) or (r[3] == 0 and r[4] > 1) or (n and r[0] in others):
         _refuse(f"{name}: rows that overlap each other's, or those of another argument")
     return r
 

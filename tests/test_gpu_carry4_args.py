@@ -66,3 +66,6 @@ def test_results_that_overlap():
     d = m.Carry4(1, 1, 64, sinks=0, ring=2)
     d.append(k[:1, :1, :1], k[:1, :1, :1], pos[:1])
     assert d.attend(q[:1, :1, :1], pos[:1], 1, out=single) is single and single.any()
+    # nor is a call of no tokens
+    a, b = m.qk_norm_rope(q[:, :0], k[:, :0], pos, f, out=(k[:, :0], k[:, :0]))
+    assert a.shape == (2, 0, 2, 64)
