@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadsParams p)
     // the rotation of this lane's dimensions (identity past rot): a group's 256
     // angles are shared out over its lanes
     float cs[8], sn[8];
-    const bool inter = p.interleaved != 0;
+    const bool inter = p.interleaved && p.rot;   // (without a rotation there are no cosines and sines)
     const int half = p.rot >> 1;
     const bool first = 8 * l < half;                     // half-split pairs: this lane holds the pairs' first members
     if (p.norm && p.rot) {

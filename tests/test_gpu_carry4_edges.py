@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2609_35115_amd import DcError, flow
-from tests.test_gpu_carry4 import DT, carry4, index, rand
+from tests.test_gpu_carry4 import DT, carry4, index, near, rand, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +159,26 @@ def test_a_call_past_the_launch_limit_leaves_no_error():
         c.attend(k, pos, 1, out=torch.empty_like(k).contiguous())
     torch.cuda.synchronize()
     assert torch.zeros(3, device="cuda").add_(1).sum().item() == 3
+
+
+@each_type
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+@pytest.mark.parametrize("B,n,Hq,H,D", [(1, 1, 1, 1, 64), (30, 687, 5, 2, 128), (256, 56, 8, 8, 64)])
+def test_norm_without_frequencies(B, n, Hq, H, D, interleaved, dtype):
+    """No rotation, whichever the pairing: the bits of one by frequencies of zero,
+    within the norm's bound, and the same keys stored."""
+    m = carry4()
+    q, k, pos = rand((B, n, Hq, D), dtype, 1), rand((B, n, H, D), dtype, 2), index([10 ** 9 + b for b in range(B)])
+    a, b = m.qk_norm_rope(q, k, pos, None, interleaved=interleaved)
+    for got, x in ((a, q), (b, k)):
+        want = turned(x, None, pos, None, 1e-6, False)
+        rel = 2.0 ** -8 if dtype == "bf16" else 0.0
+        near(got, want, rel, 2.0 ** -18 * want.abs().amax(-1, keepdim=True) * (1 + rel))
+    zero = torch.zeros(D // 2, device="cuda")
+    x, y = m.qk_norm_rope(q, k, pos, zero, interleaved=interleaved)
+    assert bool(torch.equal(a, x)) and bool(torch.equal(b, y))
+    c, d = (m.Carry4(B, H, D, sinks=0, ring=n) for _ in range(2))
+    x = c.append_rotated(q, k, k, pos, None, interleaved=interleaved)
+    y = d.append_rotated(q, k, k, pos, zero, interleaved=interleaved)
+    assert bool(torch.equal(x, a)) and bool(torch.equal(y, a))
+    assert all(bool(torch.equal(x, y)) for x, y in zip(c.read(pos, n), d.read(pos, n)))
