@@ -201,7 +201,8 @@ void dc_flow_free(dc_flow_state* s);
  * only its first lens[e] tokens (0 .. n); rows behind them are neither read
  * nor written.  These arrays are read on the device, so a captured call takes
  * their values at each replay.  Values out of range are taken as the nearest
- * that is in range; an entry with a negative position has no tokens.
+ * that is in range; an entry with a negative position, or one past 2^60, has
+ * no tokens.
  *
  * The carry keeps, per entry and key head, the first `sinks` tokens of a turn
  * (the prompt) in slots of their own and the tokens after them in a ring of

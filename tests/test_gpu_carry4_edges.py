@@ -182,3 +182,26 @@ def test_norm_without_frequencies(B, n, Hq, H, D, interleaved, dtype):
     y = d.append_rotated(q, k, k, pos, zero, interleaved=interleaved)
     assert bool(torch.equal(x, a)) and bool(torch.equal(y, a))
     assert all(bool(torch.equal(x, y)) for x, y in zip(c.read(pos, n), d.read(pos, n)))
+
+
+def test_device_values_out_of_range():
+    """Lengths past the call's and below zero, first tokens past the carry's and below
+    zero, positions below zero and past 2^60: the nearest, or no tokens; nothing else
+    of the carry is touched."""
+    m = carry4()
+    B, n, H, D, S, R = 6, 5, 2, 64, 3, 9
+    k, v, q = (rand((B, n, H, D), "f32", s) for s in (1, 2, 3))
+    pos = index([4, 4, -1, 2 ** 60 + 1, 2 ** 60, -2 ** 63])
+    lens, keep = index([99, -5, 5, 5, 2 ** 31 - 1, 5], torch.int32), index([77, -2, 0, 0, -2 ** 31, 0], torch.int32)
+    pos2, lens2, keep2 = index([4, 4, 0, 0, 2 ** 60, 0]), index([5, 0, 0, 0, 5, 0], torch.int32), index([3, 0, 0, 0, 0, 0], torch.int32)
+    freqs = torch.linspace(1, 0.01, 32).cuda()
+    got = []
+    for p, l, s in ((pos, lens, keep), (pos2, lens2, keep2)):
+        c = m.Carry4(B, H, D, sinks=S, ring=R)
+        c.memory.fill_(9)
+        r = c.append_rotated(q, k, v, p, freqs, lens=l, sinks=s)
+        got.append([r, c.attend(r, p, 4, lens=l, sinks=s, causal=False), *c.read(p, n, lens=l, sinks=s), c.memory.clone(),
+                    *m.qk_norm_rope(q, k, p, freqs, lens=l)])
+    for x, y in zip(*got):
+        assert bool(torch.equal(x, y))
+    assert not got[0][1][[1, 2, 3, 5]].any() and got[0][1][[0, 4]].any()
