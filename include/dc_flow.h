@@ -322,6 +322,132 @@ dc_status dc_carry4_read(const dc_carry4* c, const dc_span* span, int32_t dtype,
 /* Text of the calling thread's last error of these calls. */
 const char* dc_carry4_last_error(void);
 
+/* ------------------------------------------------ operators of a block
+ *
+ * What a transformer block runs around its attention, over tensors of the
+ * caller's: the norms before and after a sublayer with its gate and residual, a
+ * matrix product with an epilogue, and a paged cache of keys and values with
+ * the attention over it.  Streams, capture, errors, `lens` and rows behind them
+ * are as for the attention operators above; dc_block_last_error() explains the
+ * calling thread's last error.  Element types are named per argument: DC_F32
+ * or DC_BF16. */
+
+/* Entries of a call: `batch` of `n` tokens each, of which entry e has its first
+ * lens[e] (0 .. n) only; lens NULL: n each. */
+typedef struct dc_call {
+    const int32_t* lens;      /* device [batch] or NULL                                         */
+    int32_t batch, n;
+} dc_call;
+
+/* Rows of tokens: token i of entry e at data + e stride_b + i stride_t, in
+ * elements; a row's elements are consecutive.  A stride of 0 gives the entries,
+ * or the tokens of an entry, one row (inputs only). */
+typedef struct dc_rows {
+    void* data;               /* device, aligned to its elements                                */
+    int64_t stride_b, stride_t;
+    int32_t dtype;
+} dc_rows;
+
+#define DC_NORM_RMS 1
+#define DC_NORM_LAYER 2
+/* x / sqrt(mean(x^2) + eps) gain + bias, of x less its mean with DC_NORM_LAYER.
+ * The mean square plus eps has to be a normal fp32 number. */
+typedef struct dc_norm {
+    int32_t kind;             /* DC_NORM_RMS, DC_NORM_LAYER                                     */
+    float eps;                /* >= 0                                                           */
+    const float* gain;        /* device [width], or NULL: ones                                  */
+    const float* bias;        /* device [width], or NULL: zeros                                 */
+} dc_norm;
+
+/* The end of one sublayer and the start of the next, in one pass:
+ *   r = x_scale x + gate post(h)          the residual stream
+ *   y = pre(r) (1 + scale) + shift        the next sublayer's input
+ * r enters the second line before it is rounded.  h NULL: r = x_scale x (post
+ * and gate NULL).  post NULL: h itself; gate NULL: ones.  r_out NULL: r is not
+ * stored; y_out NULL (with pre, scale and shift): only r.  pre NULL: r itself.
+ * scale and shift NULL: zeros.  Widths of 1 to 16384.  r_out may be x or h,
+ * y_out h or x (the same rows, types of one size); otherwise rows may not
+ * overlap.  Sums in fp32, one rounding of each result. */
+dc_status dc_norm_residual(const dc_call* call, int32_t width, const dc_rows* x, float x_scale, const dc_rows* h,
+                           const dc_norm* post, const dc_rows* gate, const dc_rows* r_out, const dc_norm* pre,
+                           const dc_rows* scale, const dc_rows* shift, const dc_rows* y_out, void* hip_stream);
+
+#define DC_ACT_NONE 0
+#define DC_ACT_GELU 1         /* 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3)))              */
+#define DC_ACT_SILU 2         /* v / (1 + exp(-v))                                              */
+/* A Linear layer as PyTorch holds it.  With `glu` the weight (and the bias) has
+ * 2 n_out rows: the first n_out are activated, the others multiplied with the
+ * result. */
+typedef struct dc_linear_layer {
+    const void* weight;       /* device [n_out or 2 n_out][n_in], rows `stride` elements apart  */
+    const float* bias;        /* device, one value a row, or NULL                               */
+    int64_t stride;           /* >= n_in                                                        */
+    int32_t n_in, n_out;      /* 1 .. 2^24                                                      */
+    int32_t dtype;            /* of the weight and of x                                         */
+    int32_t act, glu;
+} dc_linear_layer;
+
+/* out = residual_scale residual + gate act(x weight^T + bias), accumulated in
+ * fp32, rounded once.  gate (ones where NULL), residual (zeros where NULL) and
+ * out in either type; out may be residual (the same rows and type), and shares
+ * no memory with another argument otherwise.  workspace: dc_linear_workspace()
+ * device bytes, 16-byte aligned (NULL where that is 0), not shared with a call
+ * that may run at the same time.  The order of the sums is fixed by the call's
+ * sizes (batch, n, n_in, n_out), types and alignment: the same call gives the
+ * same bits, whatever the other rows hold. */
+int64_t dc_linear_workspace(const dc_linear_layer* layer, int32_t batch, int32_t n);
+dc_status dc_linear(const dc_call* call, const dc_linear_layer* layer, const dc_rows* x, const dc_rows* gate,
+                    const dc_rows* residual, float residual_scale, const dc_rows* out, void* workspace,
+                    int64_t workspace_bytes, void* hip_stream);
+
+/* A cache of keys and values in pages of the caller's pool: position p of entry
+ * e lies in row p mod page_size of page table[e * table_stride + p / page_size]
+ * (a prompt's pages can stand in the tables of several entries).  A page number
+ * outside the pool is a hole: its tokens are not stored, and no query sees
+ * them.  Positions from table_pages * page_size on are none either.  The table
+ * is read on the device. */
+#define DC_PAGED_ABI_VERSION 1
+typedef struct dc_paged {
+    int32_t abi_version;      /* DC_PAGED_ABI_VERSION                                           */
+    int32_t batch, heads;     /* entries, key / value heads                                     */
+    int32_t head_dim;         /* 64 or 128                                                      */
+    int32_t dtype;            /* of keys, values and the calls' rows                            */
+    int32_t page_size;        /* tokens of a page, a power of two                               */
+    int32_t pages;            /* of the pool (>= 1)                                             */
+    int32_t table_pages;      /* of an entry (>= 1); page_size * table_pages <= 2^30            */
+    const int32_t* table;     /* device                                                         */
+    int64_t table_stride;     /* elements from entry to entry                                   */
+    void* k;                  /* device: row t of page g and head h at g stride_page +          */
+    void* v;                  /*   t stride_t + h stride_h, in elements; rows aligned to 16     */
+    int64_t k_stride_page, k_stride_t, k_stride_h;   /*   bytes                                 */
+    int64_t v_stride_page, v_stride_t, v_stride_h;
+} dc_paged;
+
+/* Store the span's keys and values (rows of the cache's heads and type) at
+ * their positions.  The span's sinks are not read.  Where a page stands in the
+ * tables of two entries that both write to it, either's rows may be kept. */
+dc_status dc_paged_append(const dc_paged* c, const dc_span* span, const dc_head_rows* k, const dc_head_rows* v,
+                          void* hip_stream);
+
+/* out = softmax(scale q k^T) v of the span's queries over the cache, which has
+ * to hold the call's own tokens already.  Query head h reads key head
+ * h / (q->heads / heads).  A query at position p sees the positions
+ *   causal:  up to p; with window > 0 of those the first `sinks` and the ones > p - window;
+ *   else:    in [0, pos + len) of its entry; with window > 0 of those the first
+ *            `sinks` and the ones >= pos - window, the same for all its queries.
+ * A query that sees nothing gives 0, one whose scores are infinite NaN; what a
+ * query does not see does not reach its result, whatever it holds.  The span's
+ * sinks are not read.  out's rows may be q's.  workspace and the sums' order:
+ * as for dc_carry4_attend, of dc_paged_workspace() bytes.  With DC_BF16 the
+ * probabilities are rounded to bf16 for the product with the values. */
+int64_t dc_paged_workspace(const dc_paged* c, int32_t q_heads, int32_t n, int32_t window, int32_t sinks);
+dc_status dc_paged_attend(const dc_paged* c, const dc_span* span, const dc_head_rows* q, const dc_head_rows* out,
+                          int32_t window, int32_t sinks, int32_t causal, float scale, void* workspace,
+                          int64_t workspace_bytes, void* hip_stream);
+
+/* Text of the calling thread's last error of these calls. */
+const char* dc_block_last_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,426 @@
+// gfx950 kernels of the matrix product with an epilogue:
+//   out = residual_scale residual + gate act(x W^T + bias).
+#include <algorithm>
+
+#include "block_internal.h"
+#include "dc_flow.h"
+
+namespace dcb {
+
+// Both operands' rows run along K, and both go to the matrix cores in chunks of
+// 16 bytes: a group of four consecutive chunks of a row (64 bytes) is what the
+// four lane groups of an operand hold, one each.  In bf16 that is one
+// 16x16x32 product, in fp32 four 16x16x4 ones, the t-th of element t of every
+// lane's chunk (a sum's terms in another order).  The weight is the first
+// operand: a lane's four results are four consecutive columns of one row.
+constexpr int kChunks = 8;   // chunks of a row that one K step takes (128 bytes)
+
+template <bool BF16> constexpr int chunk_elems() { return BF16 ? 8 : 4; }
+
+template <bool BF16> __device__ __forceinline__ f32x4 mma(u32x4 w, u32x4 x, f32x4 acc)
+{
+    if constexpr (BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; t++) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[t]), __uint_as_float(x[t]), acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+// A chunk at element k of a row of K, zeros past the row's end.
+template <bool BF16> __device__ __forceinline__ u32x4 load_chunk(const void* row, int k, int K)
+{
+    constexpr int CE = chunk_elems<BF16>();
+    if (k + CE <= K) return *(const u32x4_any*)((const char*)row + (int64_t)k * (16 / CE));
+    u32x4 c = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < CE - 1; j++) {
+        if (k + j >= K) break;
+        if constexpr (BF16) c[j >> 1] |= (uint32_t)((const uint16_t*)row)[k + j] << (16 * (j & 1));
+        else c[j] = ((const uint32_t*)row)[k + j];
+    }
+    return c;
+}
+
+// GELU in its tanh form, 0.5 v (1 + tanh z) = v / (1 + e^-2z): no cancellation for
+// negative v.
+template <bool EXACT> __device__ __forceinline__ float activate(float v, int act)
+{
+    if (act == DC_ACT_NONE) return v;
+    const float k2 = -2.0f * 0.7978845608028654f * 1.4426950408889634f;   // -2 sqrt(2 / pi) log2(e)
+    const float z = act == DC_ACT_GELU ? v * (k2 + k2 * 0.044715f * (v * v)) : v * -1.4426950408889634f;
+    const float d = 1.0f + __builtin_amdgcn_exp2f(z);
+    return EXACT ? v / d : v * __builtin_amdgcn_rcpf(d);   // 1 ulp, of a result that is rounded to bf16 next
+}
+
+struct Place {
+    int e, i;
+    bool on;
+    __device__ __forceinline__ Place(const LinearParams& p, int m)
+    {
+        const int mm = min(m, p.M - 1);
+        e = mm / p.call.n;
+        i = mm - e * p.call.n;
+        on = m < p.M && i < p.call.len(e);
+    }
+};
+
+// Columns n .. n + 3 of a row, from the sums a (and b, the factor's, with glu).
+__device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at, int n, f32x4 a, f32x4 b)
+{
+    if (!at.on || n >= p.N) return;
+    const int64_t o = at.e * p.out.sb + at.i * p.out.st + n;
+    const int64_t g = at.e * p.gate.sb + at.i * p.gate.st + n, r = at.e * p.res.sb + at.i * p.res.st + n;
+    if (n + 4 <= p.N) {
+        if (p.bias) {
+            a += load4(p.bias, n, 0);
+            if (p.glu) b += load4(p.bias, p.N + n, 0);
+        }
+        if (p.act) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) a[k] = p.out.bf16 ? activate<false>(a[k], p.act) : activate<true>(a[k], p.act);
+        }
+        if (p.glu) a *= b;
+        if (p.gate.p) a *= load4(p.gate.p, g, p.gate.bf16);
+        if (p.res.p) {
+            const f32x4 x = load4(p.res.p, r, p.res.bf16);
+#pragma unroll
+            for (int k = 0; k < 4; k++) a[k] = fmaf(p.res_scale, x[k], a[k]);
+        }
+        store4(p.out.p, o, p.out.bf16, a);
+        return;
+    }
+    for (int k = 0; k < 4 && n + k < p.N; k++) {
+        float v = a[k], w = b[k];
+        if (p.bias) {
+            v += p.bias[n + k];
+            if (p.glu) w += p.bias[p.N + n + k];
+        }
+        v = p.out.bf16 ? activate<false>(v, p.act) : activate<true>(v, p.act);
+        if (p.glu) v *= w;
+        if (p.gate.p) v *= load1(p.gate.p, g + k, p.gate.bf16);
+        if (p.res.p) v = fmaf(p.res_scale, load1(p.res.p, r + k, p.res.bf16), v);
+        store1(p.out.p, o + k, p.out.bf16, v);
+    }
+}
+
+// Partial sums of a split: [split][M][columns], a row's columns padded to four.
+__host__ __device__ inline int64_t part_row(int N, int glu) { return (int64_t)((N + 3) / 4 * 4) * (glu ? 2 : 1); }
+__device__ __forceinline__ void store_part(const LinearParams& p, int split, int m, int n, bool factor, f32x4 v)
+{
+    if (m >= p.M || n >= p.N) return;
+    *(f32x4*)(p.ws + ((int64_t)split * p.M + m) * part_row(p.N, p.glu) + (factor ? (p.N + 3) / 4 * 4 : 0) + n) = v;
+}
+
+// ----------------------------------------------------------- tiles of rows
+//
+// A block computes BM rows by BN columns (with glu BN / 2 columns and their
+// factors), its WM x WN waves a part each.  Both operands' K steps go through two
+// LDS buffers, the next one loaded while this one is multiplied; a row's eight
+// chunks are stored with their index XORed with the row's low bits, so that the
+// sixteen rows of an operand read lie in different banks.  With WIDE the loads go
+// from memory to LDS directly, else (rows or K not of whole chunks) through
+// registers.  Rows that the call does not have are read from the weight instead
+// and columns past N from its last row: their results are not stored.
+template <bool BF16, int BM, int BN, int WM, int WN, bool WIDE>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kernel(const LinearParams p)
+{
+    constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, CE = chunk_elems<BF16>(), ES = 16 / CE;
+    constexpr int KT = kChunks * CE, ROWS = BM + BN, LOADS = ROWS * kChunks / T;
+    constexpr int BUF = ROWS * kChunks * 16;
+    static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0);
+    __shared__ __align__(16) unsigned char smem[2 * BUF];
+    __shared__ int some;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
+    const int BC = p.glu ? BN / 2 : BN;                       // columns of a block
+    const int mt = (p.M + BM - 1) / BM, nt = (p.N + BC - 1) / BC;
+    // blocks are dealt to the eight XCDs in turn: each takes a run of the tiles, in
+    // strips of eight row tiles, whose operands its L2 holds
+    const int64_t blocks = (int64_t)mt * nt * p.splits;
+    int64_t id = blockIdx.x;
+    const int64_t eighth = blocks / 8;
+    if (id < eighth * 8) id = id % 8 * eighth + id / 8;
+    const int split = (int)(id % p.splits);
+    const int tile = (int)(id / p.splits), strip = tile / (8 * nt), in = tile - strip * 8 * nt;
+    const int high = min(8, mt - 8 * strip);
+    const int m0 = (8 * strip + in % high) * BM, n0 = in / high * BC;
+
+    // this thread's rows of the operands: chunk `tid % 8` of rows tid / 8 + c T / 8
+    if (tid == 0) some = 0;
+    __syncthreads();
+    const char* row[LOADS];
+    bool any = false;
+#pragma unroll
+    for (int c = 0; c < LOADS; c++) {
+        const int rr = tid / kChunks + c * (T / kChunks);
+        if (rr < BM) {
+            const Place at(p, m0 + rr);
+            any |= at.on;
+            row[c] = at.on ? (const char*)p.x.p + (at.e * p.x.sb + at.i * p.x.st) * ES : (const char*)p.w;
+        } else {
+            int r = rr - BM, col, part = 0;
+            if (p.glu) {   // a wave's first half of 16-column groups, and the same columns' factors
+                const int w = r / (BN / WN), f = r / 16 % NI;
+                part = f >= NI / 2;
+                col = n0 + w * (BN / WN / 2) + (f - part * (NI / 2)) * 16 + r % 16;
+            } else {
+                col = n0 + r;
+            }
+            row[c] = (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
+        }
+    }
+    if (any) some = 1;
+    __syncthreads();
+    if (!some) return;   // all rows are behind their entries' last tokens
+
+    const int kc = ((tid % kChunks) ^ (tid / kChunks & 7)) * CE;   // where in the K step this thread's chunk lies
+    const int steps = (p.K + KT - 1) / KT;
+    const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
+
+    u32x4 stage[WIDE ? 1 : LOADS];
+    __device__ static const u32x4 zeros = {0, 0, 0, 0};
+    auto fetch = [&](int s) {
+        const int k = s * KT + kc;
+        if constexpr (WIDE) {
+            unsigned char* to = smem + (s & 1) * BUF + wave * 1024;
+#pragma unroll
+            for (int c = 0; c < LOADS; c++)
+                __builtin_amdgcn_global_load_lds((const void*)(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros),
+                                                 (__attribute__((address_space(3))) void*)(to + c * (T * 16)), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<BF16>(row[c], k, p.K);
+        }
+    };
+    auto keep = [&](int s) {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int c = 0; c < LOADS; c++) *(u32x4*)(smem + (s & 1) * BUF + (c * T + tid) * 16) = stage[c];
+        }
+    };
+
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+
+    const int xr = (wm * (BM / WM) + l16) * 128, wr = (BM + wn * (BN / WN) + l16) * 128;
+    if (s0 < s1) {
+        fetch(s0);
+        keep(s0);
+    }
+    __syncthreads();
+    for (int s = s0; s < s1; s++) {
+        if (s + 1 < s1) fetch(s + 1);
+        const unsigned char* buf = smem + (s & 1) * BUF;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int ch = ((4 * h + g) ^ (l16 & 7)) * 16;
+            u32x4 x[MI], w[NI];
+#pragma unroll
+            for (int i = 0; i < MI; i++) x[i] = *(const u32x4*)(buf + xr + i * 2048 + ch);
+#pragma unroll
+            for (int j = 0; j < NI; j++) w[j] = *(const u32x4*)(buf + wr + j * 2048 + ch);
+#pragma unroll
+            for (int i = 0; i < MI; i++)
+#pragma unroll
+                for (int j = 0; j < NI; j++) acc[i][j] = mma<BF16>(w[j], x[i], acc[i][j]);
+        }
+        if (s + 1 < s1) keep(s + 1);
+        if constexpr (WIDE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the next step's loads are in LDS
+        __syncthreads();
+    }
+
+#pragma unroll
+    for (int i = 0; i < MI; i++) {
+        const int m = m0 + wm * (BM / WM) + 16 * i + l16;
+        const Place at(p, m);
+        if (p.glu) {
+#pragma unroll
+            for (int j = 0; j < NI / 2; j++) {
+                const int n = n0 + wn * (BN / WN / 2) + 16 * j + 4 * g;
+                if (p.splits > 1) {
+                    store_part(p, split, m, n, false, acc[i][j]);
+                    store_part(p, split, m, n, true, acc[i][j + NI / 2]);
+                } else {
+                    epilogue(p, at, n, acc[i][j], acc[i][j + NI / 2]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const int n = n0 + wn * (BN / WN) + 16 * j + 4 * g;
+                if (p.splits > 1) store_part(p, split, m, n, false, acc[i][j]);
+                else epilogue(p, at, n, acc[i][j], acc[i][j]);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------- few rows
+//
+// Calls of up to 16 MB rows: what counts is the weight's way from memory.  A block's
+// four waves share the K of NT sixteen-column groups (with glu one and its
+// factors) and all rows; weights and rows go from memory straight to the
+// operand registers, U groups of four chunks at a time, and the waves' sums meet
+// in LDS.
+template <bool BF16, int MB, int NT, bool WIDE>
+__global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
+{
+    constexpr int CE = chunk_elems<BF16>(), ES = 16 / CE, U = 4, KG = 4 * CE;   // elements of a group of chunks
+    __shared__ __align__(16) float sums[4][MB * NT * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g = lane >> 4;
+    const int BC = p.glu ? 16 : 16 * NT;
+    const int split = blockIdx.x % p.splits, n0 = blockIdx.x / p.splits * BC;
+
+    const char *xrow[MB], *wrow[NT];
+#pragma unroll
+    for (int i = 0; i < MB; i++) {
+        const Place at(p, 16 * i + l16);
+        xrow[i] = at.on ? (const char*)p.x.p + (at.e * p.x.sb + at.i * p.x.st) * ES : (const char*)p.w;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; j++) {
+        const int part = p.glu ? j : 0, col = n0 + (p.glu ? 0 : 16 * j) + l16;
+        wrow[j] = (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
+    }
+    const int groups = (p.K + KG - 1) / KG, parts = 4 * p.splits, part = 4 * split + wave;
+    const int g0 = (int)((int64_t)groups * part / parts), g1 = (int)((int64_t)groups * (part + 1) / parts);
+
+    auto chunk = [&](const char* r, int k) {
+        if constexpr (WIDE) return k < p.K ? *(const u32x4*)(r + (int64_t)k * ES) : u32x4{0, 0, 0, 0};
+        else return k < p.K ? load_chunk<BF16>(r, k, p.K) : u32x4{0, 0, 0, 0};
+    };
+    f32x4 acc[MB][NT];
+#pragma unroll
+    for (int i = 0; i < MB; i++)
+#pragma unroll
+        for (int j = 0; j < NT; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+    for (int q = g0; q < g1; q += U) {
+        u32x4 w[U][NT], x[U][MB];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int k = q + u < g1 ? (q + u) * KG + g * CE : p.K;   // (past this wave's part: zeros)
+#pragma unroll
+            for (int j = 0; j < NT; j++) w[u][j] = chunk(wrow[j], k);
+#pragma unroll
+            for (int i = 0; i < MB; i++) x[u][i] = chunk(xrow[i], k);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < MB; i++)
+#pragma unroll
+                for (int j = 0; j < NT; j++) acc[i][j] = mma<BF16>(w[u][j], x[u][i], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < MB; i++)
+#pragma unroll
+        for (int j = 0; j < NT; j++) *(f32x4*)(sums[wave] + ((i * NT + j) * 64 + lane) * 4) = acc[i][j];
+    __syncthreads();
+    // (wave w takes every fourth sixteen-by-sixteen group)
+    auto sum = [&](int ij) {
+        f32x4 v = *(const f32x4*)(sums[0] + (ij * 64 + lane) * 4);
+#pragma unroll
+        for (int w = 1; w < 4; w++) v += *(const f32x4*)(sums[w] + (ij * 64 + lane) * 4);
+        return v;
+    };
+    if (p.glu) {
+        for (int i = wave; i < MB; i += 4) {
+            const int m = 16 * i + l16, n = n0 + 4 * g;
+            const f32x4 a = sum(i * NT), b = sum(i * NT + NT - 1);
+            if (p.splits > 1) {
+                store_part(p, split, m, n, false, a);
+                store_part(p, split, m, n, true, b);
+            } else {
+                epilogue(p, Place(p, m), n, a, b);
+            }
+        }
+    } else {
+        for (int ij = wave; ij < MB * NT; ij += 4) {
+            const int m = 16 * (ij / NT) + l16, n = n0 + 16 * (ij % NT) + 4 * g;
+            const f32x4 a = sum(ij);
+            if (p.splits > 1) store_part(p, split, m, n, false, a);
+            else epilogue(p, Place(p, m), n, a, a);
+        }
+    }
+}
+
+// The splits' partial sums and the epilogue, four columns a thread.
+__global__ __launch_bounds__(256) void join_kernel(const LinearParams p)
+{
+    const int64_t quads = (p.N + 3) / 4, u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (u >= quads * p.M) return;
+    const int m = (int)(u / quads), n = 4 * (int)(u % quads);
+    const Place at(p, m);
+    if (!at.on) return;
+    const int64_t row = part_row(p.N, p.glu);
+    const float* s = p.ws + m * row + n;
+    f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    for (int k = 0; k < p.splits; k++, s += (int64_t)p.M * row) {
+        a += *(const f32x4*)s;
+        if (p.glu) b += *(const f32x4*)(s + (p.N + 3) / 4 * 4);
+    }
+    epilogue(p, at, n, a, b);
+}
+
+// ------------------------------------------------------------------ choice
+
+enum { kFew, kTile64, kTile128, kTile256 };
+
+LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
+{
+    LinearPlan pl{kFew, 1, 0};
+    const int64_t cols = (int64_t)N * (glu ? 2 : 1);
+    const int KT = bf16 ? 64 : 32, steps = (K + KT - 1) / KT;
+    if (M <= 64) {
+        const int nt = glu || M > 32 ? 2 : 1;
+        const int64_t blocks = (cols + 16 * nt - 1) / (16 * nt);
+        while (blocks * pl.splits < 256 && steps >= 16 * pl.splits && pl.splits < 16) pl.splits *= 2;
+    } else {
+        auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((cols + b - 1) / b); };
+        pl.kind = tiles(256) >= 192 ? kTile256 : tiles(128) >= 192 ? kTile128 : kTile64;
+        const int64_t blocks = tiles(pl.kind == kTile256 ? 256 : pl.kind == kTile128 ? 128 : 64);
+        while (blocks * pl.splits < 192 && steps >= 8 * pl.splits && pl.splits < 8) pl.splits *= 2;
+    }
+    if (pl.splits > 1) pl.ws_bytes = pl.splits * M * part_row(N, glu) * 4;
+    return pl;
+}
+
+template <bool BF16> hipError_t launch_linear_t(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
+{
+    hipError_t e = hipErrorInvalidValue;
+    if (plan.kind == kFew) {
+        const int nt = p.glu || p.M > 32 ? 2 : 1, bc = p.glu ? 16 : 16 * nt;
+        const int64_t blocks = (int64_t)((p.N + bc - 1) / bc) * p.splits;
+#define DCB_FEW(MB, NT) (p.wide ? launch_with(few_kernel<BF16, MB, NT, true>, blocks, 256, 0, st, p) : launch_with(few_kernel<BF16, MB, NT, false>, blocks, 256, 0, st, p))
+        if (nt == 1) e = p.M <= 16 ? DCB_FEW(1, 1) : DCB_FEW(2, 1);
+        else e = p.M <= 16 ? DCB_FEW(1, 2) : p.M <= 32 ? DCB_FEW(2, 2) : DCB_FEW(4, 2);
+#undef DCB_FEW
+    } else {
+        const int b = plan.kind == kTile64 ? 64 : plan.kind == kTile128 ? 128 : 256;
+        auto blocks = [&](int b) {
+            const int bc = p.glu ? b / 2 : b;
+            return (int64_t)((p.M + b - 1) / b) * ((p.N + bc - 1) / bc) * p.splits;
+        };
+        if (b == 64) e = p.wide ? launch_with(tile_kernel<BF16, 64, 64, 2, 2, true>, blocks(64), 256, 0, st, p)
+                                : launch_with(tile_kernel<BF16, 64, 64, 2, 2, false>, blocks(64), 256, 0, st, p);
+        else if (b == 256 && p.wide) e = launch_with(tile_kernel<BF16, 256, 256, 2, 4, true>, blocks(256), 512, 0, st, p);
+        else e = p.wide ? launch_with(tile_kernel<BF16, 128, 128, 2, 2, true>, blocks(128), 256, 0, st, p)
+                        : launch_with(tile_kernel<BF16, 128, 128, 2, 2, false>, blocks(128), 256, 0, st, p);
+    }
+    if (e != hipSuccess || p.splits == 1) return e;
+    return launch_with(join_kernel, ((int64_t)((p.N + 3) / 4) * p.M + 255) / 256, 256, 0, st, p);
+}
+
+hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
+{
+    return p.bf16 ? launch_linear_t<true>(p, plan, st) : launch_linear_t<false>(p, plan, st);
+}
+
+}  // namespace dcb

@@ -1,0 +1,713 @@
+// gfx950 kernels of the paged cache: the store of new keys and values, and the
+// attention of a call's tokens over the cache.
+#include <algorithm>
+#include <cfloat>
+
+#include "block_internal.h"
+
+namespace dcb {
+
+// An entry's span of a call.  Values that no caller may pass (a negative
+// position, a length past the call's) are taken as none and as the largest.
+struct Span {
+    int64_t pos, total;   // first position of the call, position after its last token
+    int len;
+    __device__ __forceinline__ Span(const PagedParams& p, int e)
+    {
+        pos = p.pos[e];
+        len = p.lens ? min(max(p.lens[e], 0), p.n) : p.n;
+        if (pos < 0 || pos > (int64_t)1 << 60) pos = len = 0;
+        total = pos + len;
+    }
+};
+
+// The page of position x of entry e (unsigned: a number outside the pool is
+// `pages` or more).
+__device__ __forceinline__ uint32_t page_of(const Paged& c, int e, int x) { return (uint32_t)c.table[e * c.table_stride + (x >> c.shift)]; }
+
+// ------------------------------------------------------------------- store
+//
+// A thread copies 16 bytes of a key and of its value.  What bounds it: HBM.
+template <int ES> __global__ __launch_bounds__(256) void append_kernel(const PagedParams p)
+{
+    constexpr int CE = 16 / ES;
+    const int cpr = p.c.D / CE, per = p.c.heads * cpr;   // chunks of a row, of a token
+    const uint64_t u = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t token = (uint32_t)(u / per), in = (uint32_t)(u - (uint64_t)token * per);
+    const int e = token / p.n, i = token - e * p.n, h = in / cpr, ch = in - h * cpr;
+    if (e >= p.c.batch) return;
+    const Span sp(p, e);
+    const int64_t x = sp.pos + i;
+    if (i >= sp.len || x >= p.c.limit) return;
+    const uint32_t page = page_of(p.c, e, (int)x);
+    if (page >= (uint32_t)p.c.pages) return;
+    const int off = (int)x & ((1 << p.c.shift) - 1);
+    const u32x4 a = *(const u32x4_any*)((const char*)p.k.p + (p.k.at(e, i, h) + ch * CE) * ES);
+    const u32x4 b = *(const u32x4_any*)((const char*)p.v.p + (p.v.at(e, i, h) + ch * CE) * ES);
+    *(u32x4*)(p.c.k + page * p.c.kp + off * p.c.kt + h * p.c.kh + 16 * ch) = a;
+    *(u32x4*)(p.c.v + page * p.c.vp + off * p.c.vt + h * p.c.vh + 16 * ch) = b;
+}
+
+hipError_t launch_append(const PagedParams& p, hipStream_t st)
+{
+    const int64_t threads = (int64_t)p.c.batch * p.n * p.c.heads * (p.c.D / (p.c.bf16 ? 8 : 4));
+    return p.c.bf16 ? launch_with(append_kernel<2>, (threads + 255) / 256, 256, 0, st, p)
+                    : launch_with(append_kernel<4>, (threads + 255) / 256, 256, 0, st, p);
+}
+
+// --------------------------------------------------------------- attention
+//
+// O = softmax(scale Q K^T) V.  A row is (token i, query head), the `group` query
+// heads of a key head side by side, so shared heads share the loads of their keys.
+// The keys that a block's rows see are one list of members: the first tokens
+// [0, ns), then the positions from `first` on; a row sees [0, sink_hi) and
+// [lo, hi) of it.
+//
+// S^T = K Q^T and O^T += V^T P^T, so that a lane (r, g) = (lane % 16, lane / 16)
+// holds of query r the scores of keys 4 g .. 4 g + 3 of every sixteen, and of its
+// result the dimensions 16 b + 4 g .. + 3.  bf16: a probability is rounded to bf16
+// for the product with the values, half a step of the result's own type.  fp32:
+// four 16x16x4 products of a 16-byte chunk's elements, in fp32 throughout.
+struct RowSpan {
+    int sink_hi, lo, hi;
+    __device__ __forceinline__ bool sees(int m) const { return (m < sink_hi) | ((uint32_t)(m - lo) < (uint32_t)max(hi - lo, 0)); }
+};
+
+struct KeyList {
+    int ns, nk, first;   // first tokens, members, position of the first of the others
+    __device__ __forceinline__ KeyList(const PagedParams& p, const Span& sp, int i0, int i1)
+    {
+        const int64_t limit = p.c.limit, end = min(p.causal ? sp.pos + i1 + 1 : sp.total, limit);
+        int64_t from = 0;
+        ns = 0;
+        if (p.window) {
+            from = max(p.causal ? sp.pos + i0 - p.window + 1 : sp.pos - p.window, (int64_t)p.sinks);
+            ns = (int)min(end, (int64_t)p.sinks);
+        }
+        first = (int)min(from, limit);
+        nk = ns + (int)max(end - from, (int64_t)0);
+    }
+    __device__ __forceinline__ int position(int m) const { return m < ns ? m : first + (m - ns); }
+    __device__ __forceinline__ RowSpan row(const PagedParams& p, const Span& sp, int i) const
+    {
+        RowSpan r{ns, ns, nk};
+        if (p.causal) {
+            const int64_t at = sp.pos + i, lo = at - p.window + 1;
+            r.sink_hi = (int)min((int64_t)ns, at + 1);
+            if (p.window) r.lo = ns + (int)min(max(lo - first, (int64_t)0), (int64_t)(nk - ns));
+            r.hi = ns + (int)min(max(at + 1 - first, (int64_t)0), (int64_t)(nk - ns));
+        }
+        return r;
+    }
+};
+
+template <bool BF16> __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 acc)
+{
+    if constexpr (BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; t++) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[t]), __uint_as_float(b[t]), acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ u32x4 read_tr(const unsigned char* lo, const unsigned char* hi)
+{
+    struct Two {
+        s16x4 a, b;
+    } two = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi)};
+    return __builtin_bit_cast(u32x4, two);
+}
+
+// Sets infinities and NaN among a chunk's elements to zero; whether there were any.
+template <bool BF16> __device__ __forceinline__ bool clear_special(u32x4& w)
+{
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const bool hi = (w[k] & 0x7f800000u) == 0x7f800000u;
+        if constexpr (BF16) {
+            const bool lo = (w[k] & 0x7f80u) == 0x7f80u;
+            any |= lo | hi;
+            w[k] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+        } else {
+            any |= hi;
+            if (hi) w[k] = 0;
+        }
+    }
+    return any;
+}
+
+// The base of a row's exponentials where it saw keys, all of whose scores are
+// -infinity: its result is NaN (there is no softmax), but not if a key of another
+// part has a finite score.  -infinity: it saw nothing.
+constexpr float kSawNothingFinite = -FLT_MAX;
+
+__device__ __forceinline__ float inverse(float l, float m) { return l != 0.0f ? 1.0f / l : m == -INFINITY ? 0.0f : NAN; }
+
+__device__ __forceinline__ bool any_lane_of_row(bool b)
+{
+    const uint64_t x = __ballot(b), y = x | x >> 32, z = y | y >> 16;
+    return (z >> (threadIdx.x & 15)) & 1;
+}
+
+__device__ __forceinline__ void store_result(const PagedParams& p, int e, int h, int row, int d, float inv, f32x4 x)
+{
+    const int i = row / p.group, hq = h * p.group + row % p.group;
+    store4(p.o.p, p.o.at(e, i, hq) + d, p.c.bf16, f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
+}
+// Partial results: the rows' sums [part][D], then base and sum of each.
+__device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int row, int split, int d, f32x4 x, float m, float l)
+{
+    const int64_t rows = (int64_t)p.n * p.group, part = (eh * rows + row) * p.splits + split;
+    const int64_t parts = (int64_t)p.c.batch * p.c.heads * rows * p.splits;
+    *(f32x4*)(p.ws + part * p.c.D + d) = x;
+    if (d == 0) {
+        p.ws[parts * p.c.D + 2 * part] = m;
+        p.ws[parts * p.c.D + 2 * part + 1] = l;
+    }
+}
+
+// Up to 16 rows a block.  Each of its four waves takes a tile of keys in turn,
+// straight from memory to registers, one tile ahead (the pages two ahead), with its
+// own running maximum and sums; the waves meet in LDS at the end.  Values go
+// through LDS, for transposed reads.
+template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few(const PagedParams p)
+{
+    constexpr int ES = BF16 ? 2 : 4, CE = 16 / ES, NB = BF16 ? 2 : 1, KT = 16 * NB;   // sixteens and keys of a tile
+    constexpr int KS = D * ES / 64, DB = D / 16;
+    constexpr int VROW = D * ES + (BF16 ? 32 : 16);   // bytes of a value row in LDS: its banks shift from row to row
+    constexpr int WAVE_LDS = KT * VROW > 16 * D * 4 + 128 ? KT * VROW : 16 * D * 4 + 128;
+    __shared__ __align__(16) unsigned char smem[4 * WAVE_LDS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int regions = p.c.batch * p.c.heads, split = blockIdx.x % p.splits;
+    const int eh = blockIdx.x / p.splits % regions, e = eh / p.c.heads, h = eh % p.c.heads;
+    const Span sp(p, e);
+    const int rows = sp.len * p.group, row0 = 16 * (blockIdx.x / p.splits / regions);
+    if (row0 >= rows) return;
+    const int last = min(row0 + 15, rows - 1), my_row = min(row0 + r, last);
+    const KeyList list(p, sp, row0 / p.group, last / p.group);
+    const RowSpan mine = list.row(p, sp, my_row / p.group);
+    const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
+    const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;   // from here on members are seen by every row
+
+    u32x4 qf[KS];
+    {
+        const char* q = (const char*)p.q.p + p.q.at(e, my_row / p.group, h * p.group + my_row % p.group) * ES;
+#pragma unroll
+        for (int c = 0; c < KS; c++) qf[c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
+    }
+    const int tiles = (list.nk + KT - 1) / KT;
+    const int t_lo = (int)((int64_t)tiles * split / p.splits), t_hi = (int)((int64_t)tiles * (split + 1) / p.splits);
+
+    f32x4 o[DB];
+#pragma unroll
+    for (int b = 0; b < DB; b++) o[b] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+    bool saw = false;
+
+    unsigned char* vt = smem + wave * WAVE_LDS;
+    u32x4 kn[NB][KS], vn[NB][KS];
+    uint32_t page[NB], hole_n = 0;
+    const char *kh = p.c.k + h * p.c.kh + 16 * g, *vh = p.c.v + h * p.c.vh + 16 * g;
+    auto find = [&](int t) {
+#pragma unroll
+        for (int b = 0; b < NB; b++) page[b] = page_of(p.c, e, list.position(min(t * KT + 16 * b + r, list.nk - 1)));
+    };
+    auto load = [&](int t) {
+        hole_n = 0;
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+            const int key = t * KT + 16 * b + r, off = list.position(key) & ((1 << p.c.shift) - 1);
+            const bool in = key < list.nk, hole = page[b] >= (uint32_t)p.c.pages;
+            hole_n |= (uint32_t)(__ballot(in & hole) & 0xffff) << (16 * b);
+            if (in & !hole) {
+                const char *ka = kh + page[b] * p.c.kp + off * p.c.kt, *va = vh + page[b] * p.c.vp + off * p.c.vt;
+#pragma unroll
+                for (int c = 0; c < KS; c++) {
+                    kn[b][c] = *(const u32x4*)(ka + 64 * c);
+                    vn[b][c] = *(const u32x4*)(va + 64 * c);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < KS; c++) kn[b][c] = vn[b][c] = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    int t = t_lo + wave;
+    if (t < t_hi) {
+        find(t);
+        load(t);
+        if (t + 4 < t_hi) find(t + 4);
+    }
+    for (; t < t_hi; t += 4) {
+        const int t0 = t * KT;
+        const uint32_t hole = hole_n;
+        f32x4 s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+            s[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < KS; c++) s[b] = mma<BF16>(kn[b][c], qf[c], s[b]);
+#pragma unroll
+            for (int c = 0; c < KS; c++) *(u32x4*)(vt + (16 * b + r) * VROW + 64 * c + 16 * g) = vn[b][c];
+        }
+        if (t + 4 < t_hi) {
+            load(t + 4);
+            if (t + 8 < t_hi) find(t + 8);
+        }
+        const bool open = ((t0 + KT <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + KT <= lead.hi))) & (hole == 0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int k = 16 * b + 4 * g + i;
+                const bool see = open | (mine.sees(t0 + k) & !((hole >> k) & 1));
+                saw |= see;
+                s[b][i] = see ? s[b][i] * p.scale_log2 : -INFINITY;
+                top = fmaxf(top, s[b][i]);
+            }
+        top = fmaxf(m, max_xor16_32(top));
+        const float base = top == -INFINITY ? 0.0f : top;   // nothing finite yet: every probability is 0
+        const float alpha = __builtin_amdgcn_exp2f(m - base);
+        m = top;
+        float pr[4 * NB], sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4 * NB; k++) {
+            pr[k] = __builtin_amdgcn_exp2f(s[k >> 2][k & 3] - base);
+            sum += pr[k];
+        }
+        l = l * alpha + sum;   // this lane's keys; the lanes of a query are summed at the end
+#pragma unroll
+        for (int b = 0; b < DB; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[b][i] *= alpha;
+        // (the wave's own region: its LDS operations complete in order)
+        __builtin_amdgcn_wave_barrier();
+        bool special = false;
+        if constexpr (BF16) {
+            const u32x4 pf = {pack2(pr[0], pr[1]), pack2(pr[2], pr[3]), pack2(pr[4], pr[5]), pack2(pr[6], pr[7])};
+#pragma unroll
+            for (int b = 0; b < DB; b++) {
+                const unsigned char* a = vt + (4 * g + (r >> 2)) * VROW + 32 * b + 8 * (r & 3);
+                u32x4 vf = read_tr(a, a + 16 * VROW);
+                if (!open) special |= clear_special<true>(vf);
+                o[b] = mma<true>(vf, pf, o[b]);
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < DB; b++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    uint32_t x = *(const uint32_t*)(vt + (4 * g + i) * VROW + 64 * b + 4 * r);
+                    if (!open) {
+                        u32x4 w = {x, 0, 0, 0};
+                        special |= clear_special<false>(w);
+                        x = w[0];
+                    }
+                    o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), pr[i], o[b], 0, 0, 0);
+                }
+        }
+        // values that are no numbers reach the rows that see them only
+        if (__builtin_expect(__any(special), 0)) {
+#pragma unroll 1
+            for (int k = 0; k < KT; k++) {
+                const int j = 4 * (k >> 4) + (k & 3);
+                float pk = pr[0];
+#pragma unroll
+                for (int x = 1; x < 4 * NB; x++) pk = j == x ? pr[x] : pk;
+                pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
+                if (!mine.sees(t0 + k) || ((hole >> k) & 1)) continue;
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float v = load1(vt + k * VROW, 16 * b + 4 * g + i, BF16);
+                        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[b][i] = fmaf(pk, v, o[b][i]);
+                    }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    l = sum_xor32(sum_xor16(l));
+    if (any_lane_of_row(saw) && m == -INFINITY) m = kSawNothingFinite;
+
+    __syncthreads();
+    float* mine_o = (float*)vt;                       // [16 queries][D], then m, l [16]
+#pragma unroll
+    for (int b = 0; b < DB; b++) *(f32x4*)(mine_o + r * D + 16 * b + 4 * g) = o[b];
+    if (g == 0) {
+        mine_o[16 * D + r] = m;
+        mine_o[16 * D + 16 + r] = l;
+    }
+    __syncthreads();
+    constexpr int CH = D / 4;                         // four dimensions a thread
+    for (int u = threadIdx.x; u < 16 * CH; u += 256) {
+        const int q = u / CH, d = 4 * (u % CH);
+        if (row0 + q > last) continue;
+        float mx = -INFINITY, sum = 0.0f;
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; w++) mx = fmaxf(mx, ((const float*)(smem + w * WAVE_LDS))[16 * D + q]);
+        const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            const float* src = (const float*)(smem + w * WAVE_LDS);
+            const float f = __builtin_amdgcn_exp2f(src[16 * D + q] - base);
+            sum += src[16 * D + 16 + q] * f;
+            const f32x4 y = *(const f32x4*)(src + q * D + d);
+#pragma unroll
+            for (int i = 0; i < 4; i++) x[i] += y[i] * f;
+        }
+        if (p.splits == 1) store_result(p, e, h, row0 + q, d, inverse(sum, mx), x);
+        else store_part(p, eh, row0 + q, split, d, x, mx, sum);
+    }
+}
+
+// Many rows: a block of four waves works on 64 QG rows, each wave on its own 16 QG.
+// Tiles of keys and values go from memory to LDS directly, through two buffers, the
+// next one on its way while this one is worked on (the pages two ahead); 16-byte
+// chunks are stored with their index XORed with bits of the row, so that the rows
+// of an operand read lie in different banks.  The running maximum is moved only
+// when a score passes it by more than 2^8 (a probability's rounding to bf16 is
+// relative, and 2^8 times more fits fp32 with room), so the output is rarely
+// rescaled; in bf16 the probabilities' sum is one more row of the second product.
+constexpr float kSlack = 8.0f;
+
+template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void attend_many(const PagedParams p)
+{
+    constexpr int ES = BF16 ? 2 : 4, NB = BF16 ? 4 : 2, KT = 16 * NB, KS = D * ES / 64, DB = D / 16, RB = 64 * QG;
+    constexpr int ROW = D * ES, CPR = ROW / 16, LOADS = KT * CPR / 256;   // bytes, chunks of a row; a thread's of a tile
+    constexpr int TILE = KT * ROW;
+    __shared__ __align__(16) unsigned char smem[4 * TILE];                // [buffer][keys, values]
+    __shared__ uint8_t holes[2][KT];
+    __shared__ int hole_any[2][4];
+    __device__ static const u32x4 zeros = {0, 0, 0, 0};
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int regions = p.c.batch * p.c.heads, split = blockIdx.x % p.splits;
+    const int eh = blockIdx.x / p.splits % regions, e = eh / p.c.heads, h = eh % p.c.heads;
+    const Span sp(p, e);
+    // (the last rows, which see the most keys, first)
+    const int blocks = (p.n * p.group + RB - 1) / RB;
+    const int rows = sp.len * p.group, row0 = RB * (blocks - 1 - (int)(blockIdx.x / p.splits / regions));
+    if (row0 >= rows) return;
+    const int last = min(row0 + RB - 1, rows - 1);
+    const KeyList list(p, sp, row0 / p.group, last / p.group);
+    const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
+    const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;
+
+    RowSpan mine[QG];
+    u32x4 qf[QG][KS];
+#pragma unroll
+    for (int u = 0; u < QG; u++) {
+        const int row = min(row0 + 16 * (QG * wave + u) + r, last), i = row / p.group;
+        mine[u] = list.row(p, sp, i);
+        const char* q = (const char*)p.q.p + p.q.at(e, i, h * p.group + row % p.group) * ES;
+#pragma unroll
+        for (int c = 0; c < KS; c++) qf[u][c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
+    }
+    const int tiles = (list.nk + KT - 1) / KT;
+    const int t_lo = (int)((int64_t)tiles * split / p.splits), t_hi = (int)((int64_t)tiles * (split + 1) / p.splits);
+
+    // which chunk of a row lies in place c of it (and the other way round)
+    auto swz_k = [](int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
+    auto swz_v = [](int row) { return !BF16 ? ((row >> 2) & 3) << 2 : D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; };
+    uint32_t page[LOADS];
+    auto find = [&](int t) {
+#pragma unroll
+        for (int c = 0; c < LOADS; c++)
+            page[c] = page_of(p.c, e, list.position(min(t * KT + tid / CPR + c * (256 / CPR), list.nk - 1)));
+    };
+    auto load = [&](int t) {
+        bool any = false;
+        unsigned char* to = smem + (t & 1) * 2 * TILE + wave * 1024;
+#pragma unroll
+        for (int c = 0; c < LOADS; c++) {
+            const int row = tid / CPR + c * (256 / CPR), key = t * KT + row, off = list.position(key) & ((1 << p.c.shift) - 1);
+            const bool in = key < list.nk, hole = page[c] >= (uint32_t)p.c.pages, on = in & !hole;
+            any |= in & hole;
+            if (tid % CPR == 0) holes[t & 1][row] = in & hole;
+            const char* ka = p.c.k + page[c] * p.c.kp + off * p.c.kt + h * p.c.kh + 16 * (tid % CPR ^ swz_k(row));
+            const char* va = p.c.v + page[c] * p.c.vp + off * p.c.vt + h * p.c.vh + 16 * (tid % CPR ^ swz_v(row));
+            __builtin_amdgcn_global_load_lds((const void*)(on ? ka : (const char*)&zeros),
+                                             (__attribute__((address_space(3))) void*)(to + c * 4096), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const void*)(on ? va : (const char*)&zeros),
+                                             (__attribute__((address_space(3))) void*)(to + TILE + c * 4096), 16, 0, 0);
+        }
+        hole_any[t & 1][wave] = __any(any);
+    };
+
+    f32x4 o[QG][DB], ls[QG];   // ls: the probabilities' sums (bf16: every row the whole sum; fp32: [0], this lane's keys)
+    float base[QG], limit[QG];   // of a row: what its scores are taken from (0 before any), and what moves it
+    bool saw[QG];
+#pragma unroll
+    for (int u = 0; u < QG; u++) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[u][b] = f32x4{0, 0, 0, 0};
+        ls[u] = f32x4{0, 0, 0, 0};
+        base[u] = 0.0f;
+        limit[u] = -INFINITY;
+        saw[u] = false;
+    }
+    const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+
+    const bool rows_left = row0 + 16 * QG * wave <= last;
+    if (t_lo < t_hi) {
+        find(t_lo);
+        load(t_lo);
+        if (t_lo + 1 < t_hi) find(t_lo + 1);
+    }
+    for (int t = t_lo; t < t_hi; t++) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this tile is in LDS
+        __syncthreads();                                   // for every wave, and the one before has been read
+        if (t + 1 < t_hi) {
+            load(t + 1);
+            if (t + 2 < t_hi) find(t + 2);
+        }
+        if (!rows_left) continue;
+        const unsigned char *kt = smem + (t & 1) * 2 * TILE, *vt = kt + TILE;
+        const int t0 = t * KT;
+        const bool any_hole = hole_any[t & 1][0] | hole_any[t & 1][1] | hole_any[t & 1][2] | hole_any[t & 1][3];
+        // (a scale that turns the scores' order around takes the masking path too)
+        const bool open = ((t0 + KT <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + KT <= lead.hi))) & !any_hole & (p.scale_log2 > 0.0f);
+
+        f32x4 s[QG][NB];
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+#pragma unroll
+            for (int u = 0; u < QG; u++) s[u][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < KS; c++) {
+                const u32x4 kf = *(const u32x4*)(kt + (16 * b + r) * ROW + 16 * ((4 * c + g) ^ swz_k(r)));
+#pragma unroll
+                for (int u = 0; u < QG; u++) s[u][b] = mma<BF16>(kf, qf[u][c], s[u][b]);
+            }
+        }
+        const float mul = open ? p.scale_log2 : 1.0f;
+#pragma unroll
+        for (int u = 0; u < QG; u++) {
+            // (masked scores are scaled before their mask: 0 times an infinity is NaN)
+            if (!open) {
+#pragma unroll
+                for (int b = 0; b < NB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int k = 16 * b + 4 * g + i;
+                        bool see = mine[u].sees(t0 + k);
+                        if (any_hole) see &= !holes[t & 1][k];
+                        saw[u] |= see;
+                        s[u][b][i] = see ? s[u][b][i] * p.scale_log2 : -INFINITY;
+                    }
+            } else {
+                saw[u] = true;
+            }
+            // (the lanes of a row compare their own keys; they meet only to move its base)
+            float top = s[u][0][0];
+#pragma unroll
+            for (int k = 1; k < 4 * NB; k++) top = fmaxf(top, s[u][k >> 2][k & 3]);
+            if (__any(top * mul > limit[u])) {
+                top = max_xor16_32(top) * mul;
+                const bool move = top > limit[u];
+                const float f = move ? __builtin_amdgcn_exp2f((limit[u] == -INFINITY ? -INFINITY : base[u]) - top) : 1.0f;
+                if (move) {
+                    limit[u] = top + kSlack;
+                    base[u] = top;
+                }
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[u][b][i] *= f;
+#pragma unroll
+                for (int i = 0; i < 4; i++) ls[u][i] *= f;
+            }
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) s[u][b][i] = __builtin_amdgcn_exp2f(fmaf(s[u][b][i], mul, -base[u]));
+        }
+        bool special = false;
+        if constexpr (BF16) {
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                u32x4 pf[QG];
+#pragma unroll
+                for (int u = 0; u < QG; u++) {
+                    const f32x4 a = s[u][2 * half], b = s[u][2 * half + 1];
+                    pf[u] = u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3])};
+                }
+                const int row = 32 * half + 4 * g + (r >> 2);
+#pragma unroll
+                for (int b = 0; b < DB; b++) {
+                    const unsigned char* a = vt + row * ROW + 16 * ((2 * b) ^ swz_v(row)) + 8 * (r & 3);
+                    u32x4 vf = read_tr(a, a + 16 * ROW);
+                    if (!open) special |= clear_special<true>(vf);
+#pragma unroll
+                    for (int u = 0; u < QG; u++) o[u][b] = mma<true>(vf, pf[u], o[u][b]);
+                }
+#pragma unroll
+                for (int u = 0; u < QG; u++) ls[u] = mma<true>(ones, pf[u], ls[u]);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < QG; u++)
+#pragma unroll
+                for (int k = 0; k < 4 * NB; k++) ls[u][0] += s[u][k >> 2][k & 3];
+#pragma unroll
+            for (int k = 0; k < NB; k++)
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int row = 16 * k + 4 * g + i;
+                        uint32_t x = *(const uint32_t*)(vt + row * ROW + 16 * ((4 * b) ^ swz_v(row)) + 4 * r);
+                        if (!open) {
+                            u32x4 w = {x, 0, 0, 0};
+                            special |= clear_special<false>(w);
+                            x = w[0];
+                        }
+#pragma unroll
+                        for (int u = 0; u < QG; u++)
+                            o[u][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), s[u][k][i], o[u][b], 0, 0, 0);
+                    }
+        }
+        // values that are no numbers reach the rows that see them only
+        if (__builtin_expect(__any(special), 0)) {
+#pragma unroll 1
+            for (int k = 0; k < KT; k++) {
+#pragma unroll
+                for (int u = 0; u < QG; u++) {
+                    const int j = 4 * (k >> 4) + (k & 3);
+                    float pk = s[u][0][0];
+#pragma unroll
+                    for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[u][x >> 2][x & 3] : pk;
+                    pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
+                    if (!mine[u].sees(t0 + k) || (any_hole && holes[t & 1][k])) continue;
+#pragma unroll
+                    for (int b = 0; b < DB; b++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const int d = 16 * b + 4 * g + i, ch = d * ES / 16;
+                            const float v = load1(vt + k * ROW + 16 * (ch ^ swz_v(k)), d % (16 / ES), BF16);
+                            if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[u][b][i] = fmaf(pk, v, o[u][b][i]);
+                        }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < QG; u++) {
+        const float l = BF16 ? ls[u][0] : sum_xor32(sum_xor16(ls[u][0]));
+        const float m = limit[u] != -INFINITY ? base[u] : any_lane_of_row(saw[u]) ? kSawNothingFinite : -INFINITY;
+        const int row = row0 + 16 * (QG * wave + u) + r;
+        if (row > last) continue;
+        const float inv = inverse(l, m);
+#pragma unroll
+        for (int b = 0; b < DB; b++) {
+            const int d = 16 * b + 4 * g;
+            if (p.splits > 1) store_part(p, eh, row, split, d, o[u][b], m, l);
+            else store_result(p, e, h, row, d, inv, o[u][b]);
+        }
+    }
+}
+
+// Joins the splits of a row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// NG groups of D / 4 threads share a row's splits, each with its own running
+// maximum, and meet in LDS.
+template <int D, int NG> __global__ __launch_bounds__(256) void join_kernel(const PagedParams p)
+{
+    constexpr int CH = D / 4, ROWS = 256 / (CH * NG);   // rows of a block
+    __shared__ __align__(16) float sm[NG > 1 ? ROWS * NG * (D + 2) : 1];
+    const int rows = p.n * p.group;
+    const int64_t regions = (int64_t)p.c.batch * p.c.heads;
+    const int ch = threadIdx.x % CH, grp = threadIdx.x / CH % NG, local = threadIdx.x / (CH * NG), d = 4 * ch;
+    const int64_t id = (int64_t)blockIdx.x * ROWS + local;
+    const bool in = id < regions * rows;
+    const int64_t at_id = in ? id : 0;
+    const int eh = (int)(at_id / rows), row = (int)(at_id % rows), e = eh / p.c.heads, h = eh % p.c.heads;
+    const Span sp(p, e);
+    const bool on = in && row < sp.len * p.group;
+    const int64_t parts = regions * rows * p.splits;
+    const float* ml = p.ws + parts * D + 2 * at_id * p.splits;
+    const float* po = p.ws + at_id * p.splits * D + d;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    if (on) {
+        for (int s = grp; s < p.splits; s += NG) {
+            const float ms = ml[2 * s], top = fmaxf(m, ms), base = top == -INFINITY ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - base), b = __builtin_amdgcn_exp2f(ms - base);
+            const f32x4 x = *(const f32x4*)(po + (int64_t)s * D);
+            m = top;
+            l = l * a + ml[2 * s + 1] * b;
+#pragma unroll
+            for (int k = 0; k < 4; k++) o[k] = o[k] * a + x[k] * b;
+        }
+    }
+    if constexpr (NG > 1) {
+        *(f32x4*)(sm + (local * NG + grp) * D + d) = o;
+        float* stat = sm + ROWS * NG * D + 2 * (local * NG + grp);
+        if (ch == 0) {
+            stat[0] = m;
+            stat[1] = l;
+        }
+        __syncthreads();
+        if (grp) return;
+        const float* all = sm + ROWS * NG * D + 2 * local * NG;
+        for (int g = 0; g < NG; g++) m = fmaxf(m, all[2 * g]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        l = 0.0f;
+        o = f32x4{0, 0, 0, 0};
+        for (int g = 0; g < NG; g++) {
+            const float f = __builtin_amdgcn_exp2f(all[2 * g] - base);
+            const f32x4 x = *(const f32x4*)(sm + (local * NG + g) * D + d);
+            l += all[2 * g + 1] * f;
+#pragma unroll
+            for (int k = 0; k < 4; k++) o[k] += x[k] * f;
+        }
+    }
+    if (on) store_result(p, e, h, row, d, inverse(l, m), o);
+}
+
+// ------------------------------------------------------------------ choice
+
+PagedPlan plan_paged(const Paged& c, int n, int group, int window, int sinks)
+{
+    const int64_t regions = (int64_t)c.batch * c.heads, rows = (int64_t)n * group;
+    const int64_t keys = window ? std::min((int64_t)c.limit, (int64_t)sinks + window + n) : c.limit;
+    PagedPlan pl{rows <= 16 ? 16 : c.bf16 && rows > 64 ? 128 : 64, 1, 0};
+    const int64_t blocks = regions * ((rows + pl.rows - 1) / pl.rows);
+    if (pl.rows == 16) pl.splits = (int)std::max((int64_t)1, std::min(std::min(1024 / blocks, keys / 256), (int64_t)64));
+    else pl.splits = (int)std::max((int64_t)1, std::min(std::min(512 / blocks, keys / 512), (int64_t)16));
+    if (pl.splits > 1) pl.ws_bytes = regions * rows * pl.splits * (c.D + 2) * 4;
+    return pl;
+}
+
+template <bool BF16, int D> hipError_t launch_attend_d(const PagedParams& p, const PagedPlan& plan, hipStream_t st)
+{
+    const int64_t rows = (int64_t)p.n * p.group, regions = (int64_t)p.c.batch * p.c.heads;
+    const int64_t blocks = p.splits * regions * ((rows + plan.rows - 1) / plan.rows);
+    hipError_t e = hipErrorInvalidValue;
+    if (plan.rows == 16) e = launch_with(attend_few<BF16, D>, blocks, 256, 0, st, p);
+    else if (plan.rows == 64) e = launch_with(attend_many<BF16, D, 1>, blocks, 256, 0, st, p);
+    else if constexpr (BF16) e = launch_with(attend_many<BF16, D, 2>, blocks, 256, 0, st, p);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t all = regions * rows;
+    constexpr int per = 256 / (D / 4);   // rows of a block, or groups of one row
+    if (p.splits <= 4 || all >= 2048) return launch_with(join_kernel<D, 1>, (all + per - 1) / per, 256, 0, st, p);
+    return launch_with(join_kernel<D, per>, all, 256, 0, st, p);
+}
+
+hipError_t launch_attend(const PagedParams& p, const PagedPlan& plan, hipStream_t st)
+{
+    if (p.c.D == 64) return p.c.bf16 ? launch_attend_d<true, 64>(p, plan, st) : launch_attend_d<false, 64>(p, plan, st);
+    return p.c.bf16 ? launch_attend_d<true, 128>(p, plan, st) : launch_attend_d<false, 128>(p, plan, st);
+}
+
+}  // namespace dcb

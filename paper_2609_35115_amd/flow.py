@@ -73,7 +73,32 @@ class DcQkNorm(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class DcCall(ctypes.Structure):
+    _fields_ = [("lens", _P), ("batch", ctypes.c_int32), ("n", ctypes.c_int32)]
+
+
+class DcRows(ctypes.Structure):
+    _fields_ = [("data", _P), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class DcNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("gain", _P), ("bias", _P)]
+
+
+class DcLinearLayer(ctypes.Structure):
+    _fields_ = [("weight", _P), ("bias", _P), ("stride", ctypes.c_int64), ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("glu", ctypes.c_int32)]
+
+
+class DcPaged(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("abi_version", "batch", "heads", "head_dim", "dtype", "page_size", "pages",
+                                                    "table_pages")] + [
+        ("table", _P), ("table_stride", ctypes.c_int64), ("k", _P), ("v", _P)] + [
+        (f"{x}_stride_{y}", ctypes.c_int64) for x in "kv" for y in ("page", "t", "h")]
+
+
 _CARRY, _SPAN, _NORM, _ROWS = (ctypes.POINTER(t) for t in (DcCarry4, DcSpan, DcQkNorm, DcHeadRows))
+_CALL, _TOKENS, _BLOCK_NORM, _LAYER, _PAGED = (ctypes.POINTER(t) for t in (DcCall, DcRows, DcNorm, DcLinearLayer, DcPaged))
 
 FLOW_SIGNATURES = {
     "dc_flow_blob_floats": ([ctypes.POINTER(DcFlowCfg)], ctypes.c_int64),
@@ -99,6 +124,15 @@ FLOW_SIGNATURES = {
                           _P, ctypes.c_int64, _P], ctypes.c_int),
     "dc_carry4_read": ([_CARRY, _SPAN, ctypes.c_int32, _ROWS, _ROWS, _P], ctypes.c_int),
     "dc_carry4_last_error": ([], ctypes.c_char_p),
+    "dc_norm_residual": ([_CALL, ctypes.c_int32, _TOKENS, ctypes.c_float, _TOKENS, _BLOCK_NORM, _TOKENS, _TOKENS, _BLOCK_NORM,
+                          _TOKENS, _TOKENS, _TOKENS, _P], ctypes.c_int),
+    "dc_linear_workspace": ([_LAYER, ctypes.c_int32, ctypes.c_int32], ctypes.c_int64),
+    "dc_linear": ([_CALL, _LAYER, _TOKENS, _TOKENS, _TOKENS, ctypes.c_float, _TOKENS, _P, ctypes.c_int64, _P], ctypes.c_int),
+    "dc_paged_append": ([_PAGED, _SPAN, _ROWS, _ROWS, _P], ctypes.c_int),
+    "dc_paged_workspace": ([_PAGED] + 4 * [ctypes.c_int32], ctypes.c_int64),
+    "dc_paged_attend": ([_PAGED, _SPAN, _ROWS, _ROWS, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, _P,
+                         ctypes.c_int64, _P], ctypes.c_int),
+    "dc_block_last_error": ([], ctypes.c_char_p),
 }
 
 _bound = False

@@ -1,0 +1,369 @@
+"""The norms and the matrix product of a block (GPU) against 64-bit references,
+at the sizes, strides and masks where they can go wrong.
+
+Tolerances.  U = 2^-24 is fp32's half step, h = finfo(type).eps / 2 a result's.
+A norm's sums add at most 32 values in a lane, six times across lanes and eight
+times across waves, so a mean or a mean square is off by at most 46 U of the
+sum of magnitudes, and K = 64 U covers it with the factors' few roundings.  A
+product of n_in terms is off by at most (n_in + 16) U of the terms' magnitudes
+in any order of the sum; where every term is a small whole number, sums are
+exact, and results equal the reference's rounding bit for bit."""
+from __future__ import annotations
+
+import math
+
+import pytest
+
+from tests.gpu_common import say
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+U = 2.0 ** -24
+K64 = 64 * U
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def rand(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def behind(x, lens, value):
+    """Sets the rows behind lens of x [b][n][w]."""
+    if lens is not None:
+        for b, m in enumerate(lens.tolist()):
+            x[b, m:] = value
+    return x
+
+
+def strided(x, lead, tail):
+    """x's values as a part of wider rows: `lead` elements into them."""
+    b, n, w = x.shape
+    y = torch.full((b, n, lead + w + tail), float("nan"), device="cuda", dtype=x.dtype)
+    y[..., lead:lead + w] = x
+    return y[..., lead:lead + w]
+
+
+# ------------------------------------------------------------------- norms
+
+def ref_norm(x, m, err):
+    """(norm of x, its absolute error) in 64 bits, x off by err."""
+    if m is None:
+        return x, err
+    a = x.abs()
+    if m.kind == "layer":
+        err = err + err.mean(-1, keepdim=True) + K64 * (a + a.mean(-1, keepdim=True))
+        x = x - x.mean(-1, keepdim=True)
+    f = 1 / (x.square().mean(-1, keepdim=True) + m.eps).sqrt()
+    rel = K64 + f * err.square().mean(-1, keepdim=True).sqrt()
+    y, err = x * f, err * f
+    err = err + y.abs() * rel
+    if m.gain is not None:
+        y, err = y * m.gain.double(), err * m.gain.double().abs()
+    err = err + 8 * U * y.abs()
+    if m.bias is not None:
+        y = y + m.bias.double()
+        err = err + 8 * U * m.bias.double().abs()
+    return y, err
+
+
+def wide(m, x):
+    """A modulation against [b][n][w]."""
+    m = m.double()
+    return m[:, None] if m.dim() == 2 and x.dim() == 3 else m
+
+
+def check_norm(x, h, lens, out=None, **k):
+    from paper_2609_35115_amd.block import norm_residual
+    x0, h0 = x.clone(), None if h is None else h.clone()
+    got = norm_residual(x, h, lens=lens, out=out, **k)
+    xs = k.get("x_scale", 1.0)
+    r = x0.double() * xs
+    err = U * r.abs()
+    if h is not None:
+        p, e = ref_norm(h0.double(), k.get("post"), torch.zeros_like(h0, dtype=torch.float64))
+        if k.get("gate") is not None:
+            g = wide(k["gate"], x)
+            p, e = p * g, e * g.abs() + 8 * U * (p * g).abs()
+        r = r + p
+        err = err + e + 4 * U * (r.abs() + p.abs())
+    want = [(r, err) if got[0] is not None else None, None]
+    if got[1] is not None:
+        y, e = ref_norm(r, k.get("pre"), err)
+        if k.get("scale") is not None:
+            s = 1 + wide(k["scale"], x)
+            e, y = e * s.abs() + 8 * U * (y * s).abs() + 8 * U * y.abs(), y * s
+        if k.get("shift") is not None:
+            e, y = e + 4 * U * (wide(k["shift"], x).abs() + y.abs()), y + wide(k["shift"], x)
+        want[1] = (y, e + 4 * U * y.abs())
+    rows = torch.ones(x.shape[:2], dtype=torch.bool, device="cuda")
+    if lens is not None:
+        rows = torch.arange(x.shape[1], device="cuda") < lens[:, None]
+    for name, o, w in zip("ry", got, want):
+        if o is None:
+            continue
+        v, e = (t[rows] for t in w)
+        off = (o[rows].double() - v).abs() - (e + half(o.dtype) * (v.abs() + e))
+        assert bool((off <= 0).all()), f"{name}: {float(off.max())} past its tolerance"
+    return got
+
+
+WIDTHS = [1, 7, 8, 64, 200, 512, 520, 1001, 1024, 1025, 2048, 2571, 4099, 8192, 16384]
+
+
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("types", ["bb", "fb", "bf", "ff"])
+def test_norm_residual(width, types):
+    from paper_2609_35115_amd.block import Norm
+    xt, ht = (BF16 if c == "b" else F32 for c in types)
+    g = gen(width)
+    B, n = 3, 5
+    x, h = 3 * rand(g, B, n, width, dtype=xt) + 1, rand(g, B, n, width, dtype=ht) + 0.5
+    x = x.to(xt)
+    vec = lambda: 1 + 0.3 * rand(g, width)   # noqa: E731
+    lens = torch.tensor([5, 0, 2], device="cuda", dtype=torch.int32)
+    say(f"norm {width} {types}")
+    check_norm(x, h, None, post=Norm("rms", vec()), pre=Norm("rms", vec()), x_scale=0.7)
+    check_norm(x, h, lens, post=Norm("layer", vec(), vec()), gate=vec(), pre=Norm("layer", vec(), vec(), eps=1e-3), scale=vec(), shift=vec())
+    check_norm(x, h, lens, gate=rand(g, B, width), pre=Norm("layer"), scale=rand(g, B, width, dtype=BF16), shift=rand(g, B, n, width))
+    check_norm(x, h, None, post=Norm("rms", None, vec()), gate=rand(g, B, n, width), scale=rand(g, 1, n, width), shift=rand(g, B, 1, width))
+    assert check_norm(x, h, None, post=Norm("layer", vec()))[1] is None
+    assert check_norm(x, None, lens, pre=Norm("rms", vec()), x_scale=2.0)[0] is None
+
+
+def test_norm_rows_in_place_strided_and_behind():
+    from paper_2609_35115_amd.block import Norm
+    g = gen(5)
+    lens = torch.tensor([4, 1, 0, 6], device="cuda", dtype=torch.int32)
+    for width, lead, dt in ((257, 3, BF16), (512, 8, BF16), (100, 1, F32)):
+        x, h = rand(g, 4, 6, width, dtype=dt), rand(g, 4, 6, width, dtype=dt)
+        want = check_norm(x, h, lens, post=Norm("rms"), pre=Norm("layer"))
+        # rows behind lens are neither read nor written
+        xs, hs = (strided(behind(t.clone(), lens, float("nan")), lead, 2) for t in (x, h))
+        out = tuple(strided(torch.full_like(t, 7.0), lead, 5) for t in (x, h))
+        check_norm(xs, hs, lens, out=out, post=Norm("rms"), pre=Norm("layer"))
+        for o, w in zip(out, want):
+            assert torch.equal(o, behind(w.clone(), lens, 7.0))
+        # in place, rows of other entries' order too
+        xs, hs = x.clone(), h.clone()
+        check_norm(xs, hs, lens, out=(xs, hs), post=Norm("rms"), pre=Norm("layer"))
+        rows = torch.arange(6, device="cuda") < lens[:, None]
+        assert torch.equal(xs[rows], want[0][rows]) and torch.equal(hs[rows], want[1][rows])
+        assert torch.equal(xs[~rows], x[~rows]) and torch.equal(hs[~rows], h[~rows])
+        check_norm(x.transpose(0, 1), h.transpose(0, 1), None, post=Norm("rms"), pre=Norm("layer"))
+
+
+def test_norm_many_rows_walk():
+    """More rows than blocks: walks that cross entries, some without tokens."""
+    from paper_2609_35115_amd.block import Norm
+    g = gen(6)
+    B, n, width = 700, 41, 24
+    lens = torch.randint(0, n + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    lens[::5] = 0
+    x, h = rand(g, B, n, width), rand(g, B, n, width, dtype=BF16)
+    check_norm(x, h, lens, post=Norm("rms"), gate=rand(g, B, width), pre=Norm("layer"), scale=rand(g, B, width), shift=rand(g, B, width))
+    x, h = rand(g, 9, 1100, 1100), rand(g, 9, 1100, 1100, dtype=BF16)
+    lens = torch.tensor([0, 1100, 3, 0, 0, 700, 1, 1099, 0], device="cuda", dtype=torch.int32)
+    check_norm(x, h, lens, gate=rand(g, 9, 1100), pre=Norm("layer"))
+
+
+def test_norm_special_values():
+    from paper_2609_35115_amd.block import Norm, norm_residual
+    x = torch.zeros(1, 4, 64, device="cuda")
+    x[0, 1, 3], x[0, 2, 5] = float("nan"), 1e19
+    r, y = norm_residual(x, torch.zeros_like(x), pre=Norm("rms"))
+    assert torch.equal(y[0, 0], torch.zeros(64, device="cuda")) and bool(y[0, 1].isnan().all())
+    assert torch.equal(r.isnan(), x.isnan()) and bool((y[0, 3] == 0).all())
+
+
+# ------------------------------------------------------------------ linear
+
+ACTS = ["none", "gelu", "silu", "none_glu", "gelu_glu", "silu_glu"]
+
+
+def ref_act(v, act):
+    """(activation, a bound on its slope)."""
+    if act.startswith("gelu"):
+        return 0.5 * v * (1 + torch.tanh(math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3))), 1.13
+    if act.startswith("silu"):
+        return v * torch.sigmoid(v), 1.1
+    return v, 1.0
+
+
+def check_linear(x, w, bias=None, act="none", gate=None, residual=None, residual_scale=1.0, lens=None, out=None, out_dtype=None, exact=False):
+    from paper_2609_35115_amd.block import linear
+    res0 = None if residual is None else residual.clone()
+    got = linear(x, w, bias, act=act, gate=gate, residual=residual, residual_scale=residual_scale, lens=lens, out=out, out_dtype=out_dtype)
+    n_in = x.shape[-1]
+    z = x.double() @ w.double().t()
+    e = (n_in + 16) * U * (x.double().abs() @ w.double().abs().t())
+    if bias is not None:
+        z, e = z + bias.double(), e + 2 * U * bias.double().abs()
+    a, b = z.chunk(2, -1) if act.endswith("glu") else (z, None)
+    ea, eb = e.chunk(2, -1) if act.endswith("glu") else (e, None)
+    v, slope = ref_act(a, act)
+    # the activation itself: an exponential whose argument (up to 1.6 a + 0.1 a^3 in size) is rounded, and a division
+    ev = ea * slope + (8 + 4 * a.abs() + a.abs() ** 3 * 0.3 * act.startswith("gelu")) * U * v.abs() * (act.split("_")[0] != "none")
+    if act.split("_")[0] != "none" and got.dtype == BF16:
+        ev = ev + 4 * U * v.abs()
+    if b is not None:
+        ev = ev * b.abs() + eb * (v.abs() + ev) + U * (v * b).abs()
+        v = v * b
+    if gate is not None:
+        g = wide(gate, x)
+        ev, v = ev * g.abs() + U * (v * g).abs(), v * g
+    if residual is not None:
+        v = v + residual_scale * res0.double()
+        ev = ev + 2 * U * (v.abs() + abs(residual_scale) * res0.double().abs())
+    rows = torch.ones(x.shape[:2], dtype=torch.bool, device="cuda")
+    if lens is not None:
+        rows = torch.arange(x.shape[1], device="cuda") < lens[:, None]
+    if exact:
+        assert torch.equal(got[rows], v[rows].to(got.dtype))
+    else:
+        off = (got[rows].double() - v[rows]).abs() - (ev[rows] + half(got.dtype) * (v[rows].abs() + ev[rows]))
+        assert bool((off <= 0).all()), f"{float(off.max())} past its tolerance"
+    return got
+
+
+def whole(g, *shape, most=3, dtype=F32):
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda").to(dtype)
+
+
+ROWS = [(1, 1), (1, 5), (4, 4), (1, 17), (3, 11), (1, 64), (5, 13), (2, 65), (3, 100)]
+SIZES = [(1, 1), (7, 3), (8, 16), (31, 20), (64, 64), (72, 65), (100, 129), (513, 40), (1024, 260)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("K,N", SIZES)
+def test_linear_whole_numbers(K, N, dtype):
+    """Every size at every number of rows, exact."""
+    g = gen(K)
+    say(f"linear {K} -> {N} {dtype}")
+    for B, n in ROWS:
+        x, w = whole(g, B, n, K, dtype=dtype), whole(g, N, K, dtype=dtype)
+        check_linear(x, w, exact=True, out_dtype=F32)
+        lens = torch.randint(0, n + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+        check_linear(x, w, whole(g, N), gate=whole(g, B, N), residual=whole(g, B, n, N, dtype=dtype), residual_scale=2.0, lens=lens, exact=True)
+        check_linear(x, whole(g, 2 * N, K, dtype=dtype), whole(g, 2 * N, most=1), act="none_glu", gate=whole(g, N), lens=lens, exact=True, out_dtype=F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B,n,K,N", [(1, 3100, 72, 3900), (2, 1560, 200, 3841), (1, 3100, 75, 3900), (1, 700, 64, 2000), (1, 200, 4096, 130), (1, 70, 1030, 70),
+                                     (1, 8, 4096, 16), (3, 12, 2050, 100), (1, 50, 8192, 48)])
+def test_linear_tiles_and_splits(B, n, K, N, dtype):
+    """Each tile of rows, rows not of whole chunks, and K split over blocks."""
+    g = gen(n)
+    say(f"linear {B} x {n}: {K} -> {N} {dtype}")
+    x, w = whole(g, B, n, K, dtype=dtype), whole(g, N, K, dtype=dtype)
+    check_linear(x, w, whole(g, N), residual=whole(g, B, n, N), exact=True, out_dtype=F32)
+    lens = torch.full((B,), n // 3, device="cuda", dtype=torch.int32)
+    check_linear(x, whole(g, 2 * N, K, dtype=dtype, most=1), act="none_glu", lens=lens, exact=True, out_dtype=F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("out", [BF16, F32], ids=["to_bf16", "to_f32"])
+def test_linear_epilogue(act, dtype, out):
+    g = gen(3)
+    for B, n, K, N in ((2, 3, 96, 50), (1, 200, 130, 70), (3, 40, 1024, 96)):
+        R = 2 * N if act.endswith("glu") else N
+        x, w = rand(g, B, n, K, dtype=dtype), (2 * rand(g, R, K) * K ** -0.5).to(dtype)
+        check_linear(x, w, rand(g, R), act=act, out_dtype=out)
+        check_linear(x, w, act=act, gate=rand(g, B, n, N, dtype=BF16), residual=rand(g, B, n, N), out_dtype=out)
+        check_linear(x, w, act=act, gate=rand(g, N), residual=rand(g, B, n, N, dtype=BF16), residual_scale=0.3, out_dtype=out)
+
+
+def test_linear_rows_in_place_strided_and_behind():
+    g = gen(9)
+    lens = torch.tensor([4, 0, 9], device="cuda", dtype=torch.int32)
+    for dtype, K, N, lead in ((BF16, 64, 33, 8), (BF16, 65, 40, 1), (F32, 100, 64, 4), (F32, 36, 20, 1)):
+        for n in (9, 90):
+            x, w = whole(g, 3, n, K, dtype=dtype), whole(g, N, K, dtype=dtype)
+            r = whole(g, 3, n, N, dtype=dtype)
+            want = check_linear(x, w, residual=r, lens=lens, exact=True)
+            # rows behind lens are neither read nor written; rows and weights inside wider ones
+            xs, rs = (strided(behind(t.clone(), lens, float("nan")), lead, 7) for t in (x, r))
+            ws = strided(w[None], lead, 3)[0]
+            out = strided(torch.full_like(r, 7.0), lead, 1)
+            check_linear(xs, ws, residual=rs, lens=lens, out=out, exact=True)
+            assert torch.equal(out, behind(want.clone(), lens, 7.0))
+            assert not bool(want.isnan().any())
+            rs = r.clone()
+            check_linear(x, w, residual=rs, lens=lens, out=rs, exact=True)
+            rows = torch.arange(n, device="cuda") < lens[:, None]
+            assert torch.equal(rs[~rows], r[~rows])
+            check_linear(x.transpose(0, 1), w, exact=True)
+
+
+def test_linear_special_values_stay_in_their_rows():
+    """An infinity or NaN of one row reaches no other row; one of the weight only its column."""
+    g = gen(4)
+    for n in (5, 100):
+        for dtype in (BF16, F32):
+            x, w = whole(g, 1, n, 70, dtype=dtype), whole(g, 30, 70, dtype=dtype)
+            want = check_linear(x, w, exact=True)
+            x[0, 2, 69], w[7, 0] = float("nan"), float("inf")
+            x[0, :, 0] = 1
+            from paper_2609_35115_amd.block import linear
+            got = linear(x, w)
+            bad = torch.zeros_like(got, dtype=torch.bool)
+            bad[0, 2], bad[0, :, 7] = True, True
+            assert not bool(got[bad].isfinite().any()) and bool(got[~bad].isfinite().all())
+            assert got.shape == want.shape
+
+
+def test_block_calls_are_captured_and_replayed():
+    from paper_2609_35115_amd.block import Norm, linear, norm_residual
+    g = gen(11)
+    lens = torch.tensor([3, 1], device="cuda", dtype=torch.int32)
+    x, h, w = rand(g, 2, 3, 256), rand(g, 2, 3, 256, dtype=BF16), rand(g, 40, 4096, dtype=BF16)
+    big = rand(g, 2, 3, 4096, dtype=BF16)
+    pre = Norm("layer")
+    r, y, o = torch.zeros_like(x), torch.zeros_like(h), torch.zeros(2, 3, 40, device="cuda", dtype=BF16)
+
+    def calls():
+        norm_residual(x, h, pre=pre, lens=lens, out=(r, y))
+        linear(big, w, lens=lens, out=o)    # K split over blocks
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for turn in range(3):
+        x.copy_(rand(g, 2, 3, 256))
+        big.copy_(rand(g, 2, 3, 4096, dtype=BF16))
+        lens.copy_(torch.tensor([turn, 3 - turn], dtype=torch.int32))
+        for t in (r, y, o):
+            t.zero_()
+        graph.replay()
+        got = [t.clone() for t in (r, y, o)]
+        for t in (r, y, o):
+            t.zero_()
+        calls()
+        for a, b in zip(got, (r, y, o)):
+            assert torch.equal(a, b), turn
+
+
+def test_the_same_call_gives_the_same_bits():
+    """Whatever the other rows hold."""
+    from paper_2609_35115_amd.block import linear
+    g = gen(12)
+    for n, K, N in ((6, 4096, 40), (150, 2048, 130), (40, 1024, 512)):
+        x, w = rand(g, 2, n, K, dtype=BF16), rand(g, N, K, dtype=BF16)
+        a = linear(x, w, out_dtype=F32)
+        y = x.clone()
+        y[1] = float("nan")
+        b = linear(y, w, out_dtype=F32)
+        assert torch.equal(a[0], b[0]) and torch.equal(a, linear(x, w, out_dtype=F32))
