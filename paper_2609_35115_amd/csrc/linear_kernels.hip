@@ -66,51 +66,109 @@ struct Place {
     }
 };
 
-// Columns n .. n + 3 of a row, from the sums a (and b, the factor's, with glu).
-__device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at, int n, f32x4 a, f32x4 b)
+// Columns n .. n + 7 of a row, from the sums a (and b, the factor's, with glu),
+// biases ba, bb.
+struct Eight {
+    float v[8];
+};
+__device__ __forceinline__ Eight load8(const void* p, int64_t at, int bf16)
+{
+    const f32x4 a = load4(p, at, bf16), b = load4(p, at + 4, bf16);
+    return Eight{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+__device__ __forceinline__ Eight load_bias(const LinearParams& p, int n, int part)
+{
+    Eight x{};
+    if (p.bias && n + 8 <= p.N) {
+        x = load8(p.bias, (int64_t)part * p.N + n, 0);
+    } else if (p.bias) {
+#pragma unroll
+        for (int k = 0; k < 7; k++)
+            if (n + k < p.N) x.v[k] = p.bias[(int64_t)part * p.N + n + k];
+    }
+    return x;
+}
+__device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at, int n, Eight a, Eight b, const Eight& ba, const Eight& bb)
 {
     if (!at.on || n >= p.N) return;
     const int64_t o = at.e * p.out.sb + at.i * p.out.st + n;
     const int64_t g = at.e * p.gate.sb + at.i * p.gate.st + n, r = at.e * p.res.sb + at.i * p.res.st + n;
-    if (n + 4 <= p.N) {
-        if (p.bias) {
-            a += load4(p.bias, n, 0);
-            if (p.glu) b += load4(p.bias, p.N + n, 0);
-        }
-        if (p.act) {
+    const bool full = n + 8 <= p.N;
 #pragma unroll
-            for (int k = 0; k < 4; k++) a[k] = p.out.bf16 ? activate<false>(a[k], p.act) : activate<true>(a[k], p.act);
+    for (int k = 0; k < 8; k++) a.v[k] += ba.v[k];
+    if (p.act) {
+        if (p.out.bf16) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) a.v[k] = activate<false>(a.v[k], p.act);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++) a.v[k] = activate<true>(a.v[k], p.act);
         }
-        if (p.glu) a *= b;
-        if (p.gate.p) a *= load4(p.gate.p, g, p.gate.bf16);
+    }
+    if (p.glu) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) a.v[k] *= b.v[k] + bb.v[k];
+    }
+    if (full) {
+        if (p.gate.p) {
+            const Eight x = load8(p.gate.p, g, p.gate.bf16);
+#pragma unroll
+            for (int k = 0; k < 8; k++) a.v[k] *= x.v[k];
+        }
         if (p.res.p) {
-            const f32x4 x = load4(p.res.p, r, p.res.bf16);
+            const Eight x = load8(p.res.p, r, p.res.bf16);
 #pragma unroll
-            for (int k = 0; k < 4; k++) a[k] = fmaf(p.res_scale, x[k], a[k]);
+            for (int k = 0; k < 8; k++) a.v[k] = fmaf(p.res_scale, x.v[k], a.v[k]);
         }
-        store4(p.out.p, o, p.out.bf16, a);
+        if (p.out.bf16) store8<true>(p.out.p, o, a.v);
+        else store8<false>(p.out.p, o, a.v);
         return;
     }
-    for (int k = 0; k < 4 && n + k < p.N; k++) {
-        float v = a[k], w = b[k];
-        if (p.bias) {
-            v += p.bias[n + k];
-            if (p.glu) w += p.bias[p.N + n + k];
-        }
-        v = p.out.bf16 ? activate<false>(v, p.act) : activate<true>(v, p.act);
-        if (p.glu) v *= w;
+#pragma unroll
+    for (int k = 0; k < 7; k++) {
+        if (n + k >= p.N) break;
+        float v = a.v[k];
         if (p.gate.p) v *= load1(p.gate.p, g + k, p.gate.bf16);
         if (p.res.p) v = fmaf(p.res_scale, load1(p.res.p, r + k, p.res.bf16), v);
         store1(p.out.p, o + k, p.out.bf16, v);
     }
 }
 
-// Partial sums of a split: [split][M][columns], a row's columns padded to four.
-__host__ __device__ inline int64_t part_row(int N, int glu) { return (int64_t)((N + 3) / 4 * 4) * (glu ? 2 : 1); }
-__device__ __forceinline__ void store_part(const LinearParams& p, int split, int m, int n, bool factor, f32x4 v)
+// Partial sums of a split: [split][M][columns], a row's columns padded to eight.
+__host__ __device__ inline int part_half(int N) { return (N + 7) / 8 * 8; }
+__host__ __device__ inline int64_t part_row(int N, int glu) { return (int64_t)part_half(N) * (glu ? 2 : 1); }
+
+// What a wave does with its `rows` rows of sums in LDS (`pitch` floats apart, with
+// glu the factors COLS / 2 floats behind): the epilogue, or a split's partial sums,
+// eight columns a lane and whole rows side by side.
+template <int COLS> __device__ __forceinline__ void finish(const LinearParams& p, const float* sums, int rows, int pitch, int m0, int n0, int split)
 {
-    if (m >= p.M || n >= p.N) return;
-    *(f32x4*)(p.ws + ((int64_t)split * p.M + m) * part_row(p.N, p.glu) + (factor ? (p.N + 3) / 4 * 4 : 0) + n) = v;
+    const int lane = threadIdx.x & 63;
+    const int per = p.glu ? COLS / 16 : COLS / 8;             // lanes of a row
+    const int q = lane & (per - 1), n = n0 + 8 * q;
+    const Eight ba = load_bias(p, n, 0), bb = p.glu ? load_bias(p, n, 1) : Eight{};
+#pragma unroll 1
+    for (int r = lane / per; r < rows; r += 64 / per) {
+        const float* s = sums + r * pitch + 8 * q;
+        auto eight = [](const float* s) {
+            const f32x4 x = *(const f32x4*)s, y = *(const f32x4*)(s + 4);
+            return Eight{{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}};
+        };
+        const Eight a = eight(s), b = eight(s + (p.glu ? COLS / 2 : 0));
+        if (p.splits > 1) {
+            if (m0 + r >= p.M || n >= p.N) continue;
+            float* to = p.ws + ((int64_t)split * p.M + m0 + r) * part_row(p.N, p.glu) + n;
+            *(f32x4*)to = f32x4{a.v[0], a.v[1], a.v[2], a.v[3]};
+            *(f32x4*)(to + 4) = f32x4{a.v[4], a.v[5], a.v[6], a.v[7]};
+            if (p.glu) {
+                to += part_half(p.N);
+                *(f32x4*)to = f32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
+                *(f32x4*)(to + 4) = f32x4{b.v[4], b.v[5], b.v[6], b.v[7]};
+            }
+        } else {
+            epilogue(p, Place(p, m0 + r), n, a, b, ba, bb);
+        }
+    }
 }
 
 // ----------------------------------------------------------- tiles of rows
@@ -129,8 +187,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
     constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, CE = chunk_elems<BF16>(), ES = 16 / CE;
     constexpr int KT = kChunks * CE, ROWS = BM + BN, LOADS = ROWS * kChunks / T;
     constexpr int BUF = ROWS * kChunks * 16;
+    constexpr int COLS = BN / WN, PITCH = COLS + 4, SR = BM / WM < 64 ? BM / WM : 64;   // the sums' way through LDS
+    constexpr int OUT = WM * WN * SR * PITCH * 4, LDS = 2 * BUF > OUT ? 2 * BUF : OUT;
     static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0);
-    __shared__ __align__(16) unsigned char smem[2 * BUF];
+    __shared__ __align__(16) unsigned char smem[LDS];
     __shared__ int some;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -235,29 +295,19 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
         __syncthreads();
     }
 
+    // the sums go through LDS, up to 64 rows of a wave at a time, so that a row's
+    // columns are stored side by side
+    float* mine = (float*)smem + wave * SR * PITCH;
 #pragma unroll
-    for (int i = 0; i < MI; i++) {
-        const int m = m0 + wm * (BM / WM) + 16 * i + l16;
-        const Place at(p, m);
-        if (p.glu) {
+    for (int c = 0; c < MI; c += SR / 16) {
 #pragma unroll
-            for (int j = 0; j < NI / 2; j++) {
-                const int n = n0 + wn * (BN / WN / 2) + 16 * j + 4 * g;
-                if (p.splits > 1) {
-                    store_part(p, split, m, n, false, acc[i][j]);
-                    store_part(p, split, m, n, true, acc[i][j + NI / 2]);
-                } else {
-                    epilogue(p, at, n, acc[i][j], acc[i][j + NI / 2]);
-                }
-            }
-        } else {
+        for (int i = 0; i < SR / 16; i++)
 #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                const int n = n0 + wn * (BN / WN) + 16 * j + 4 * g;
-                if (p.splits > 1) store_part(p, split, m, n, false, acc[i][j]);
-                else epilogue(p, at, n, acc[i][j], acc[i][j]);
-            }
-        }
+            for (int j = 0; j < NI; j++) *(f32x4*)(mine + (16 * i + l16) * PITCH + 16 * j + 4 * g) = acc[c + i][j];
+        // (the wave's own region: its LDS operations complete in order)
+        __builtin_amdgcn_wave_barrier();
+        finish<COLS>(p, mine, SR, PITCH, m0 + wm * (BM / WM) + 16 * c, n0 + wn * (p.glu ? COLS / 2 : COLS), split);
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -272,7 +322,7 @@ template <bool BF16, int MB, int NT, bool WIDE>
 __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 {
     constexpr int CE = chunk_elems<BF16>(), ES = 16 / CE, U = 4, KG = 4 * CE;   // elements of a group of chunks
-    __shared__ __align__(16) float sums[4][MB * NT * 256];
+    __shared__ __align__(16) float sums[4][16 * MB * (16 * NT + 4)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
     const int BC = p.glu ? 16 : 16 * NT;
@@ -318,55 +368,45 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 #pragma unroll
                 for (int j = 0; j < NT; j++) acc[i][j] = mma<BF16>(w[u][j], x[u][i], acc[i][j]);
     }
+    constexpr int COLS = 16 * NT, PITCH = COLS + 4;
 #pragma unroll
     for (int i = 0; i < MB; i++)
 #pragma unroll
-        for (int j = 0; j < NT; j++) *(f32x4*)(sums[wave] + ((i * NT + j) * 64 + lane) * 4) = acc[i][j];
+        for (int j = 0; j < NT; j++) *(f32x4*)(sums[wave] + (16 * i + l16) * PITCH + 16 * j + 4 * g) = acc[i][j];
     __syncthreads();
-    // (wave w takes every fourth sixteen-by-sixteen group)
-    auto sum = [&](int ij) {
-        f32x4 v = *(const f32x4*)(sums[0] + (ij * 64 + lane) * 4);
+    for (int u = tid; u < 16 * MB * COLS / 4; u += 256) {
+        const int at = u / (COLS / 4) * PITCH + 4 * (u % (COLS / 4));
+        f32x4 v = *(const f32x4*)(sums[0] + at);
 #pragma unroll
-        for (int w = 1; w < 4; w++) v += *(const f32x4*)(sums[w] + (ij * 64 + lane) * 4);
-        return v;
-    };
-    if (p.glu) {
-        for (int i = wave; i < MB; i += 4) {
-            const int m = 16 * i + l16, n = n0 + 4 * g;
-            const f32x4 a = sum(i * NT), b = sum(i * NT + NT - 1);
-            if (p.splits > 1) {
-                store_part(p, split, m, n, false, a);
-                store_part(p, split, m, n, true, b);
-            } else {
-                epilogue(p, Place(p, m), n, a, b);
-            }
-        }
-    } else {
-        for (int ij = wave; ij < MB * NT; ij += 4) {
-            const int m = 16 * (ij / NT) + l16, n = n0 + 16 * (ij % NT) + 4 * g;
-            const f32x4 a = sum(ij);
-            if (p.splits > 1) store_part(p, split, m, n, false, a);
-            else epilogue(p, Place(p, m), n, a, a);
-        }
+        for (int w = 1; w < 4; w++) v += *(const f32x4*)(sums[w] + at);
+        *(f32x4*)(sums[0] + at) = v;
     }
+    __syncthreads();
+    if (wave < MB) finish<COLS>(p, sums[0] + 16 * wave * PITCH, 16, PITCH, 16 * wave, n0, split);
 }
 
-// The splits' partial sums and the epilogue, four columns a thread.
+// The splits' partial sums and the epilogue, eight columns a thread.
 __global__ __launch_bounds__(256) void join_kernel(const LinearParams p)
 {
-    const int64_t quads = (p.N + 3) / 4, u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (u >= quads * p.M) return;
-    const int m = (int)(u / quads), n = 4 * (int)(u % quads);
+    const int64_t eights = part_half(p.N) / 8, u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (u >= eights * p.M) return;
+    const int m = (int)(u / eights), n = 8 * (int)(u % eights);
     const Place at(p, m);
     if (!at.on) return;
     const int64_t row = part_row(p.N, p.glu);
     const float* s = p.ws + m * row + n;
-    f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    Eight a{}, b{};
     for (int k = 0; k < p.splits; k++, s += (int64_t)p.M * row) {
-        a += *(const f32x4*)s;
-        if (p.glu) b += *(const f32x4*)(s + (p.N + 3) / 4 * 4);
+        const Eight x = load8(s, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 8; j++) a.v[j] += x.v[j];
+        if (p.glu) {
+            const Eight y = load8(s, part_half(p.N), 0);
+#pragma unroll
+            for (int j = 0; j < 8; j++) b.v[j] += y.v[j];
+        }
     }
-    epilogue(p, at, n, a, b);
+    epilogue(p, at, n, a, b, load_bias(p, n, 0), p.glu ? load_bias(p, n, 1) : Eight{});
 }
 
 // ------------------------------------------------------------------ choice
@@ -415,7 +455,7 @@ template <bool BF16> hipError_t launch_linear_t(const LinearParams& p, const Lin
                         : launch_with(tile_kernel<BF16, 128, 128, 2, 2, false>, blocks(128), 256, 0, st, p);
     }
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch_with(join_kernel, ((int64_t)((p.N + 3) / 4) * p.M + 255) / 256, 256, 0, st, p);
+    return launch_with(join_kernel, ((int64_t)(part_half(p.N) / 8) * p.M + 255) / 256, 256, 0, st, p);
 }
 
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
