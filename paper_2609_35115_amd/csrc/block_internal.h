@@ -194,6 +194,20 @@ template <bool BF16> __device__ __forceinline__ void store8(void* p, int64_t at,
     }
 }
 
+// 16 bytes a lane from memory to LDS, lane i's to `lds` + 16 i (an LDS byte address,
+// uniform).  As an instruction of its own: the compiler waits for a load of the
+// builtin before any LDS read, since the two might meet.  The caller waits
+// (dma_wait) before the barrier behind which the bytes are read.
+__device__ __forceinline__ void dma16(const void* from, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "m0");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
 template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v)
 {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);

@@ -242,14 +242,13 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
 
     u32x4 stage[WIDE ? 1 : LOADS];
     __device__ static const u32x4 zeros = {0, 0, 0, 0};
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * 1024);
     auto fetch = [&](int s) {
         const int k = s * KT + kc;
         if constexpr (WIDE) {
-            unsigned char* to = smem + (s & 1) * BUF + wave * 1024;
 #pragma unroll
             for (int c = 0; c < LOADS; c++)
-                __builtin_amdgcn_global_load_lds((const void*)(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros),
-                                                 (__attribute__((address_space(3))) void*)(to + c * (T * 16)), 16, 0, 0);
+                dma16(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros, lds0 + (s & 1) * BUF + c * (T * 16));
         } else {
 #pragma unroll
             for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<BF16>(row[c], k, p.K);
@@ -268,32 +267,58 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
 #pragma unroll
         for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    const int xr = (wm * (BM / WM) + l16) * 128, wr = (BM + wn * (BN / WN) + l16) * 128;
+    // operands of a half step (four chunks)
+    struct Half {
+        u32x4 x[MI], w[NI];
+    } even, odd;
+    const unsigned char *xl = smem + (wm * (BM / WM) + l16) * 128, *wl = smem + (BM + wn * (BN / WN) + l16) * 128;
+    auto read = [&](Half& o, int s, int h) {
+        const int ch = (s & 1) * BUF + ((4 * h + g) ^ (l16 & 7)) * 16;
+#pragma unroll
+        for (int j = 0; j < NI; j++) o.w[j] = *(const u32x4*)(wl + j * 2048 + ch);
+#pragma unroll
+        for (int i = 0; i < MI; i++) o.x[i] = *(const u32x4*)(xl + i * 2048 + ch);
+    };
+    auto multiply = [&](const Half& o) {
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) acc[i][j] = mma<BF16>(o.w[j], o.x[i], acc[i][j]);
+    };
+    // one read for every few products
+    auto mix = [&]() {
+#pragma unroll
+        for (int k = 0; k < MI + NI; k++) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, MI * NI * (BF16 ? 1 : 4) / (MI + NI), 0);
+        }
+    };
+
+    // Step s: its second half is read while the first is multiplied; then every
+    // wave is done with its buffer and the next step's has arrived, so that the
+    // loads of step s + 2 begin and the next first half is read while the second is
+    // multiplied.
     if (s0 < s1) {
         fetch(s0);
         keep(s0);
+        if constexpr (WIDE) dma_wait();
+        __syncthreads();
+        if (s0 + 1 < s1) fetch(s0 + 1);
+        read(even, s0, 0);
+        for (int s = s0; s < s1; s++) {
+            read(odd, s, 1);
+            multiply(even);
+            mix();
+            if (!WIDE && s + 1 < s1) keep(s + 1);
+            if constexpr (WIDE) dma_wait();
+            __syncthreads();
+            if (s + 2 < s1) fetch(s + 2);
+            read(even, s + 1, 0);   // (past the last step: what lies there, unused)
+            multiply(odd);
+            mix();
+        }
     }
     __syncthreads();
-    for (int s = s0; s < s1; s++) {
-        if (s + 1 < s1) fetch(s + 1);
-        const unsigned char* buf = smem + (s & 1) * BUF;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int ch = ((4 * h + g) ^ (l16 & 7)) * 16;
-            u32x4 x[MI], w[NI];
-#pragma unroll
-            for (int i = 0; i < MI; i++) x[i] = *(const u32x4*)(buf + xr + i * 2048 + ch);
-#pragma unroll
-            for (int j = 0; j < NI; j++) w[j] = *(const u32x4*)(buf + wr + j * 2048 + ch);
-#pragma unroll
-            for (int i = 0; i < MI; i++)
-#pragma unroll
-                for (int j = 0; j < NI; j++) acc[i][j] = mma<BF16>(w[j], x[i], acc[i][j]);
-        }
-        if (s + 1 < s1) keep(s + 1);
-        if constexpr (WIDE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the next step's loads are in LDS
-        __syncthreads();
-    }
 
     // the sums go through LDS, up to 64 rows of a wave at a time, so that a row's
     // columns are stored side by side
