@@ -79,7 +79,7 @@ struct Paged {
     const int* table;
     int64_t table_stride;
     char *k, *v;
-    int64_t kp, kt, kh, vp, vt, vh;   // strides in bytes
+    uint32_t kp, kt, kh, vp, vt, vh;  // strides in units of 16 bytes
     int batch, heads, D, bf16;
     int shift, pages, limit;          // log2 of the page size; pages of the pool; positions of an entry
 };
@@ -196,11 +196,17 @@ template <bool BF16> __device__ __forceinline__ void store8(void* p, int64_t at,
 
 // 16 bytes a lane from memory to LDS, lane i's to `lds` + 16 i (an LDS byte address,
 // uniform).  As an instruction of its own: the compiler waits for a load of the
-// builtin before any LDS read, since the two might meet.  The caller waits
-// (dma_wait) before the barrier behind which the bytes are read.
+// builtin before any LDS read, since the two might meet.  (M0 is a register that the
+// compiler keeps nothing in.)  The caller waits (dma_wait) before the barrier
+// behind which the bytes are read.
 __device__ __forceinline__ void dma16(const void* from, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds));
+}
+// The same from base + off, base uniform.
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds));
 }
 __device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p)

@@ -111,25 +111,26 @@ dc_status check_pool(const dc_paged* c)
 {
     PASS(check_paged(c));
     CHECK(c->table && (uintptr_t)c->table % 4 == 0, DC_EINVAL, "the table is NULL or not aligned to its elements");
-    const int64_t per = 16 / size_of(c->dtype);
+    const int64_t per = 16 / size_of(c->dtype), most = ((int64_t)1 << 32) * per;
     for (int v = 0; v < 2; v++) {
         const void* data = v ? c->v : c->k;
-        const int64_t a = v ? c->v_stride_page : c->k_stride_page, b = v ? c->v_stride_t : c->k_stride_t, d = v ? c->v_stride_h : c->k_stride_h;
-        CHECK_OF(data, DC_EINVAL, v ? "v" : "k", ": the pool is NULL");
-        CHECK_OF((uintptr_t)data % 16 == 0 && a % per == 0 && b % per == 0 && d % per == 0, DC_EINVAL, v ? "v" : "k",
-                 ": the pool's rows must be aligned to 16 bytes");
+        const char* what = v ? "v" : "k";
+        CHECK_OF(data && (uintptr_t)data % 16 == 0, DC_EINVAL, what, ": the pool is NULL or not aligned to 16 bytes");
+        for (int64_t s : {v ? c->v_stride_page : c->k_stride_page, v ? c->v_stride_t : c->k_stride_t, v ? c->v_stride_h : c->k_stride_h}) {
+            CHECK_OF(s >= 0 && s % per == 0, DC_EINVAL, what, ": the pool's strides must be >= 0 and keep rows aligned to 16 bytes");
+            CHECK_OF(s < most, DC_ERANGE, what, ": the pool's strides must be below 2^36 bytes");
+        }
     }
     return DC_OK;
 }
 
 Paged paged(const dc_paged* c)
 {
-    const int64_t es = size_of(c->dtype);
-    // (strides in bytes, modulo 2^64 as the addresses that they lead to)
-    auto bytes = [&](int64_t s) { return (int64_t)((uint64_t)s * (uint64_t)es); };
+    const int64_t per = 16 / size_of(c->dtype);
+    auto units = [&](int64_t s) { return (uint32_t)(s / per); };
     return Paged{c->table, c->table_stride, (char*)c->k, (char*)c->v,
-                 bytes(c->k_stride_page), bytes(c->k_stride_t), bytes(c->k_stride_h),
-                 bytes(c->v_stride_page), bytes(c->v_stride_t), bytes(c->v_stride_h),
+                 units(c->k_stride_page), units(c->k_stride_t), units(c->k_stride_h),
+                 units(c->v_stride_page), units(c->v_stride_t), units(c->v_stride_h),
                  c->batch, c->heads, c->head_dim, c->dtype == DC_BF16,
                  __builtin_ctz((unsigned)c->page_size), c->pages, c->page_size * c->table_pages};
 }

@@ -25,6 +25,12 @@ struct Span {
 // `pages` or more).
 __device__ __forceinline__ uint32_t page_of(const Paged& c, int e, int x) { return (uint32_t)c.table[e * c.table_stride + (x >> c.shift)]; }
 
+// Bytes from a pool's start to row `off` of a page.
+__device__ __forceinline__ uint64_t row_offset(uint32_t page, uint32_t sp, uint32_t off, uint32_t st)
+{
+    return ((uint64_t)page * sp + (uint64_t)off * st) << 4;
+}
+
 // ------------------------------------------------------------------- store
 //
 // A thread copies 16 bytes of a key and of its value.  What bounds it: HBM.
@@ -44,8 +50,8 @@ template <int ES> __global__ __launch_bounds__(256) void append_kernel(const Pag
     const int off = (int)x & ((1 << p.c.shift) - 1);
     const u32x4 a = *(const u32x4_any*)((const char*)p.k.p + (p.k.at(e, i, h) + ch * CE) * ES);
     const u32x4 b = *(const u32x4_any*)((const char*)p.v.p + (p.v.at(e, i, h) + ch * CE) * ES);
-    *(u32x4*)(p.c.k + page * p.c.kp + off * p.c.kt + h * p.c.kh + 16 * ch) = a;
-    *(u32x4*)(p.c.v + page * p.c.vp + off * p.c.vt + h * p.c.vh + 16 * ch) = b;
+    *(u32x4*)(p.c.k + row_offset(page, p.c.kp, off, p.c.kt) + 16 * ((uint64_t)h * p.c.kh + ch)) = a;
+    *(u32x4*)(p.c.v + row_offset(page, p.c.vp, off, p.c.vt) + 16 * ((uint64_t)h * p.c.vh + ch)) = b;
 }
 
 hipError_t launch_append(const PagedParams& p, hipStream_t st)
@@ -59,9 +65,8 @@ hipError_t launch_append(const PagedParams& p, hipStream_t st)
 //
 // O = softmax(scale Q K^T) V.  A row is (token i, query head), the `group` query
 // heads of a key head side by side, so shared heads share the loads of their keys.
-// The keys that a block's rows see are one list of members: the first tokens
-// [0, ns), then the positions from `first` on; a row sees [0, sink_hi) and
-// [lo, hi) of it.
+// A block walks tiles of KT keys, which begin at multiples of KT: those of the first
+// tokens, then those from its first row's window on.
 //
 // S^T = K Q^T and O^T += V^T P^T, so that a lane (r, g) = (lane % 16, lane / 16)
 // holds of query r the scores of keys 4 g .. 4 g + 3 of every sixteen, and of its
@@ -69,36 +74,32 @@ hipError_t launch_append(const PagedParams& p, hipStream_t st)
 // for the product with the values, half a step of the result's own type.  fp32:
 // four 16x16x4 products of a 16-byte chunk's elements, in fp32 throughout.
 struct RowSpan {
-    int sink_hi, lo, hi;
-    __device__ __forceinline__ bool sees(int m) const { return (m < sink_hi) | ((uint32_t)(m - lo) < (uint32_t)max(hi - lo, 0)); }
+    int hi, lo, sinks;   // a row sees the positions below hi, of those the ones from lo on and the first `sinks`
+    __device__ __forceinline__ RowSpan(const PagedParams& p, const Span& sp, int i)
+    {
+        const int64_t at = sp.pos + i, limit = p.c.limit;
+        hi = (int)min(p.causal ? at + 1 : sp.total, limit);
+        lo = p.window ? (int)min(max(p.causal ? at + 1 - p.window : sp.pos - p.window, (int64_t)0), limit) : 0;
+        sinks = p.sinks;
+    }
+    __device__ __forceinline__ bool sees(int x) const { return (x < hi) & ((x >= lo) | (x < sinks)); }
 };
 
-struct KeyList {
-    int ns, nk, first;   // first tokens, members, position of the first of the others
-    __device__ __forceinline__ KeyList(const PagedParams& p, const Span& sp, int i0, int i1)
+// The tiles of a block whose rows lie between `lead` and `tail`.
+template <int KT> struct Tiles {
+    int of_sinks, skip, n;   // tiles of the first tokens, tiles left out behind them, tiles in all
+    int all_hi, all_lo;      // every row sees [all_lo, all_hi)
+    __device__ __forceinline__ Tiles(const RowSpan& lead, const RowSpan& tail)
     {
-        const int64_t limit = p.c.limit, end = min(p.causal ? sp.pos + i1 + 1 : sp.total, limit);
-        int64_t from = 0;
-        ns = 0;
-        if (p.window) {
-            from = max(p.causal ? sp.pos + i0 - p.window + 1 : sp.pos - p.window, (int64_t)p.sinks);
-            ns = (int)min(end, (int64_t)p.sinks);
-        }
-        first = (int)min(from, limit);
-        nk = ns + (int)max(end - from, (int64_t)0);
+        of_sinks = (min(tail.sinks, tail.hi) + KT - 1) / KT;
+        const int from = max(lead.lo / KT, of_sinks), end = (tail.hi + KT - 1) / KT;
+        skip = from - of_sinks;
+        n = of_sinks + max(end - from, 0);
+        all_hi = lead.hi;
+        all_lo = tail.lo <= tail.sinks ? 0 : tail.lo;
     }
-    __device__ __forceinline__ int position(int m) const { return m < ns ? m : first + (m - ns); }
-    __device__ __forceinline__ RowSpan row(const PagedParams& p, const Span& sp, int i) const
-    {
-        RowSpan r{ns, ns, nk};
-        if (p.causal) {
-            const int64_t at = sp.pos + i, lo = at - p.window + 1;
-            r.sink_hi = (int)min((int64_t)ns, at + 1);
-            if (p.window) r.lo = ns + (int)min(max(lo - first, (int64_t)0), (int64_t)(nk - ns));
-            r.hi = ns + (int)min(max(at + 1 - first, (int64_t)0), (int64_t)(nk - ns));
-        }
-        return r;
-    }
+    __device__ __forceinline__ int first(int t) const { return KT * (t < of_sinks ? t : t + skip); }   // position
+    __device__ __forceinline__ bool open(int x, int sinks) const { return (x + KT <= all_hi) & ((x >= all_lo) | (x + KT <= sinks)); }
 };
 
 template <bool BF16> __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 acc)
@@ -146,6 +147,11 @@ template <bool BF16> __device__ __forceinline__ bool clear_special(u32x4& w)
 // part has a finite score.  -infinity: it saw nothing.
 constexpr float kSawNothingFinite = -FLT_MAX;
 
+// A row's base is moved only when a score passes it by more than this (a
+// probability's rounding to bf16 is relative, and 2^8 times more fits fp32 with
+// room), so its sums are rarely rescaled.
+constexpr float kSlack = 8.0f;
+
 __device__ __forceinline__ float inverse(float l, float m) { return l != 0.0f ? 1.0f / l : m == -INFINITY ? 0.0f : NAN; }
 
 __device__ __forceinline__ bool any_lane_of_row(bool b)
@@ -173,7 +179,7 @@ __device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int
 
 // Up to 16 rows a block.  Each of its four waves takes a tile of keys in turn,
 // straight from memory to registers, one tile ahead (the pages two ahead), with its
-// own running maximum and sums; the waves meet in LDS at the end.  Values go
+// own base and sums; the waves meet in LDS at the end.  Values go
 // through LDS, for transposed reads.
 template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few(const PagedParams p)
 {
@@ -191,10 +197,8 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
     const int rows = sp.len * p.group, row0 = 16 * (blockIdx.x / p.splits / regions);
     if (row0 >= rows) return;
     const int last = min(row0 + 15, rows - 1), my_row = min(row0 + r, last);
-    const KeyList list(p, sp, row0 / p.group, last / p.group);
-    const RowSpan mine = list.row(p, sp, my_row / p.group);
-    const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
-    const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;   // from here on members are seen by every row
+    const RowSpan mine(p, sp, my_row / p.group), lead(p, sp, row0 / p.group), tail(p, sp, last / p.group);
+    const Tiles<KT> tiles(lead, tail);
 
     u32x4 qf[KS];
     {
@@ -202,40 +206,55 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
 #pragma unroll
         for (int c = 0; c < KS; c++) qf[c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
     }
-    const int tiles = (list.nk + KT - 1) / KT;
-    const int t_lo = (int)((int64_t)tiles * split / p.splits), t_hi = (int)((int64_t)tiles * (split + 1) / p.splits);
+    const int t_lo = (int)((int64_t)tiles.n * split / p.splits), t_hi = (int)((int64_t)tiles.n * (split + 1) / p.splits);
 
     f32x4 o[DB];
 #pragma unroll
     for (int b = 0; b < DB; b++) o[b] = f32x4{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
+    float base = 0.0f, limit = -INFINITY, l = 0.0f;   // what a row's scores are taken from (0 before any), and what moves it
     bool saw = false;
 
     unsigned char* vt = smem + wave * WAVE_LDS;
     u32x4 kn[NB][KS], vn[NB][KS];
     uint32_t page[NB], hole_n = 0;
-    const char *kh = p.c.k + h * p.c.kh + 16 * g, *vh = p.c.v + h * p.c.vh + 16 * g;
+    const int in_page = (1 << p.c.shift) - 1;
+    const bool wide_pages = p.c.shift >= 4;   // sixteen rows lie in one page
+    const char *kh = p.c.k + 16 * (uint64_t)h * p.c.kh, *vh = p.c.v + 16 * (uint64_t)h * p.c.vh;
+    const uint64_t kl = row_offset(0, 0, r, p.c.kt) + 16 * g, vl = row_offset(0, 0, r, p.c.vt) + 16 * g;
     auto find = [&](int t) {
+        const int x = tiles.first(t) + r;
 #pragma unroll
-        for (int b = 0; b < NB; b++) page[b] = page_of(p.c, e, list.position(min(t * KT + 16 * b + r, list.nk - 1)));
+        for (int b = 0; b < NB; b++) page[b] = page_of(p.c, e, min(x + 16 * b, tail.hi - 1));
     };
     auto load = [&](int t) {
         hole_n = 0;
 #pragma unroll
         for (int b = 0; b < NB; b++) {
-            const int key = t * KT + 16 * b + r, off = list.position(key) & ((1 << p.c.shift) - 1);
-            const bool in = key < list.nk, hole = page[b] >= (uint32_t)p.c.pages;
-            hole_n |= (uint32_t)(__ballot(in & hole) & 0xffff) << (16 * b);
-            if (in & !hole) {
-                const char *ka = kh + page[b] * p.c.kp + off * p.c.kt, *va = vh + page[b] * p.c.vp + off * p.c.vt;
+            const int x0 = tiles.first(t) + 16 * b;
+            const uint32_t one = __builtin_amdgcn_readfirstlane(page[b]);
+            if (wide_pages & (one < (uint32_t)p.c.pages) & (x0 + 16 <= tail.hi)) {
+                const uint32_t off = x0 & in_page;
+                const char *ka = kh + row_offset(one, p.c.kp, off, p.c.kt) + kl, *va = vh + row_offset(one, p.c.vp, off, p.c.vt) + vl;
 #pragma unroll
                 for (int c = 0; c < KS; c++) {
                     kn[b][c] = *(const u32x4*)(ka + 64 * c);
                     vn[b][c] = *(const u32x4*)(va + 64 * c);
                 }
-            } else {
+                continue;
+            }
+            // rows past the last key and holes are zeros
+            const bool in = x0 + r < tail.hi, hole = page[b] >= (uint32_t)p.c.pages;
+            const uint32_t off = (x0 + r) & in_page;
+            hole_n |= (uint32_t)(__ballot(in & hole) & 0xffff) << (16 * b);
+            const char *ka = kh + row_offset(page[b], p.c.kp, off, p.c.kt) + 16 * g, *va = vh + row_offset(page[b], p.c.vp, off, p.c.vt) + 16 * g;
 #pragma unroll
-                for (int c = 0; c < KS; c++) kn[b][c] = vn[b][c] = u32x4{0, 0, 0, 0};
+            for (int c = 0; c < KS; c++) kn[b][c] = vn[b][c] = u32x4{0, 0, 0, 0};
+            if (in & !hole) {
+#pragma unroll
+                for (int c = 0; c < KS; c++) {
+                    kn[b][c] = *(const u32x4*)(ka + 64 * c);
+                    vn[b][c] = *(const u32x4*)(va + 64 * c);
+                }
             }
         }
     };
@@ -246,7 +265,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
         if (t + 4 < t_hi) find(t + 4);
     }
     for (; t < t_hi; t += 4) {
-        const int t0 = t * KT;
+        const int x0 = tiles.first(t);
         const uint32_t hole = hole_n;
         f32x4 s[NB];
 #pragma unroll
@@ -261,38 +280,54 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
             load(t + 4);
             if (t + 8 < t_hi) find(t + 8);
         }
-        const bool open = ((t0 + KT <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + KT <= lead.hi))) & (hole == 0);
-        float top = -INFINITY;
+        const bool open = tiles.open(x0, p.sinks) & (hole == 0);
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) s[b][i] *= p.scale_log2;
+        if (open) {
+            saw = true;
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int k = 16 * b + 4 * g + i;
+                    const bool see = mine.sees(x0 + k) & !((hole >> k) & 1);
+                    saw |= see;
+                    s[b][i] = see ? s[b][i] : -INFINITY;
+                }
+        }
+        // (the lanes of a row compare their own keys; they meet only to move its base)
+        float top = s[0][0];
+#pragma unroll
+        for (int k = 1; k < 4 * NB; k++) top = fmaxf(top, s[k >> 2][k & 3]);
+        if (__any(top > limit)) {
+            top = max_xor16_32(top);
+            const bool move = top > limit;
+            const float f = move ? __builtin_amdgcn_exp2f((limit == -INFINITY ? -INFINITY : base) - top) : 1.0f;
+            if (move) {
+                limit = top + kSlack;
+                base = top;
+            }
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < DB; b++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[b][i] *= f;
+        }
 #pragma unroll
         for (int b = 0; b < NB; b++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                const int k = 16 * b + 4 * g + i;
-                const bool see = open | (mine.sees(t0 + k) & !((hole >> k) & 1));
-                saw |= see;
-                s[b][i] = see ? s[b][i] * p.scale_log2 : -INFINITY;
-                top = fmaxf(top, s[b][i]);
+                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - base);
+                l += s[b][i];   // this lane's keys; the lanes of a query are summed at the end
             }
-        top = fmaxf(m, max_xor16_32(top));
-        const float base = top == -INFINITY ? 0.0f : top;   // nothing finite yet: every probability is 0
-        const float alpha = __builtin_amdgcn_exp2f(m - base);
-        m = top;
-        float pr[4 * NB], sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4 * NB; k++) {
-            pr[k] = __builtin_amdgcn_exp2f(s[k >> 2][k & 3] - base);
-            sum += pr[k];
-        }
-        l = l * alpha + sum;   // this lane's keys; the lanes of a query are summed at the end
-#pragma unroll
-        for (int b = 0; b < DB; b++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) o[b][i] *= alpha;
         // (the wave's own region: its LDS operations complete in order)
         __builtin_amdgcn_wave_barrier();
         bool special = false;
         if constexpr (BF16) {
-            const u32x4 pf = {pack2(pr[0], pr[1]), pack2(pr[2], pr[3]), pack2(pr[4], pr[5]), pack2(pr[6], pr[7])};
+            const u32x4 pf = {pack2(s[0][0], s[0][1]), pack2(s[0][2], s[0][3]), pack2(s[1][0], s[1][1]), pack2(s[1][2], s[1][3])};
 #pragma unroll
             for (int b = 0; b < DB; b++) {
                 const unsigned char* a = vt + (4 * g + (r >> 2)) * VROW + 32 * b + 8 * (r & 3);
@@ -311,7 +346,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
                         special |= clear_special<false>(w);
                         x = w[0];
                     }
-                    o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), pr[i], o[b], 0, 0, 0);
+                    o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), s[0][i], o[b], 0, 0, 0);
                 }
         }
         // values that are no numbers reach the rows that see them only
@@ -319,11 +354,11 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
 #pragma unroll 1
             for (int k = 0; k < KT; k++) {
                 const int j = 4 * (k >> 4) + (k & 3);
-                float pk = pr[0];
+                float pk = s[0][0];
 #pragma unroll
-                for (int x = 1; x < 4 * NB; x++) pk = j == x ? pr[x] : pk;
+                for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[x >> 2][x & 3] : pk;
                 pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
-                if (!mine.sees(t0 + k) || ((hole >> k) & 1)) continue;
+                if (!mine.sees(x0 + k) || ((hole >> k) & 1)) continue;
 #pragma unroll
                 for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -336,7 +371,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
         __builtin_amdgcn_wave_barrier();
     }
     l = sum_xor32(sum_xor16(l));
-    if (any_lane_of_row(saw) && m == -INFINITY) m = kSawNothingFinite;
+    const float m = limit != -INFINITY ? base : any_lane_of_row(saw) ? kSawNothingFinite : -INFINITY;
 
     __syncthreads();
     float* mine_o = (float*)vt;                       // [16 queries][D], then m, l [16]
@@ -374,12 +409,8 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
 // Tiles of keys and values go from memory to LDS directly, through two buffers, the
 // next one on its way while this one is worked on (the pages two ahead); 16-byte
 // chunks are stored with their index XORed with bits of the row, so that the rows
-// of an operand read lie in different banks.  The running maximum is moved only
-// when a score passes it by more than 2^8 (a probability's rounding to bf16 is
-// relative, and 2^8 times more fits fp32 with room), so the output is rarely
-// rescaled; in bf16 the probabilities' sum is one more row of the second product.
-constexpr float kSlack = 8.0f;
-
+// of an operand read lie in different banks.  In bf16 the probabilities' sum is one
+// more row of the second product.
 template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void attend_many(const PagedParams p)
 {
     constexpr int ES = BF16 ? 2 : 4, NB = BF16 ? 4 : 2, KT = 16 * NB, KS = D * ES / 64, DB = D / 16, RB = 64 * QG;
@@ -400,47 +431,59 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
     const int rows = sp.len * p.group, row0 = RB * (blocks - 1 - (int)(blockIdx.x / p.splits / regions));
     if (row0 >= rows) return;
     const int last = min(row0 + RB - 1, rows - 1);
-    const KeyList list(p, sp, row0 / p.group, last / p.group);
-    const RowSpan lead = list.row(p, sp, row0 / p.group), tail = list.row(p, sp, last / p.group);
-    const int open_lo = lead.sink_hi == list.ns && tail.lo == list.ns ? 0 : tail.lo;
+    const RowSpan lead(p, sp, row0 / p.group), tail(p, sp, last / p.group);
+    const Tiles<KT> tiles(lead, tail);
 
-    RowSpan mine[QG];
+    int row_at[QG];
     u32x4 qf[QG][KS];
 #pragma unroll
     for (int u = 0; u < QG; u++) {
         const int row = min(row0 + 16 * (QG * wave + u) + r, last), i = row / p.group;
-        mine[u] = list.row(p, sp, i);
+        row_at[u] = i;
         const char* q = (const char*)p.q.p + p.q.at(e, i, h * p.group + row % p.group) * ES;
 #pragma unroll
         for (int c = 0; c < KS; c++) qf[u][c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
     }
-    const int tiles = (list.nk + KT - 1) / KT;
-    const int t_lo = (int)((int64_t)tiles * split / p.splits), t_hi = (int)((int64_t)tiles * (split + 1) / p.splits);
+    const int t_lo = (int)((int64_t)tiles.n * split / p.splits), t_hi = (int)((int64_t)tiles.n * (split + 1) / p.splits);
 
     // which chunk of a row lies in place c of it (and the other way round)
     auto swz_k = [](int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; };
     auto swz_v = [](int row) { return !BF16 ? ((row >> 2) & 3) << 2 : D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; };
+    // an instruction of a wave loads WR consecutive rows; their place, if they lie in one page, is uniform
+    constexpr int WR = 64 / CPR;
+    const bool wide_pages = ((1 << p.c.shift) >= WR) & (p.c.kt < 1u << 24) & (p.c.vt < 1u << 24);
+    const int in_page = (1 << p.c.shift) - 1;
+    const char *kh = p.c.k + 16 * (uint64_t)h * p.c.kh, *vh = p.c.v + 16 * (uint64_t)h * p.c.vh;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * 1024);
     uint32_t page[LOADS];
     auto find = [&](int t) {
+        const int x = tiles.first(t) + tid / CPR;
 #pragma unroll
-        for (int c = 0; c < LOADS; c++)
-            page[c] = page_of(p.c, e, list.position(min(t * KT + tid / CPR + c * (256 / CPR), list.nk - 1)));
+        for (int c = 0; c < LOADS; c++) page[c] = page_of(p.c, e, min(x + c * (256 / CPR), tail.hi - 1));
     };
     auto load = [&](int t) {
         bool any = false;
-        unsigned char* to = smem + (t & 1) * 2 * TILE + wave * 1024;
+        const int x0 = tiles.first(t);
+        const uint32_t to = lds0 + (t & 1) * 2 * TILE;
 #pragma unroll
         for (int c = 0; c < LOADS; c++) {
-            const int row = tid / CPR + c * (256 / CPR), key = t * KT + row, off = list.position(key) & ((1 << p.c.shift) - 1);
-            const bool in = key < list.nk, hole = page[c] >= (uint32_t)p.c.pages, on = in & !hole;
-            any |= in & hole;
-            if (tid % CPR == 0) holes[t & 1][row] = in & hole;
-            const char* ka = p.c.k + page[c] * p.c.kp + off * p.c.kt + h * p.c.kh + 16 * (tid % CPR ^ swz_k(row));
-            const char* va = p.c.v + page[c] * p.c.vp + off * p.c.vt + h * p.c.vh + 16 * (tid % CPR ^ swz_v(row));
-            __builtin_amdgcn_global_load_lds((const void*)(on ? ka : (const char*)&zeros),
-                                             (__attribute__((address_space(3))) void*)(to + c * 4096), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const void*)(on ? va : (const char*)&zeros),
-                                             (__attribute__((address_space(3))) void*)(to + TILE + c * 4096), 16, 0, 0);
+            const int row = tid / CPR + c * (256 / CPR), w0 = wave * WR + c * (256 / CPR), in = lane / CPR;
+            const uint32_t ck = 16 * (tid % CPR ^ swz_k(row)), cv = 16 * (tid % CPR ^ swz_v(row));
+            const uint32_t one = __builtin_amdgcn_readfirstlane(page[c]);
+            if (wide_pages & (one < (uint32_t)p.c.pages) & (x0 + w0 + WR <= tail.hi)) {
+                const uint32_t off = (x0 + w0) & in_page;
+                dma16(kh + row_offset(one, p.c.kp, off, p.c.kt), 16 * in * p.c.kt + ck, to + c * 4096);
+                dma16(vh + row_offset(one, p.c.vp, off, p.c.vt), 16 * in * p.c.vt + cv, to + TILE + c * 4096);
+                if (lane < WR) holes[t & 1][w0 + lane] = 0;
+            } else {   // rows past the last key and holes are zeros
+                const bool on = x0 + row < tail.hi, hole = page[c] >= (uint32_t)p.c.pages;
+                const uint32_t off = (x0 + row) & in_page;
+                any |= on & hole;
+                if (lane % CPR == 0) holes[t & 1][row] = on & hole;
+                const bool there = on & !hole;
+                dma16(there ? kh + row_offset(page[c], p.c.kp, off, p.c.kt) + ck : (const char*)&zeros, to + c * 4096);
+                dma16(there ? vh + row_offset(page[c], p.c.vp, off, p.c.vt) + cv : (const char*)&zeros, to + TILE + c * 4096);
+            }
         }
         hole_any[t & 1][wave] = __any(any);
     };
@@ -466,18 +509,18 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
         if (t_lo + 1 < t_hi) find(t_lo + 1);
     }
     for (int t = t_lo; t < t_hi; t++) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this tile is in LDS
-        __syncthreads();                                   // for every wave, and the one before has been read
+        dma_wait();        // this tile is in LDS
+        __syncthreads();   // for every wave, and the one before has been read
         if (t + 1 < t_hi) {
             load(t + 1);
             if (t + 2 < t_hi) find(t + 2);
         }
         if (!rows_left) continue;
         const unsigned char *kt = smem + (t & 1) * 2 * TILE, *vt = kt + TILE;
-        const int t0 = t * KT;
+        const int x0 = tiles.first(t);
         const bool any_hole = hole_any[t & 1][0] | hole_any[t & 1][1] | hole_any[t & 1][2] | hole_any[t & 1][3];
         // (a scale that turns the scores' order around takes the masking path too)
-        const bool open = ((t0 + KT <= lead.sink_hi) | ((t0 >= open_lo) & (t0 + KT <= lead.hi))) & !any_hole & (p.scale_log2 > 0.0f);
+        const bool open = tiles.open(x0, p.sinks) & !any_hole & (p.scale_log2 > 0.0f);
 
         f32x4 s[QG][NB];
 #pragma unroll
@@ -496,12 +539,13 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
         for (int u = 0; u < QG; u++) {
             // (masked scores are scaled before their mask: 0 times an infinity is NaN)
             if (!open) {
+                const RowSpan mine(p, sp, row_at[u]);
 #pragma unroll
                 for (int b = 0; b < NB; b++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         const int k = 16 * b + 4 * g + i;
-                        bool see = mine[u].sees(t0 + k);
+                        bool see = mine.sees(x0 + k);
                         if (any_hole) see &= !holes[t & 1][k];
                         saw[u] |= see;
                         s[u][b][i] = see ? s[u][b][i] * p.scale_log2 : -INFINITY;
@@ -589,7 +633,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 #pragma unroll
                     for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[u][x >> 2][x & 3] : pk;
                     pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
-                    if (!mine[u].sees(t0 + k) || (any_hole && holes[t & 1][k])) continue;
+                    if (!RowSpan(p, sp, row_at[u]).sees(x0 + k) || (any_hole && holes[t & 1][k])) continue;
 #pragma unroll
                     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -683,7 +727,8 @@ PagedPlan plan_paged(const Paged& c, int n, int group, int window, int sinks)
     const int64_t keys = window ? std::min((int64_t)c.limit, (int64_t)sinks + window + n) : c.limit;
     PagedPlan pl{rows <= 16 ? 16 : c.bf16 && rows > 64 ? 128 : 64, 1, 0};
     const int64_t blocks = regions * ((rows + pl.rows - 1) / pl.rows);
-    if (pl.rows == 16) pl.splits = (int)std::max((int64_t)1, std::min(std::min(1024 / blocks, keys / 256), (int64_t)64));
+    const int fit = c.D == 64 ? 4 : c.bf16 ? 3 : 2;   // blocks of 16 rows on a CU
+    if (pl.rows == 16) pl.splits = (int)std::max((int64_t)1, std::min(std::min(256 * fit / blocks, keys / 256), (int64_t)64));
     else pl.splits = (int)std::max((int64_t)1, std::min(std::min(512 / blocks, keys / 512), (int64_t)16));
     if (pl.splits > 1) pl.ws_bytes = regions * rows * pl.splits * (c.D + 2) * 4;
     return pl;
