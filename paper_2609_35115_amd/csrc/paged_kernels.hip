@@ -2,6 +2,7 @@
 // attention of a call's tokens over the cache.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "block_internal.h"
 
@@ -75,6 +76,7 @@ hipError_t launch_append(const PagedParams& p, hipStream_t st)
 // four 16x16x4 products of a 16-byte chunk's elements, in fp32 throughout.
 struct RowSpan {
     int hi, lo, sinks;   // a row sees the positions below hi, of those the ones from lo on and the first `sinks`
+    RowSpan() = default;
     __device__ __forceinline__ RowSpan(const PagedParams& p, const Span& sp, int i)
     {
         const int64_t at = sp.pos + i, limit = p.c.limit;
@@ -434,12 +436,12 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
     const RowSpan lead(p, sp, row0 / p.group), tail(p, sp, last / p.group);
     const Tiles<KT> tiles(lead, tail);
 
-    int row_at[QG];
+    RowSpan mine[QG];
     u32x4 qf[QG][KS];
 #pragma unroll
     for (int u = 0; u < QG; u++) {
         const int row = min(row0 + 16 * (QG * wave + u) + r, last), i = row / p.group;
-        row_at[u] = i;
+        mine[u] = RowSpan(p, sp, i);
         const char* q = (const char*)p.q.p + p.q.at(e, i, h * p.group + row % p.group) * ES;
 #pragma unroll
         for (int c = 0; c < KS; c++) qf[u][c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
@@ -452,6 +454,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
     // an instruction of a wave loads WR consecutive rows; their place, if they lie in one page, is uniform
     constexpr int WR = 64 / CPR;
     const bool wide_pages = ((1 << p.c.shift) >= WR) & (p.c.kt < 1u << 24) & (p.c.vt < 1u << 24);
+    const bool one_page = wide_pages & ((1 << p.c.shift) >= KT);
     const int in_page = (1 << p.c.shift) - 1;
     const char *kh = p.c.k + 16 * (uint64_t)h * p.c.kh, *vh = p.c.v + 16 * (uint64_t)h * p.c.vh;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * 1024);
@@ -461,10 +464,27 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 #pragma unroll
         for (int c = 0; c < LOADS; c++) page[c] = page_of(p.c, e, min(x + c * (256 / CPR), tail.hi - 1));
     };
-    auto load = [&](int t) {
-        bool any = false;
+    // tile t into buffer `buf`
+    auto load = [&](int t, int buf) {
         const int x0 = tiles.first(t);
-        const uint32_t to = lds0 + (t & 1) * 2 * TILE;
+        const uint32_t to = lds0 + buf * 2 * TILE;
+        const uint32_t page0 = __builtin_amdgcn_readfirstlane(page[0]);
+        if (one_page & (page0 < (uint32_t)p.c.pages) & (x0 + KT <= tail.hi)) {   // the usual tile: whole, of one page
+            const int w0 = wave * WR, in = lane / CPR;
+            const uint32_t off = (x0 & in_page) + w0;
+            const char *kb = kh + row_offset(page0, p.c.kp, off, p.c.kt), *vb = vh + row_offset(page0, p.c.vp, off, p.c.vt);
+#pragma unroll
+            for (int c = 0; c < LOADS; c++) {
+                const int row = tid / CPR + c * (256 / CPR);
+                dma16(kb, 16 * in * p.c.kt + 16 * (tid % CPR ^ swz_k(row)), to + c * 4096);
+                dma16(vb, 16 * in * p.c.vt + 16 * (tid % CPR ^ swz_v(row)), to + TILE + c * 4096);
+                kb += (uint64_t)p.c.kt * (16 * (256 / CPR));
+                vb += (uint64_t)p.c.vt * (16 * (256 / CPR));
+            }
+            if (tid < 4) hole_any[buf][tid] = 0;
+            return;
+        }
+        bool any = false;
 #pragma unroll
         for (int c = 0; c < LOADS; c++) {
             const int row = tid / CPR + c * (256 / CPR), w0 = wave * WR + c * (256 / CPR), in = lane / CPR;
@@ -474,18 +494,18 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                 const uint32_t off = (x0 + w0) & in_page;
                 dma16(kh + row_offset(one, p.c.kp, off, p.c.kt), 16 * in * p.c.kt + ck, to + c * 4096);
                 dma16(vh + row_offset(one, p.c.vp, off, p.c.vt), 16 * in * p.c.vt + cv, to + TILE + c * 4096);
-                if (lane < WR) holes[t & 1][w0 + lane] = 0;
+                if (lane < WR) holes[buf][w0 + lane] = 0;
             } else {   // rows past the last key and holes are zeros
                 const bool on = x0 + row < tail.hi, hole = page[c] >= (uint32_t)p.c.pages;
                 const uint32_t off = (x0 + row) & in_page;
                 any |= on & hole;
-                if (lane % CPR == 0) holes[t & 1][row] = on & hole;
+                if (lane % CPR == 0) holes[buf][row] = on & hole;
                 const bool there = on & !hole;
                 dma16(there ? kh + row_offset(page[c], p.c.kp, off, p.c.kt) + ck : (const char*)&zeros, to + c * 4096);
                 dma16(there ? vh + row_offset(page[c], p.c.vp, off, p.c.vt) + cv : (const char*)&zeros, to + TILE + c * 4096);
             }
         }
-        hole_any[t & 1][wave] = __any(any);
+        hole_any[buf][wave] = __any(any);
     };
 
     f32x4 o[QG][DB], ls[QG];   // ls: the probabilities' sums (bf16: every row the whole sum; fp32: [0], this lane's keys)
@@ -503,22 +523,27 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
     const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 
     const bool rows_left = row0 + 16 * QG * wave <= last;
-    if (t_lo < t_hi) {
-        find(t_lo);
-        load(t_lo);
-        if (t_lo + 1 < t_hi) find(t_lo + 1);
+    // where this lane's operands lie in a buffer
+    uint32_t ka[KS], va[DB];
+#pragma unroll
+    for (int c = 0; c < KS; c++) ka[c] = r * ROW + 16 * ((4 * c + g) ^ swz_k(r));
+#pragma unroll
+    for (int b = 0; b < DB; b++) {
+        const int row = 4 * g + (r >> 2);   // (bf16; fp32: of the first of four rows that have the same places)
+        va[b] = BF16 ? row * ROW + 16 * ((2 * b) ^ swz_v(row)) + 8 * (r & 3) : 4 * g * ROW + 16 * ((4 * b) ^ swz_v(4 * g)) + 4 * r;
     }
-    for (int t = t_lo; t < t_hi; t++) {
+    auto step = [&](int t, auto which) {
+        constexpr int buf = decltype(which)::value;
         dma_wait();        // this tile is in LDS
         __syncthreads();   // for every wave, and the one before has been read
         if (t + 1 < t_hi) {
-            load(t + 1);
+            load(t + 1, 1 - buf);
             if (t + 2 < t_hi) find(t + 2);
         }
-        if (!rows_left) continue;
-        const unsigned char *kt = smem + (t & 1) * 2 * TILE, *vt = kt + TILE;
+        if (!rows_left) return;
+        const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE;
         const int x0 = tiles.first(t);
-        const bool any_hole = hole_any[t & 1][0] | hole_any[t & 1][1] | hole_any[t & 1][2] | hole_any[t & 1][3];
+        const bool any_hole = hole_any[buf][0] | hole_any[buf][1] | hole_any[buf][2] | hole_any[buf][3];
         // (a scale that turns the scores' order around takes the masking path too)
         const bool open = tiles.open(x0, p.sinks) & !any_hole & (p.scale_log2 > 0.0f);
 
@@ -529,7 +554,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
             for (int u = 0; u < QG; u++) s[u][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < KS; c++) {
-                const u32x4 kf = *(const u32x4*)(kt + (16 * b + r) * ROW + 16 * ((4 * c + g) ^ swz_k(r)));
+                const u32x4 kf = *(const u32x4*)(kt + 16 * b * ROW + ka[c]);
 #pragma unroll
                 for (int u = 0; u < QG; u++) s[u][b] = mma<BF16>(kf, qf[u][c], s[u][b]);
             }
@@ -539,14 +564,13 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
         for (int u = 0; u < QG; u++) {
             // (masked scores are scaled before their mask: 0 times an infinity is NaN)
             if (!open) {
-                const RowSpan mine(p, sp, row_at[u]);
 #pragma unroll
                 for (int b = 0; b < NB; b++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         const int k = 16 * b + 4 * g + i;
-                        bool see = mine.sees(x0 + k);
-                        if (any_hole) see &= !holes[t & 1][k];
+                        bool see = mine[u].sees(x0 + k);
+                        if (any_hole) see &= !holes[buf][k];
                         saw[u] |= see;
                         s[u][b][i] = see ? s[u][b][i] * p.scale_log2 : -INFINITY;
                     }
@@ -587,10 +611,9 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                     const f32x4 a = s[u][2 * half], b = s[u][2 * half + 1];
                     pf[u] = u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3])};
                 }
-                const int row = 32 * half + 4 * g + (r >> 2);
 #pragma unroll
                 for (int b = 0; b < DB; b++) {
-                    const unsigned char* a = vt + row * ROW + 16 * ((2 * b) ^ swz_v(row)) + 8 * (r & 3);
+                    const unsigned char* a = vt + 32 * half * ROW + va[b];
                     u32x4 vf = read_tr(a, a + 16 * ROW);
                     if (!open) special |= clear_special<true>(vf);
 #pragma unroll
@@ -610,8 +633,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                 for (int b = 0; b < DB; b++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const int row = 16 * k + 4 * g + i;
-                        uint32_t x = *(const uint32_t*)(vt + row * ROW + 16 * ((4 * b) ^ swz_v(row)) + 4 * r);
+                        uint32_t x = *(const uint32_t*)(vt + (16 * k + i) * ROW + va[b]);
                         if (!open) {
                             u32x4 w = {x, 0, 0, 0};
                             special |= clear_special<false>(w);
@@ -633,7 +655,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 #pragma unroll
                     for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[u][x >> 2][x & 3] : pk;
                     pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
-                    if (!RowSpan(p, sp, row_at[u]).sees(x0 + k) || (any_hole && holes[t & 1][k])) continue;
+                    if (!mine[u].sees(x0 + k) || (any_hole && holes[buf][k])) continue;
 #pragma unroll
                     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -645,6 +667,15 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                 }
             }
         }
+    };
+    if (t_lo < t_hi) {
+        find(t_lo);
+        load(t_lo, 0);
+        if (t_lo + 1 < t_hi) find(t_lo + 1);
+    }
+    for (int t = t_lo; t < t_hi; t += 2) {   // (the buffers' places are constants of the code)
+        step(t, std::integral_constant<int, 0>{});
+        if (t + 1 < t_hi) step(t + 1, std::integral_constant<int, 1>{});
     }
 #pragma unroll
     for (int u = 0; u < QG; u++) {
