@@ -125,6 +125,10 @@ __device__ __forceinline__ u32x4 read_tr(const unsigned char* lo, const unsigned
     return __builtin_bit_cast(u32x4, two);
 }
 
+// A loaded value is waited for here (or the compiler waits where a loop uses it, in
+// every turn, and for that turn's loads as well).
+__device__ __forceinline__ void arrived(u32x4& x) { asm volatile("" : "+v"(x)); }
+
 // Sets infinities and NaN among a chunk's elements to zero; whether there were any.
 template <bool BF16> __device__ __forceinline__ bool clear_special(u32x4& w)
 {
@@ -207,6 +211,8 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
         const char* q = (const char*)p.q.p + p.q.at(e, my_row / p.group, h * p.group + my_row % p.group) * ES;
 #pragma unroll
         for (int c = 0; c < KS; c++) qf[c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
+#pragma unroll
+        for (int c = 0; c < KS; c++) arrived(qf[c]);
     }
     const int t_lo = (int)((int64_t)tiles.n * split / p.splits), t_hi = (int)((int64_t)tiles.n * (split + 1) / p.splits);
 
@@ -446,6 +452,10 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 #pragma unroll
         for (int c = 0; c < KS; c++) qf[u][c] = *(const u32x4_any*)(q + 64 * c + 16 * g);
     }
+#pragma unroll
+    for (int u = 0; u < QG; u++)
+#pragma unroll
+        for (int c = 0; c < KS; c++) arrived(qf[u][c]);
     const int t_lo = (int)((int64_t)tiles.n * split / p.splits), t_hi = (int)((int64_t)tiles.n * (split + 1) / p.splits);
 
     // which chunk of a row lies in place c of it (and the other way round)
@@ -547,18 +557,36 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
         // (a scale that turns the scores' order around takes the masking path too)
         const bool open = tiles.open(x0, p.sinks) & !any_hole & (p.scale_log2 > 0.0f);
 
+        // scores: the next keys' operands are read while these are multiplied
         f32x4 s[QG][NB];
+        u32x4 kf[2][KS];
+        auto read_k = [&](int b) {
+#pragma unroll
+            for (int c = 0; c < KS; c++) kf[b & 1][c] = *(const u32x4*)(kt + 16 * b * ROW + ka[c]);
+        };
+        read_k(0);
 #pragma unroll
         for (int b = 0; b < NB; b++) {
+            if (b + 1 < NB) read_k(b + 1);
 #pragma unroll
             for (int u = 0; u < QG; u++) s[u][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < KS; c++) {
-                const u32x4 kf = *(const u32x4*)(kt + 16 * b * ROW + ka[c]);
+            for (int c = 0; c < KS; c++)
 #pragma unroll
-                for (int u = 0; u < QG; u++) s[u][b] = mma<BF16>(kf, qf[u][c], s[u][b]);
-            }
+                for (int u = 0; u < QG; u++) s[u][b] = mma<BF16>(kf[b & 1][c], qf[u][c], s[u][b]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        // the first values' operands, read while the probabilities are computed
+        constexpr int VB = 4;
+        u32x4 vf[2][VB];
+        auto read_v = [&](int half, int b0) {
+#pragma unroll
+            for (int b = 0; b < VB; b++) {
+                const unsigned char* a = vt + 32 * half * ROW + va[b0 + b];
+                vf[(half * DB + b0) / VB & 1][b] = read_tr(a, a + 16 * ROW);
+            }
+        };
+        if constexpr (BF16) read_v(0, 0);
         const float mul = open ? p.scale_log2 : 1.0f;
 #pragma unroll
         for (int u = 0; u < QG; u++) {
@@ -612,12 +640,17 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                     pf[u] = u32x4{pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3])};
                 }
 #pragma unroll
-                for (int b = 0; b < DB; b++) {
-                    const unsigned char* a = vt + 32 * half * ROW + va[b];
-                    u32x4 vf = read_tr(a, a + 16 * ROW);
-                    if (!open) special |= clear_special<true>(vf);
+                for (int b0 = 0; b0 < DB; b0 += VB) {
+                    if (b0 + VB < DB) read_v(half, b0 + VB);
+                    else if (half == 0) read_v(1, 0);
 #pragma unroll
-                    for (int u = 0; u < QG; u++) o[u][b] = mma<true>(vf, pf[u], o[u][b]);
+                    for (int b = 0; b < VB; b++) {
+                        u32x4& v = vf[(half * DB + b0) / VB & 1][b];
+                        if (!open) special |= clear_special<true>(v);
+#pragma unroll
+                        for (int u = 0; u < QG; u++) o[u][b0 + b] = mma<true>(v, pf[u], o[u][b0 + b]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
                 for (int u = 0; u < QG; u++) ls[u] = mma<true>(ones, pf[u], ls[u]);
