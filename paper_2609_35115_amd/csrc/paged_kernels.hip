@@ -129,23 +129,68 @@ __device__ __forceinline__ u32x4 read_tr(const unsigned char* lo, const unsigned
 // every turn, and for that turn's loads as well).
 __device__ __forceinline__ void arrived(u32x4& x) { asm volatile("" : "+v"(x)); }
 
-// Sets infinities and NaN among a chunk's elements to zero; whether there were any.
-template <bool BF16> __device__ __forceinline__ bool clear_special(u32x4& w)
+// Bits of a chunk's elements that are an infinity or a NaN.
+template <bool BF16> __device__ __forceinline__ uint32_t special_of(u32x4 w)
 {
-    bool any = false;
+    uint32_t bits = 0;
 #pragma unroll
     for (int k = 0; k < 4; k++) {
-        const bool hi = (w[k] & 0x7f800000u) == 0x7f800000u;
-        if constexpr (BF16) {
-            const bool lo = (w[k] & 0x7f80u) == 0x7f80u;
-            any |= lo | hi;
-            w[k] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
-        } else {
-            any |= hi;
-            if (hi) w[k] = 0;
+        const uint32_t hi = (w[k] & 0x7f800000u) == 0x7f800000u, lo = (w[k] & 0x7f80u) == 0x7f80u;
+        bits |= BF16 ? (lo | hi << 1) << (2 * k) : hi << k;
+    }
+    return bits;
+}
+
+// Values that are no numbers reach the rows that see them only, and 0 times them is
+// not 0: they are added to the rows' results one by one here, and the caller sets
+// them to zero before the product.  `where(c)` is the lane's c-th chunk of a tile's
+// `chunks`: its address, key and first dimension; s holds the probabilities.
+struct ChunkAt {
+    unsigned char* p;
+    int key, d;
+};
+template <bool BF16, int QG, int NB, int DB, class Where, class Sees>
+__device__ __forceinline__ void add_special(int chunks, Where where, Sees sees, const f32x4 (&s)[QG][NB], f32x4 (&o)[QG][DB])
+{
+    const int r = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+#pragma unroll 1
+    for (int c = 0; c < chunks; c++) {
+        const ChunkAt at = where(c);
+        uint32_t bits = special_of<BF16>(*(const u32x4*)at.p);
+#pragma unroll 1
+        for (uint64_t lanes = __ballot(bits != 0); lanes; lanes = __ballot(bits != 0)) {
+            const int from = __builtin_ctzll(lanes), el = __builtin_ctz(__builtin_amdgcn_readlane(bits, from));
+            const int key = __builtin_amdgcn_readlane(at.key, from), d = __builtin_amdgcn_readlane(at.d, from) + el;
+            float v = load1(at.p, el, BF16);
+            v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), from));
+            if ((int)(threadIdx.x & 63) == from) bits &= bits - 1;
+            const int j = 4 * (key >> 4) + (key & 3);
+#pragma unroll
+            for (int u = 0; u < QG; u++) {
+                float pk = s[u][0][0];
+#pragma unroll
+                for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[u][x >> 2][x & 3] : pk;
+                pk = __shfl(pk, 16 * ((key >> 2) & 3) + r);
+                const bool mine = sees(u, key) & (g == ((d >> 2) & 3));
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (mine & (16 * b + i == (d & ~12))) o[u][b][i] = fmaf(pk, v, o[u][b][i]);
+            }
         }
     }
-    return any;
+}
+// A chunk without them.
+template <bool BF16> __device__ __forceinline__ u32x4 clear_special(u32x4 w)
+{
+    const uint32_t bits = special_of<BF16>(w);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        if constexpr (BF16) w[k] &= ((bits >> (2 * k)) & 1 ? 0xffff0000u : 0xffffffffu) & ((bits >> (2 * k)) & 2 ? 0x0000ffffu : 0xffffffffu);
+        else w[k] = (bits >> k) & 1 ? 0 : w[k];
+    }
+    return w;
 }
 
 // The base of a row's exponentials where it saw keys, all of whose scores are
@@ -187,7 +232,8 @@ __device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int
 // straight from memory to registers, one tile ahead (the pages two ahead), with its
 // own base and sums; the waves meet in LDS at the end.  Values go
 // through LDS, for transposed reads.
-template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few(const PagedParams p)
+template <bool BF16, int D> constexpr int few_blocks() { return D == 64 ? 4 : BF16 ? 3 : 2; }   // on a CU
+template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, D>())) void attend_few(const PagedParams p)
 {
     constexpr int ES = BF16 ? 2 : 4, CE = 16 / ES, NB = BF16 ? 2 : 1, KT = 16 * NB;   // sixteens and keys of a tile
     constexpr int KS = D * ES / 64, DB = D / 16;
@@ -216,9 +262,9 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
     }
     const int t_lo = (int)((int64_t)tiles.n * split / p.splits), t_hi = (int)((int64_t)tiles.n * (split + 1) / p.splits);
 
-    f32x4 o[DB];
+    f32x4 o[1][DB];
 #pragma unroll
-    for (int b = 0; b < DB; b++) o[b] = f32x4{0, 0, 0, 0};
+    for (int b = 0; b < DB; b++) o[0][b] = f32x4{0, 0, 0, 0};
     float base = 0.0f, limit = -INFINITY, l = 0.0f;   // what a row's scores are taken from (0 before any), and what moves it
     bool saw = false;
 
@@ -275,12 +321,12 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
     for (; t < t_hi; t += 4) {
         const int x0 = tiles.first(t);
         const uint32_t hole = hole_n;
-        f32x4 s[NB];
+        f32x4 s[1][NB];
 #pragma unroll
         for (int b = 0; b < NB; b++) {
-            s[b] = f32x4{0, 0, 0, 0};
+            s[0][b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < KS; c++) s[b] = mma<BF16>(kn[b][c], qf[c], s[b]);
+            for (int c = 0; c < KS; c++) s[0][b] = mma<BF16>(kn[b][c], qf[c], s[0][b]);
 #pragma unroll
             for (int c = 0; c < KS; c++) *(u32x4*)(vt + (16 * b + r) * VROW + 64 * c + 16 * g) = vn[b][c];
         }
@@ -292,7 +338,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
 #pragma unroll
         for (int b = 0; b < NB; b++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) s[b][i] *= p.scale_log2;
+            for (int i = 0; i < 4; i++) s[0][b][i] *= p.scale_log2;
         if (open) {
             saw = true;
         } else {
@@ -303,13 +349,13 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
                     const int k = 16 * b + 4 * g + i;
                     const bool see = mine.sees(x0 + k) & !((hole >> k) & 1);
                     saw |= see;
-                    s[b][i] = see ? s[b][i] : -INFINITY;
+                    s[0][b][i] = see ? s[0][b][i] : -INFINITY;
                 }
         }
         // (the lanes of a row compare their own keys; they meet only to move its base)
-        float top = s[0][0];
+        float top = s[0][0][0];
 #pragma unroll
-        for (int k = 1; k < 4 * NB; k++) top = fmaxf(top, s[k >> 2][k & 3]);
+        for (int k = 1; k < 4 * NB; k++) top = fmaxf(top, s[0][k >> 2][k & 3]);
         if (__any(top > limit)) {
             top = max_xor16_32(top);
             const bool move = top > limit;
@@ -322,59 +368,45 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
 #pragma unroll
             for (int b = 0; b < DB; b++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) o[b][i] *= f;
+                for (int i = 0; i < 4; i++) o[0][b][i] *= f;
         }
 #pragma unroll
         for (int b = 0; b < NB; b++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - base);
-                l += s[b][i];   // this lane's keys; the lanes of a query are summed at the end
+                s[0][b][i] = __builtin_amdgcn_exp2f(s[0][b][i] - base);
+                l += s[0][b][i];   // this lane's keys; the lanes of a query are summed at the end
             }
         // (the wave's own region: its LDS operations complete in order)
         __builtin_amdgcn_wave_barrier();
-        bool special = false;
+        if (!open) {
+            bool special = false;
+            auto where = [&](int c) {
+                const int key = 16 * (c / KS) + r, at = 64 * (c % KS) + 16 * g;
+                return ChunkAt{vt + key * VROW + at, key, at / ES};
+            };
+#pragma unroll
+            for (int c = 0; c < NB * KS; c++) special |= special_of<BF16>(*(const u32x4*)where(c).p) != 0;
+            if (__builtin_expect(__any(special), 0)) {
+                add_special<BF16>(NB * KS, where, [&](int, int k) { return mine.sees(x0 + k) & !((hole >> k) & 1); }, s, o);
+#pragma unroll
+                for (int c = 0; c < NB * KS; c++) *(u32x4*)where(c).p = clear_special<BF16>(*(const u32x4*)where(c).p);
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
         if constexpr (BF16) {
-            const u32x4 pf = {pack2(s[0][0], s[0][1]), pack2(s[0][2], s[0][3]), pack2(s[1][0], s[1][1]), pack2(s[1][2], s[1][3])};
+            const u32x4 pf = {pack2(s[0][0][0], s[0][0][1]), pack2(s[0][0][2], s[0][0][3]), pack2(s[0][1][0], s[0][1][1]), pack2(s[0][1][2], s[0][1][3])};
 #pragma unroll
             for (int b = 0; b < DB; b++) {
                 const unsigned char* a = vt + (4 * g + (r >> 2)) * VROW + 32 * b + 8 * (r & 3);
-                u32x4 vf = read_tr(a, a + 16 * VROW);
-                if (!open) special |= clear_special<true>(vf);
-                o[b] = mma<true>(vf, pf, o[b]);
+                o[0][b] = mma<true>(read_tr(a, a + 16 * VROW), pf, o[0][b]);
             }
         } else {
 #pragma unroll
             for (int b = 0; b < DB; b++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    uint32_t x = *(const uint32_t*)(vt + (4 * g + i) * VROW + 64 * b + 4 * r);
-                    if (!open) {
-                        u32x4 w = {x, 0, 0, 0};
-                        special |= clear_special<false>(w);
-                        x = w[0];
-                    }
-                    o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), s[0][i], o[b], 0, 0, 0);
-                }
-        }
-        // values that are no numbers reach the rows that see them only
-        if (__builtin_expect(__any(special), 0)) {
-#pragma unroll 1
-            for (int k = 0; k < KT; k++) {
-                const int j = 4 * (k >> 4) + (k & 3);
-                float pk = s[0][0];
-#pragma unroll
-                for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[x >> 2][x & 3] : pk;
-                pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
-                if (!mine.sees(x0 + k) || ((hole >> k) & 1)) continue;
-#pragma unroll
-                for (int b = 0; b < DB; b++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float v = load1(vt + k * VROW, 16 * b + 4 * g + i, BF16);
-                        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[b][i] = fmaf(pk, v, o[b][i]);
-                    }
-            }
+                for (int i = 0; i < 4; i++)
+                    o[0][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(const float*)(vt + (4 * g + i) * VROW + 64 * b + 4 * r), s[0][0][i], o[0][b], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -384,7 +416,7 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, 2) void attend_few
     __syncthreads();
     float* mine_o = (float*)vt;                       // [16 queries][D], then m, l [16]
 #pragma unroll
-    for (int b = 0; b < DB; b++) *(f32x4*)(mine_o + r * D + 16 * b + 4 * g) = o[b];
+    for (int b = 0; b < DB; b++) *(f32x4*)(mine_o + r * D + 16 * b + 4 * g) = o[0][b];
     if (g == 0) {
         mine_o[16 * D + r] = m;
         mine_o[16 * D + 16 + r] = l;
@@ -425,8 +457,8 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
     constexpr int ROW = D * ES, CPR = ROW / 16, LOADS = KT * CPR / 256;   // bytes, chunks of a row; a thread's of a tile
     constexpr int TILE = KT * ROW;
     __shared__ __align__(16) unsigned char smem[4 * TILE];                // [buffer][keys, values]
-    __shared__ uint8_t holes[2][KT];
-    __shared__ int hole_any[2][4];
+    __shared__ __align__(4) uint8_t holes[2][KT];
+    __shared__ int hole_any[2][4], special_any[4];
     __device__ static const u32x4 zeros = {0, 0, 0, 0};
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -550,14 +582,25 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
             load(t + 1, 1 - buf);
             if (t + 2 < t_hi) find(t + 2);
         }
-        if (!rows_left) return;
-        const unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE;
+        unsigned char *kt = smem + buf * 2 * TILE, *vt = kt + TILE;
         const int x0 = tiles.first(t);
         const bool any_hole = hole_any[buf][0] | hole_any[buf][1] | hole_any[buf][2] | hole_any[buf][3];
         // (a scale that turns the scores' order around takes the masking path too)
         const bool open = tiles.open(x0, p.sinks) & !any_hole & (p.scale_log2 > 0.0f);
 
         // scores: the next keys' operands are read while these are multiplied
+        bool special = false;
+        auto where = [&](int c) {
+            const int at = 1024 * c + 16 * lane, key = at / ROW;
+            return ChunkAt{vt + at, key, ((at % ROW / 16) ^ swz_v(key)) * (16 / ES)};
+        };
+        if (!open) {
+            for (int c = wave; c < TILE / 1024; c += 4) special |= special_of<BF16>(*(const u32x4*)where(c).p) != 0;
+            special_any[wave] = __any(special);
+            __syncthreads();
+            special = special_any[0] | special_any[1] | special_any[2] | special_any[3];
+        }
+        if (!rows_left & !special) return;
         f32x4 s[QG][NB];
         u32x4 kf[2][KS];
         auto read_k = [&](int b) {
@@ -593,15 +636,15 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
             // (masked scores are scaled before their mask: 0 times an infinity is NaN)
             if (!open) {
 #pragma unroll
-                for (int b = 0; b < NB; b++)
+                for (int b = 0; b < NB; b++) {
+                    const uint32_t hole = any_hole ? *(const uint32_t*)(holes[buf] + 16 * b + 4 * g) : 0;   // of four keys, a byte each
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const int k = 16 * b + 4 * g + i;
-                        bool see = mine[u].sees(x0 + k);
-                        if (any_hole) see &= !holes[buf][k];
+                        const bool see = mine[u].sees(x0 + 16 * b + 4 * g + i) & !((hole >> (8 * i)) & 1);
                         saw[u] |= see;
                         s[u][b][i] = see ? s[u][b][i] * p.scale_log2 : -INFINITY;
                     }
+                }
             } else {
                 saw[u] = true;
             }
@@ -629,7 +672,15 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 #pragma unroll
                 for (int i = 0; i < 4; i++) s[u][b][i] = __builtin_amdgcn_exp2f(fmaf(s[u][b][i], mul, -base[u]));
         }
-        bool special = false;
+        if (__builtin_expect(special, 0)) {   // (a rule on the tile: the block's waves meet here)
+            if (rows_left)
+                add_special<BF16>(TILE / 1024, where, [&](int u, int k) { return mine[u].sees(x0 + k) & !(any_hole && holes[buf][k]); }, s, o);
+            __syncthreads();
+            for (int c = wave; c < TILE / 1024; c += 4) *(u32x4*)where(c).p = clear_special<BF16>(*(const u32x4*)where(c).p);
+            __syncthreads();
+            if constexpr (BF16) read_v(0, 0);
+        }
+        if (!rows_left) return;
         if constexpr (BF16) {
 #pragma unroll
             for (int half = 0; half < 2; half++) {
@@ -644,12 +695,9 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                     if (b0 + VB < DB) read_v(half, b0 + VB);
                     else if (half == 0) read_v(1, 0);
 #pragma unroll
-                    for (int b = 0; b < VB; b++) {
-                        u32x4& v = vf[(half * DB + b0) / VB & 1][b];
-                        if (!open) special |= clear_special<true>(v);
+                    for (int b = 0; b < VB; b++)
 #pragma unroll
-                        for (int u = 0; u < QG; u++) o[u][b0 + b] = mma<true>(v, pf[u], o[u][b0 + b]);
-                    }
+                        for (int u = 0; u < QG; u++) o[u][b0 + b] = mma<true>(vf[(half * DB + b0) / VB & 1][b], pf[u], o[u][b0 + b]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
@@ -666,39 +714,10 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
                 for (int b = 0; b < DB; b++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        uint32_t x = *(const uint32_t*)(vt + (16 * k + i) * ROW + va[b]);
-                        if (!open) {
-                            u32x4 w = {x, 0, 0, 0};
-                            special |= clear_special<false>(w);
-                            x = w[0];
-                        }
+                        const float x = *(const float*)(vt + (16 * k + i) * ROW + va[b]);
 #pragma unroll
-                        for (int u = 0; u < QG; u++)
-                            o[u][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x), s[u][k][i], o[u][b], 0, 0, 0);
+                        for (int u = 0; u < QG; u++) o[u][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[u][k][i], o[u][b], 0, 0, 0);
                     }
-        }
-        // values that are no numbers reach the rows that see them only
-        if (__builtin_expect(__any(special), 0)) {
-#pragma unroll 1
-            for (int k = 0; k < KT; k++) {
-#pragma unroll
-                for (int u = 0; u < QG; u++) {
-                    const int j = 4 * (k >> 4) + (k & 3);
-                    float pk = s[u][0][0];
-#pragma unroll
-                    for (int x = 1; x < 4 * NB; x++) pk = j == x ? s[u][x >> 2][x & 3] : pk;
-                    pk = __shfl(pk, 16 * ((k >> 2) & 3) + r);
-                    if (!mine[u].sees(x0 + k) || (any_hole && holes[buf][k])) continue;
-#pragma unroll
-                    for (int b = 0; b < DB; b++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const int d = 16 * b + 4 * g + i, ch = d * ES / 16;
-                            const float v = load1(vt + k * ROW + 16 * (ch ^ swz_v(k)), d % (16 / ES), BF16);
-                            if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[u][b][i] = fmaf(pk, v, o[u][b][i]);
-                        }
-                }
-            }
         }
     };
     if (t_lo < t_hi) {
