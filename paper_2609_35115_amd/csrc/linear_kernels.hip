@@ -174,90 +174,131 @@ template <int COLS> __device__ __forceinline__ void finish(const LinearParams& p
 // ----------------------------------------------------------- tiles of rows
 //
 // A block computes BM rows by BN columns (with glu BN / 2 columns and their
-// factors), its WM x WN waves a part each.  Both operands' K steps go through two
-// LDS buffers, the next one loaded while this one is multiplied; a row's eight
-// chunks are stored with their index XORed with the row's low bits, so that the
-// sixteen rows of an operand read lie in different banks.  With WIDE the loads go
-// from memory to LDS directly, else (rows or K not of whole chunks) through
-// registers.  Rows that the call does not have are read from the weight instead
-// and columns past N from its last row: their results are not stored.
-template <bool BF16, int BM, int BN, int WM, int WN, bool WIDE>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kernel(const LinearParams p)
+// factors), its WM x WN waves a part each.
+
+// Which tile and split a block has.  Blocks are dealt to the eight XCDs in turn: each
+// takes a run of the tiles, in strips of eight row tiles, whose operands its L2
+// holds.
+template <int BM, int BN> struct TileAt {
+    int m0, n0, split;
+    __device__ __forceinline__ TileAt(const LinearParams& p)
+    {
+        const int BC = p.glu ? BN / 2 : BN;   // columns of a block
+        const int mt = (p.M + BM - 1) / BM, nt = (p.N + BC - 1) / BC;
+        const int64_t eighth = (int64_t)mt * nt * p.splits / 8;
+        int64_t id = blockIdx.x;
+        if (id < eighth * 8) id = id % 8 * eighth + id / 8;
+        split = (int)(id % p.splits);
+        const int tile = (int)(id / p.splits), strip = tile / (8 * nt), in = tile - strip * 8 * nt;
+        const int high = min(8, mt - 8 * strip);
+        m0 = (8 * strip + in % high) * BM;
+        n0 = in / high * BC;
+    }
+};
+
+// The operands' rows that a thread loads: its chunk of rows tid / 8 + c T / 8, first
+// the BM rows of x, then those of the weight.  Rows that the call does not have are
+// read from the weight instead and columns past N from its last row: their results
+// are not stored.  Whether any of them is a row of x that the call has.
+template <int BM, int BN, int WN, int T, int ES, int LOADS>
+__device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt<BM, BN>& at, const char* (&row)[LOADS])
 {
-    constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, CE = chunk_elems<BF16>(), ES = 16 / CE;
-    constexpr int KT = kChunks * CE, ROWS = BM + BN, LOADS = ROWS * kChunks / T;
-    constexpr int BUF = ROWS * kChunks * 16;
-    constexpr int COLS = BN / WN, PITCH = COLS + 4, SR = BM / WM < 64 ? BM / WM : 64;   // the sums' way through LDS
-    constexpr int OUT = WM * WN * SR * PITCH * 4, LDS = 2 * BUF > OUT ? 2 * BUF : OUT;
-    static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0);
-    __shared__ __align__(16) unsigned char smem[LDS];
-    __shared__ int some;
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
-    const int BC = p.glu ? BN / 2 : BN;                       // columns of a block
-    const int mt = (p.M + BM - 1) / BM, nt = (p.N + BC - 1) / BC;
-    // blocks are dealt to the eight XCDs in turn: each takes a run of the tiles, in
-    // strips of eight row tiles, whose operands its L2 holds
-    const int64_t blocks = (int64_t)mt * nt * p.splits;
-    int64_t id = blockIdx.x;
-    const int64_t eighth = blocks / 8;
-    if (id < eighth * 8) id = id % 8 * eighth + id / 8;
-    const int split = (int)(id % p.splits);
-    const int tile = (int)(id / p.splits), strip = tile / (8 * nt), in = tile - strip * 8 * nt;
-    const int high = min(8, mt - 8 * strip);
-    const int m0 = (8 * strip + in % high) * BM, n0 = in / high * BC;
-
-    // this thread's rows of the operands: chunk `tid % 8` of rows tid / 8 + c T / 8
-    if (tid == 0) some = 0;
-    __syncthreads();
-    const char* row[LOADS];
+    constexpr int NI = BN / WN / 16;
     bool any = false;
 #pragma unroll
     for (int c = 0; c < LOADS; c++) {
-        const int rr = tid / kChunks + c * (T / kChunks);
+        const int rr = threadIdx.x / kChunks + c * (T / kChunks);
         if (rr < BM) {
-            const Place at(p, m0 + rr);
-            any |= at.on;
-            row[c] = at.on ? (const char*)p.x.p + (at.e * p.x.sb + at.i * p.x.st) * ES : (const char*)p.w;
+            const Place x(p, at.m0 + rr);
+            any |= x.on;
+            row[c] = x.on ? (const char*)p.x.p + (x.e * p.x.sb + x.i * p.x.st) * ES : (const char*)p.w;
         } else {
             int r = rr - BM, col, part = 0;
             if (p.glu) {   // a wave's first half of 16-column groups, and the same columns' factors
                 const int w = r / (BN / WN), f = r / 16 % NI;
                 part = f >= NI / 2;
-                col = n0 + w * (BN / WN / 2) + (f - part * (NI / 2)) * 16 + r % 16;
+                col = at.n0 + w * (BN / WN / 2) + (f - part * (NI / 2)) * 16 + r % 16;
             } else {
-                col = n0 + r;
+                col = at.n0 + r;
             }
             row[c] = (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
         }
     }
-    if (any) some = 1;
+    return any;
+}
+
+// The sums of a wave's rows (m0 on) and columns (n0 on) go through LDS, up to 64 rows
+// at a time, so that a row's columns are stored side by side.
+template <int MI, int NI> constexpr int out_rows() { return MI < 4 ? 16 * MI : 64; }
+template <int MI, int NI> constexpr int out_bytes() { return out_rows<MI, NI>() * (16 * NI + 4) * 4; }
+template <int MI, int NI>
+__device__ __forceinline__ void write_out(const LinearParams& p, float* mine, const f32x4 (&acc)[MI][NI], int m0, int n0, int split)
+{
+    constexpr int SR = out_rows<MI, NI>(), PITCH = 16 * NI + 4;
+    const int l16 = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int c = 0; c < MI; c += SR / 16) {
+#pragma unroll
+        for (int i = 0; i < SR / 16; i++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) *(f32x4*)(mine + (16 * i + l16) * PITCH + 16 * j + 4 * g) = acc[c + i][j];
+        // (the wave's own region: its LDS operations complete in order)
+        __builtin_amdgcn_wave_barrier();
+        finish<16 * NI>(p, mine, SR, PITCH, m0 + 16 * c, n0, split);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <int N> __device__ __forceinline__ void dma_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Both operands' K steps go through a ring of ST LDS buffers, the next ones on
+// their way while one is multiplied; a row's eight chunks are stored with their index
+// XORed with the row's low bits, so that the sixteen rows of an operand read lie in
+// different banks.  With WIDE the loads go from memory to LDS directly, else (rows
+// or K not of whole chunks) through registers.
+template <bool BF16, int BM, int BN, int WM, int WN, bool WIDE, int ST>
+__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParams p)
+{
+    constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, CE = chunk_elems<BF16>(), ES = 16 / CE;
+    constexpr int KT = kChunks * CE, ROWS = BM + BN, LOADS = ROWS * kChunks / T;
+    constexpr int BUF = ROWS * kChunks * 16;
+    constexpr int OUT = WM * WN * out_bytes<MI, NI>(), LDS = ST * BUF > OUT ? ST * BUF : OUT;
+    static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0 && (WIDE || ST == 2));
+    __shared__ __align__(16) unsigned char smem[LDS];
+    __shared__ int some;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
+    const TileAt<BM, BN> at(p);
+    if (tid == 0) some = 0;
+    __syncthreads();
+    const char* row[LOADS];
+    if (operand_rows<BM, BN, WN, T, ES>(p, at, row)) some = 1;
     __syncthreads();
     if (!some) return;   // all rows are behind their entries' last tokens
 
     const int kc = ((tid % kChunks) ^ (tid / kChunks & 7)) * CE;   // where in the K step this thread's chunk lies
     const int steps = (p.K + KT - 1) / KT;
-    const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
+    const int s0 = (int)((int64_t)steps * at.split / p.splits), s1 = (int)((int64_t)steps * (at.split + 1) / p.splits);
 
     u32x4 stage[WIDE ? 1 : LOADS];
     __device__ static const u32x4 zeros = {0, 0, 0, 0};
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * 1024);
-    auto fetch = [&](int s) {
+    auto fetch = [&](int s, int slot) {
         const int k = s * KT + kc;
         if constexpr (WIDE) {
 #pragma unroll
             for (int c = 0; c < LOADS; c++)
-                dma16(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros, lds0 + (s & 1) * BUF + c * (T * 16));
+                dma16(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros, lds0 + slot * BUF + c * (T * 16));
         } else {
 #pragma unroll
             for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<BF16>(row[c], k, p.K);
         }
     };
-    auto keep = [&](int s) {
+    auto keep = [&](int slot) {
         if constexpr (!WIDE) {
 #pragma unroll
-            for (int c = 0; c < LOADS; c++) *(u32x4*)(smem + (s & 1) * BUF + (c * T + tid) * 16) = stage[c];
+            for (int c = 0; c < LOADS; c++) *(u32x4*)(smem + slot * BUF + (c * T + tid) * 16) = stage[c];
         }
     };
 
@@ -272,8 +313,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
         u32x4 x[MI], w[NI];
     } even, odd;
     const unsigned char *xl = smem + (wm * (BM / WM) + l16) * 128, *wl = smem + (BM + wn * (BN / WN) + l16) * 128;
-    auto read = [&](Half& o, int s, int h) {
-        const int ch = (s & 1) * BUF + ((4 * h + g) ^ (l16 & 7)) * 16;
+    auto read = [&](Half& o, int slot, int h) {
+        const int ch = slot * BUF + ((4 * h + g) ^ (l16 & 7)) * 16;
 #pragma unroll
         for (int j = 0; j < NI; j++) o.w[j] = *(const u32x4*)(wl + j * 2048 + ch);
 #pragma unroll
@@ -296,44 +337,136 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void tile_kerne
 
     // Step s: its second half is read while the first is multiplied; then every
     // wave is done with its buffer and the next step's has arrived, so that the
-    // loads of step s + 2 begin and the next first half is read while the second is
+    // loads of step s + ST begin and the next first half is read while the second is
     // multiplied.
     if (s0 < s1) {
-        fetch(s0);
-        keep(s0);
-        if constexpr (WIDE) dma_wait();
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int q = 0; q < ST; q++)
+                if (s0 + q < s1) fetch(s0 + q, q);
+            if (s0 + ST <= s1) dma_wait_but<(ST - 1) * LOADS>();
+            else dma_wait();
+        } else {
+            fetch(s0, 0);
+            keep(0);
+            if (s0 + 1 < s1) fetch(s0 + 1, 1);
+        }
         __syncthreads();
-        if (s0 + 1 < s1) fetch(s0 + 1);
-        read(even, s0, 0);
+        read(even, 0, 0);
+        int slot = 0, next = 1;
         for (int s = s0; s < s1; s++) {
-            read(odd, s, 1);
+            read(odd, slot, 1);
             multiply(even);
             mix();
-            if (!WIDE && s + 1 < s1) keep(s + 1);
-            if constexpr (WIDE) dma_wait();
+            if constexpr (!WIDE) {
+                if (s + 1 < s1) keep(next);
+            } else {
+                if (s + ST <= s1) dma_wait_but<(ST - 2) * LOADS>();   // (the last steps' waits are for all that is left)
+                else dma_wait();
+            }
             __syncthreads();
-            if (s + 2 < s1) fetch(s + 2);
-            read(even, s + 1, 0);   // (past the last step: what lies there, unused)
+            if (s + ST < s1) fetch(s + ST, slot);
+            slot = next;
+            next = next + 1 == ST ? 0 : next + 1;
+            read(even, slot, 0);   // (past the last step: what lies there, unused)
             multiply(odd);
             mix();
         }
     }
     __syncthreads();
+    write_out<MI, NI>(p, (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
+                      at.n0 + wn * (p.glu ? BN / WN / 2 : BN / WN), at.split);
+}
 
-    // the sums go through LDS, up to 64 rows of a wave at a time, so that a row's
-    // columns are stored side by side
-    float* mine = (float*)smem + wave * SR * PITCH;
+// fp32 on the bf16 matrix cores, which are sixteen times as fast: every value is
+// the sum of three bf16 planes of eight of its bits each (cut off one after the
+// other, exactly; below 2^-110 the last bits are lost), and six of the nine products
+// of planes are added, the smallest first.  What is left out is below 2^-23 of a
+// product's magnitude.  An infinity comes out as NaN.  The planes are made on the way
+// to LDS: K steps of 32 values through registers and two buffers.
+template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM * WN, 2) void plane_kernel(const LinearParams p)
+{
+    constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, KT = 32;
+    constexpr int ROWS = BM + BN, LOADS = ROWS * kChunks / T, PLANE = ROWS * 64, BUF = 3 * PLANE;
+    constexpr int OUT = WM * WN * out_bytes<MI, NI>(), LDS = 2 * BUF > OUT ? 2 * BUF : OUT;
+    static_assert(ROWS * kChunks % T == 0);
+    __shared__ __align__(16) unsigned char smem[LDS];
+    __shared__ int some;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
+    const TileAt<BM, BN> at(p);
+    if (tid == 0) some = 0;
+    __syncthreads();
+    const char* row[LOADS];
+    if (operand_rows<BM, BN, WN, T, 4>(p, at, row)) some = 1;
+    __syncthreads();
+    if (!some) return;
+
+    const int steps = (p.K + KT - 1) / KT;
+    const int s0 = (int)((int64_t)steps * at.split / p.splits), s1 = (int)((int64_t)steps * (at.split + 1) / p.splits);
+    u32x4 stage[LOADS];
+    auto fetch = [&](int s) {
 #pragma unroll
-    for (int c = 0; c < MI; c += SR / 16) {
+        for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<false>(row[c], s * KT + 4 * (tid % kChunks), p.K);
+    };
+    // (chunks of eight values, their index XORed with bits of the row: the sixteen rows of a read lie in different banks)
+    auto keep = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < SR / 16; i++)
+        for (int c = 0; c < LOADS; c++) {
+            const int r = tid / kChunks + c * (T / kChunks);
+            unsigned char* to = smem + buf * BUF + r * 64 + ((tid % kChunks / 2) ^ ((r >> 2) & 3)) * 16 + tid % 2 * 8;
+            uint32_t y[4];
 #pragma unroll
-            for (int j = 0; j < NI; j++) *(f32x4*)(mine + (16 * i + l16) * PITCH + 16 * j + 4 * g) = acc[c + i][j];
-        // (the wave's own region: its LDS operations complete in order)
-        __builtin_amdgcn_wave_barrier();
-        finish<COLS>(p, mine, SR, PITCH, m0 + wm * (BM / WM) + 16 * c, n0 + wn * (p.glu ? COLS / 2 : COLS), split);
-        __builtin_amdgcn_wave_barrier();
+            for (int j = 0; j < 4; j++) y[j] = stage[c][j];
+#pragma unroll
+            for (int q = 0; q < 3; q++) {
+                *(u32x2*)(to + q * PLANE) = u32x2{__builtin_amdgcn_perm(y[1], y[0], 0x07060302u), __builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
+#pragma unroll
+                for (int j = 0; j < 4; j++) y[j] = __float_as_uint(__uint_as_float(y[j]) - __uint_as_float(y[j] & 0xffff0000u));
+            }
+        }
+    };
+
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+    const int ch = l16 * 64 + (g ^ ((l16 >> 2) & 3)) * 16;
+    const unsigned char *xl = smem + wm * (BM / WM) * 64 + ch, *wl = smem + (BM + wn * (BN / WN)) * 64 + ch;
+
+    if (s0 < s1) {
+        fetch(s0);
+        keep(0);
+        if (s0 + 1 < s1) fetch(s0 + 1);
+        __syncthreads();
+        for (int s = s0, buf = 0; s < s1; s++, buf ^= 1) {
+            u32x4 w[3][NI];
+#pragma unroll
+            for (int q = 0; q < 3; q++)
+#pragma unroll
+                for (int j = 0; j < NI; j++) w[q][j] = *(const u32x4*)(wl + buf * BUF + q * PLANE + j * 1024);
+#pragma unroll
+            for (int i = 0; i < MI; i++) {
+                u32x4 x[3];
+#pragma unroll
+                for (int q = 0; q < 3; q++) x[q] = *(const u32x4*)(xl + buf * BUF + q * PLANE + i * 1024);
+#pragma unroll
+                for (int t = 0; t < 6; t++) {
+                    constexpr int kw[6] = {2, 0, 1, 1, 0, 0}, kx[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+                    for (int j = 0; j < NI; j++) acc[i][j] = mma<true>(w[kw[t]][j], x[kx[t]], acc[i][j]);
+                }
+            }
+            if (s + 1 < s1) keep(buf ^ 1);
+            if (s + 2 < s1) fetch(s + 2);
+            __syncthreads();
+        }
     }
+    __syncthreads();
+    write_out<MI, NI>(p, (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
+                      at.n0 + wn * (p.glu ? BN / WN / 2 : BN / WN), at.split);
 }
 
 // ------------------------------------------------------------- few rows
@@ -436,7 +569,18 @@ __global__ __launch_bounds__(256) void join_kernel(const LinearParams p)
 
 // ------------------------------------------------------------------ choice
 
-enum { kFew, kTile64, kTile128, kTile256 };
+// Rows and columns of a block.
+struct Shape {
+    int bm, bn;
+};
+enum { kFew, kTile64, kTile128, kTile256, kPlane64, kPlane128, kPlane256 };
+constexpr Shape kShapes[] = {{0, 0}, {64, 64}, {128, 128}, {256, 256}, {64, 64}, {128, 128}, {256, 128}};
+
+static int64_t tiles(int kind, int64_t M, int64_t cols)
+{
+    const Shape s = kShapes[kind];
+    return ((M + s.bm - 1) / s.bm) * ((cols + s.bn - 1) / s.bn);
+}
 
 LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
 {
@@ -448,44 +592,51 @@ LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
         const int64_t blocks = (cols + 16 * nt - 1) / (16 * nt);
         while (blocks * pl.splits < 256 && steps >= 16 * pl.splits && pl.splits < 16) pl.splits *= 2;
     } else {
-        auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((cols + b - 1) / b); };
-        pl.kind = tiles(256) >= 192 ? kTile256 : tiles(128) >= 192 ? kTile128 : kTile64;
-        const int64_t blocks = tiles(pl.kind == kTile256 ? 256 : pl.kind == kTile128 ? 128 : 64);
+        const int small = bf16 ? kTile64 : kPlane64;
+        pl.kind = tiles(small + 2, M, cols) >= 192 ? small + 2 : tiles(small + 1, M, cols) >= 192 ? small + 1 : small;
+        const int64_t blocks = tiles(pl.kind, M, cols);
         while (blocks * pl.splits < 192 && steps >= 8 * pl.splits && pl.splits < 8) pl.splits *= 2;
     }
     if (pl.splits > 1) pl.ws_bytes = pl.splits * M * part_row(N, glu) * 4;
     return pl;
 }
 
-template <bool BF16> hipError_t launch_linear_t(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
+template <bool BF16> hipError_t launch_few(const LinearParams& p, hipStream_t st)
 {
-    hipError_t e = hipErrorInvalidValue;
-    if (plan.kind == kFew) {
-        const int nt = p.glu || p.M > 32 ? 2 : 1, bc = p.glu ? 16 : 16 * nt;
-        const int64_t blocks = (int64_t)((p.N + bc - 1) / bc) * p.splits;
+    const int nt = p.glu || p.M > 32 ? 2 : 1, bc = p.glu ? 16 : 16 * nt;
+    const int64_t blocks = (int64_t)((p.N + bc - 1) / bc) * p.splits;
 #define DCB_FEW(MB, NT) (p.wide ? launch_with(few_kernel<BF16, MB, NT, true>, blocks, 256, 0, st, p) : launch_with(few_kernel<BF16, MB, NT, false>, blocks, 256, 0, st, p))
-        if (nt == 1) e = p.M <= 16 ? DCB_FEW(1, 1) : DCB_FEW(2, 1);
-        else e = p.M <= 16 ? DCB_FEW(1, 2) : p.M <= 32 ? DCB_FEW(2, 2) : DCB_FEW(4, 2);
+    if (nt == 1) return p.M <= 16 ? DCB_FEW(1, 1) : DCB_FEW(2, 1);
+    return p.M <= 16 ? DCB_FEW(1, 2) : p.M <= 32 ? DCB_FEW(2, 2) : DCB_FEW(4, 2);
 #undef DCB_FEW
-    } else {
-        const int b = plan.kind == kTile64 ? 64 : plan.kind == kTile128 ? 128 : 256;
-        auto blocks = [&](int b) {
-            const int bc = p.glu ? b / 2 : b;
-            return (int64_t)((p.M + b - 1) / b) * ((p.N + bc - 1) / bc) * p.splits;
-        };
-        if (b == 64) e = p.wide ? launch_with(tile_kernel<BF16, 64, 64, 2, 2, true>, blocks(64), 256, 0, st, p)
-                                : launch_with(tile_kernel<BF16, 64, 64, 2, 2, false>, blocks(64), 256, 0, st, p);
-        else if (b == 256 && p.wide) e = launch_with(tile_kernel<BF16, 256, 256, 2, 4, true>, blocks(256), 512, 0, st, p);
-        else e = p.wide ? launch_with(tile_kernel<BF16, 128, 128, 2, 2, true>, blocks(128), 256, 0, st, p)
-                        : launch_with(tile_kernel<BF16, 128, 128, 2, 2, false>, blocks(128), 256, 0, st, p);
+}
+
+static hipError_t launch_tiles(const LinearParams& p, int kind, hipStream_t st)
+{
+    // (256 x 256 has no variant for rows that are not of whole chunks)
+    if (kind == kTile256 && !p.wide) kind = kTile128;
+    const int bm = kShapes[kind].bm, bc = p.glu ? kShapes[kind].bn / 2 : kShapes[kind].bn;
+    const int64_t blocks = (int64_t)((p.M + bm - 1) / bm) * ((p.N + bc - 1) / bc) * p.splits;
+    switch (kind) {
+    case kTile64:
+        return p.wide ? launch_with(tile_kernel<true, 64, 64, 2, 2, true, 4>, blocks, 256, 0, st, p)
+                      : launch_with(tile_kernel<true, 64, 64, 2, 2, false, 2>, blocks, 256, 0, st, p);
+    case kTile128:
+        return p.wide ? launch_with(tile_kernel<true, 128, 128, 2, 2, true, 2>, blocks, 256, 0, st, p)
+                      : launch_with(tile_kernel<true, 128, 128, 2, 2, false, 2>, blocks, 256, 0, st, p);
+    case kTile256: return launch_with(tile_kernel<true, 256, 256, 2, 4, true, 2>, blocks, 512, 0, st, p);
+    case kPlane64: return launch_with(plane_kernel<64, 64, 2, 2>, blocks, 256, 0, st, p);
+    case kPlane128: return launch_with(plane_kernel<128, 128, 2, 4>, blocks, 512, 0, st, p);
+    case kPlane256: return launch_with(plane_kernel<256, 128, 4, 2>, blocks, 512, 0, st, p);
     }
-    if (e != hipSuccess || p.splits == 1) return e;
-    return launch_with(join_kernel, ((int64_t)(part_half(p.N) / 8) * p.M + 255) / 256, 256, 0, st, p);
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
 {
-    return p.bf16 ? launch_linear_t<true>(p, plan, st) : launch_linear_t<false>(p, plan, st);
+    const hipError_t e = plan.kind != kFew ? launch_tiles(p, plan.kind, st) : p.bf16 ? launch_few<true>(p, st) : launch_few<false>(p, st);
+    if (e != hipSuccess || p.splits == 1) return e;
+    return launch_with(join_kernel, ((int64_t)(part_half(p.N) / 8) * p.M + 255) / 256, 256, 0, st, p);
 }
 
 }  // namespace dcb
