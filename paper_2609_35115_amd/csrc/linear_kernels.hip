@@ -1,6 +1,7 @@
 // gfx950 kernels of the matrix product with an epilogue:
 //   out = residual_scale residual + gate act(x W^T + bias).
 #include <algorithm>
+#include <type_traits>
 
 #include "block_internal.h"
 #include "dc_flow.h"
@@ -43,6 +44,18 @@ template <bool BF16> __device__ __forceinline__ u32x4 load_chunk(const void* row
     return c;
 }
 
+// Chunks at element k of several rows, `whole` (uniform) where none passes its row's end.
+template <bool BF16, int N> __device__ __forceinline__ void load_chunks(const char* const (&row)[N], int k, int K, bool whole, u32x4 (&to)[N])
+{
+    if (whole) {
+#pragma unroll
+        for (int c = 0; c < N; c++) to[c] = *(const u32x4_any*)(row[c] + (int64_t)k * (BF16 ? 2 : 4));
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; c++) to[c] = load_chunk<BF16>(row[c], k, K);
+    }
+}
+
 // GELU in its tanh form, 0.5 v (1 + tanh z) = v / (1 + e^-2z): no cancellation for
 // negative v.
 template <bool EXACT> __device__ __forceinline__ float activate(float v, int act)
@@ -54,17 +67,16 @@ template <bool EXACT> __device__ __forceinline__ float activate(float v, int act
     return EXACT ? v / d : v * __builtin_amdgcn_rcpf(d);   // 1 ulp, of a result that is rounded to bf16 next
 }
 
+// Token i of entry e that row m of the call is; i < 0 where the call does not have it.
 struct Place {
     int e, i;
-    bool on;
-    __device__ __forceinline__ Place(const LinearParams& p, int m)
-    {
-        const int mm = min(m, p.M - 1);
-        e = mm / p.call.n;
-        i = mm - e * p.call.n;
-        on = m < p.M && i < p.call.len(e);
-    }
+    __device__ __forceinline__ bool on() const { return i >= 0; }
 };
+__device__ __forceinline__ Place place_of(const LinearParams& p, int m)
+{
+    const int e = min(m, p.M - 1) / p.call.n, i = m - e * p.call.n;
+    return Place{e, m < p.M && i < p.call.len(e) ? i : -1};
+}
 
 // Columns n .. n + 7 of a row, from the sums a (and b, the factor's, with glu),
 // biases ba, bb.
@@ -90,9 +102,9 @@ __device__ __forceinline__ Eight load_bias(const LinearParams& p, int n, int par
 }
 __device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at, int n, Eight a, Eight b, const Eight& ba, const Eight& bb)
 {
-    if (!at.on || n >= p.N) return;
-    const int64_t o = at.e * p.out.sb + at.i * p.out.st + n;
-    const int64_t g = at.e * p.gate.sb + at.i * p.gate.st + n, r = at.e * p.res.sb + at.i * p.res.st + n;
+    if (!at.on() || n >= p.N) return;
+    auto row = [&](const Rows& x) { return at.e * x.sb + at.i * x.st + n; };
+    const int64_t o = row(p.out);
     const bool full = n + 8 <= p.N;
 #pragma unroll
     for (int k = 0; k < 8; k++) a.v[k] += ba.v[k];
@@ -111,12 +123,12 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at,
     }
     if (full) {
         if (p.gate.p) {
-            const Eight x = load8(p.gate.p, g, p.gate.bf16);
+            const Eight x = load8(p.gate.p, row(p.gate), p.gate.bf16);
 #pragma unroll
             for (int k = 0; k < 8; k++) a.v[k] *= x.v[k];
         }
         if (p.res.p) {
-            const Eight x = load8(p.res.p, r, p.res.bf16);
+            const Eight x = load8(p.res.p, row(p.res), p.res.bf16);
 #pragma unroll
             for (int k = 0; k < 8; k++) a.v[k] = fmaf(p.res_scale, x.v[k], a.v[k]);
         }
@@ -128,8 +140,8 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at,
     for (int k = 0; k < 7; k++) {
         if (n + k >= p.N) break;
         float v = a.v[k];
-        if (p.gate.p) v *= load1(p.gate.p, g + k, p.gate.bf16);
-        if (p.res.p) v = fmaf(p.res_scale, load1(p.res.p, r + k, p.res.bf16), v);
+        if (p.gate.p) v *= load1(p.gate.p, row(p.gate) + k, p.gate.bf16);
+        if (p.res.p) v = fmaf(p.res_scale, load1(p.res.p, row(p.res) + k, p.res.bf16), v);
         store1(p.out.p, o + k, p.out.bf16, v);
     }
 }
@@ -139,15 +151,17 @@ __host__ __device__ inline int part_half(int N) { return (N + 7) / 8 * 8; }
 __host__ __device__ inline int64_t part_row(int N, int glu) { return (int64_t)part_half(N) * (glu ? 2 : 1); }
 
 // What a wave does with its `rows` rows of sums in LDS (`pitch` floats apart, with
-// glu the factors COLS / 2 floats behind): the epilogue, or a split's partial sums,
-// eight columns a lane and whole rows side by side.
-template <int COLS> __device__ __forceinline__ void finish(const LinearParams& p, const float* sums, int rows, int pitch, int m0, int n0, int split)
+// glu the factors COLS / 2 floats behind; `places` are the rows', m0 on): the
+// epilogue, or a split's partial sums, eight columns a lane and whole rows side by
+// side.
+template <int COLS>
+__device__ __forceinline__ void finish(const LinearParams& p, const Place* places, const float* sums, int rows, int pitch, int m0, int n0, int split)
 {
     const int lane = threadIdx.x & 63;
     const int per = p.glu ? COLS / 16 : COLS / 8;             // lanes of a row
     const int q = lane & (per - 1), n = n0 + 8 * q;
     const Eight ba = load_bias(p, n, 0), bb = p.glu ? load_bias(p, n, 1) : Eight{};
-#pragma unroll 1
+#pragma unroll 2
     for (int r = lane / per; r < rows; r += 64 / per) {
         const float* s = sums + r * pitch + 8 * q;
         auto eight = [](const float* s) {
@@ -166,7 +180,7 @@ template <int COLS> __device__ __forceinline__ void finish(const LinearParams& p
                 *(f32x4*)(to + 4) = f32x4{b.v[4], b.v[5], b.v[6], b.v[7]};
             }
         } else {
-            epilogue(p, Place(p, m0 + r), n, a, b, ba, bb);
+            epilogue(p, places[r], n, a, b, ba, bb);
         }
     }
 }
@@ -199,19 +213,22 @@ template <int BM, int BN> struct TileAt {
 // The operands' rows that a thread loads: its chunk of rows tid / 8 + c T / 8, first
 // the BM rows of x, then those of the weight.  Rows that the call does not have are
 // read from the weight instead and columns past N from its last row: their results
-// are not stored.  Whether any of them is a row of x that the call has.
+// are not stored.  `places` becomes the rows' places (every thread calls).  Whether
+// any of this thread's is a row of x that the call has.
 template <int BM, int BN, int WN, int T, int ES, int LOADS>
-__device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt<BM, BN>& at, const char* (&row)[LOADS])
+__device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt<BM, BN>& at, Place (&places)[BM], const char* (&row)[LOADS])
 {
     constexpr int NI = BN / WN / 16;
+    for (int m = threadIdx.x; m < BM; m += T) places[m] = place_of(p, at.m0 + m);
+    __syncthreads();
     bool any = false;
 #pragma unroll
     for (int c = 0; c < LOADS; c++) {
         const int rr = threadIdx.x / kChunks + c * (T / kChunks);
         if (rr < BM) {
-            const Place x(p, at.m0 + rr);
-            any |= x.on;
-            row[c] = x.on ? (const char*)p.x.p + (x.e * p.x.sb + x.i * p.x.st) * ES : (const char*)p.w;
+            const Place x = places[rr];
+            any |= x.on();
+            row[c] = x.on() ? (const char*)p.x.p + (x.e * p.x.sb + x.i * p.x.st) * ES : (const char*)p.w;
         } else {
             int r = rr - BM, col, part = 0;
             if (p.glu) {   // a wave's first half of 16-column groups, and the same columns' factors
@@ -232,7 +249,7 @@ __device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt
 template <int MI, int NI> constexpr int out_rows() { return MI < 4 ? 16 * MI : 64; }
 template <int MI, int NI> constexpr int out_bytes() { return out_rows<MI, NI>() * (16 * NI + 4) * 4; }
 template <int MI, int NI>
-__device__ __forceinline__ void write_out(const LinearParams& p, float* mine, const f32x4 (&acc)[MI][NI], int m0, int n0, int split)
+__device__ __forceinline__ void write_out(const LinearParams& p, const Place* places, float* mine, const f32x4 (&acc)[MI][NI], int m0, int n0, int split)
 {
     constexpr int SR = out_rows<MI, NI>(), PITCH = 16 * NI + 4;
     const int l16 = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
@@ -244,7 +261,7 @@ __device__ __forceinline__ void write_out(const LinearParams& p, float* mine, co
             for (int j = 0; j < NI; j++) *(f32x4*)(mine + (16 * i + l16) * PITCH + 16 * j + 4 * g) = acc[c + i][j];
         // (the wave's own region: its LDS operations complete in order)
         __builtin_amdgcn_wave_barrier();
-        finish<16 * NI>(p, mine, SR, PITCH, m0 + 16 * c, n0, split);
+        finish<16 * NI>(p, places + 16 * c, mine, SR, PITCH, m0 + 16 * c, n0, split);
         __builtin_amdgcn_wave_barrier();
     }
 }
@@ -266,14 +283,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
     static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0 && (WIDE || ST == 2));
     __shared__ __align__(16) unsigned char smem[LDS];
     __shared__ int some;
+    __shared__ Place places[BM];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
     const TileAt<BM, BN> at(p);
     if (tid == 0) some = 0;
-    __syncthreads();
     const char* row[LOADS];
-    if (operand_rows<BM, BN, WN, T, ES>(p, at, row)) some = 1;
+    if (operand_rows<BM, BN, WN, T, ES>(p, at, places, row)) some = 1;
     __syncthreads();
     if (!some) return;   // all rows are behind their entries' last tokens
 
@@ -281,7 +298,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
     const int steps = (p.K + KT - 1) / KT;
     const int s0 = (int)((int64_t)steps * at.split / p.splits), s1 = (int)((int64_t)steps * (at.split + 1) / p.splits);
 
-    u32x4 stage[WIDE ? 1 : LOADS];
+    u32x4 stage[LOADS];   // (not WIDE)
     __device__ static const u32x4 zeros = {0, 0, 0, 0};
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * 1024);
     auto fetch = [&](int s, int slot) {
@@ -291,8 +308,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
             for (int c = 0; c < LOADS; c++)
                 dma16(k < p.K ? row[c] + (int64_t)k * ES : (const char*)&zeros, lds0 + slot * BUF + c * (T * 16));
         } else {
-#pragma unroll
-            for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<BF16>(row[c], k, p.K);
+            load_chunks<BF16>(row, k, p.K, (s + 1) * KT <= p.K, stage);
         }
     };
     auto keep = [&](int slot) {
@@ -374,7 +390,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
         }
     }
     __syncthreads();
-    write_out<MI, NI>(p, (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
+    write_out<MI, NI>(p, places + wm * (BM / WM), (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
                       at.n0 + wn * (p.glu ? BN / WN / 2 : BN / WN), at.split);
 }
 
@@ -392,33 +408,33 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
     static_assert(ROWS * kChunks % T == 0);
     __shared__ __align__(16) unsigned char smem[LDS];
     __shared__ int some;
+    __shared__ Place places[BM];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
     const TileAt<BM, BN> at(p);
     if (tid == 0) some = 0;
-    __syncthreads();
     const char* row[LOADS];
-    if (operand_rows<BM, BN, WN, T, 4>(p, at, row)) some = 1;
+    if (operand_rows<BM, BN, WN, T, 4>(p, at, places, row)) some = 1;
     __syncthreads();
     if (!some) return;
 
     const int steps = (p.K + KT - 1) / KT;
     const int s0 = (int)((int64_t)steps * at.split / p.splits), s1 = (int)((int64_t)steps * (at.split + 1) / p.splits);
+    // loads of step s, and their way into a buffer
     u32x4 stage[LOADS];
-    auto fetch = [&](int s) {
-#pragma unroll
-        for (int c = 0; c < LOADS; c++) stage[c] = load_chunk<false>(row[c], s * KT + 4 * (tid % kChunks), p.K);
+    auto fetch = [&](int s, u32x4 (&to)[LOADS]) {
+        load_chunks<false>(row, s * KT + 4 * (tid % kChunks), p.K, (s + 1) * KT <= p.K, to);
     };
     // (chunks of eight values, their index XORed with bits of the row: the sixteen rows of a read lie in different banks)
-    auto keep = [&](int buf) {
+    auto keep = [&](const u32x4 (&from)[LOADS], int buf) {
 #pragma unroll
         for (int c = 0; c < LOADS; c++) {
             const int r = tid / kChunks + c * (T / kChunks);
             unsigned char* to = smem + buf * BUF + r * 64 + ((tid % kChunks / 2) ^ ((r >> 2) & 3)) * 16 + tid % 2 * 8;
             uint32_t y[4];
 #pragma unroll
-            for (int j = 0; j < 4; j++) y[j] = stage[c][j];
+            for (int j = 0; j < 4; j++) y[j] = from[c][j];
 #pragma unroll
             for (int q = 0; q < 3; q++) {
                 *(u32x2*)(to + q * PLANE) = u32x2{__builtin_amdgcn_perm(y[1], y[0], 0x07060302u), __builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
@@ -436,12 +452,20 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
     const int ch = l16 * 64 + (g ^ ((l16 >> 2) & 3)) * 16;
     const unsigned char *xl = smem + wm * (BM / WM) * 64 + ch, *wl = smem + (BM + wn * (BN / WN)) * 64 + ch;
 
+    // Of the two waves on a SIMD one makes the next step's planes before its products,
+    // the other after them: vector and matrix work side by side.
+    const bool ahead = T == 512 && wave >= 4;
     if (s0 < s1) {
-        fetch(s0);
-        keep(0);
-        if (s0 + 1 < s1) fetch(s0 + 1);
+        fetch(s0, stage);
+        keep(stage, 0);
+        if (s0 + 1 < s1) fetch(s0 + 1, stage);
         __syncthreads();
         for (int s = s0, buf = 0; s < s1; s++, buf ^= 1) {
+            auto next = [&]() {
+                if (s + 1 < s1) keep(stage, buf ^ 1);
+                if (s + 2 < s1) fetch(s + 2, stage);
+            };
+            if (ahead) next();
             u32x4 w[3][NI];
 #pragma unroll
             for (int q = 0; q < 3; q++)
@@ -459,13 +483,12 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
                     for (int j = 0; j < NI; j++) acc[i][j] = mma<true>(w[kw[t]][j], x[kx[t]], acc[i][j]);
                 }
             }
-            if (s + 1 < s1) keep(buf ^ 1);
-            if (s + 2 < s1) fetch(s + 2);
+            if (!ahead) next();
             __syncthreads();
         }
     }
     __syncthreads();
-    write_out<MI, NI>(p, (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
+    write_out<MI, NI>(p, places + wm * (BM / WM), (float*)(smem + wave * out_bytes<MI, NI>()), acc, at.m0 + wm * (BM / WM),
                       at.n0 + wn * (p.glu ? BN / WN / 2 : BN / WN), at.split);
 }
 
@@ -481,6 +504,7 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 {
     constexpr int CE = chunk_elems<BF16>(), ES = 16 / CE, U = 4, KG = 4 * CE;   // elements of a group of chunks
     __shared__ __align__(16) float sums[4][16 * MB * (16 * NT + 4)];
+    __shared__ Place places[16 * MB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
     const int BC = p.glu ? 16 : 16 * NT;
@@ -489,8 +513,9 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
     const char *xrow[MB], *wrow[NT];
 #pragma unroll
     for (int i = 0; i < MB; i++) {
-        const Place at(p, 16 * i + l16);
-        xrow[i] = at.on ? (const char*)p.x.p + (at.e * p.x.sb + at.i * p.x.st) * ES : (const char*)p.w;
+        const Place at = place_of(p, 16 * i + l16);
+        if (wave == 0 && g == 0) places[16 * i + l16] = at;
+        xrow[i] = at.on() ? (const char*)p.x.p + (at.e * p.x.sb + at.i * p.x.st) * ES : (const char*)p.w;
     }
 #pragma unroll
     for (int j = 0; j < NT; j++) {
@@ -540,7 +565,7 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
         *(f32x4*)(sums[0] + at) = v;
     }
     __syncthreads();
-    if (wave < MB) finish<COLS>(p, sums[0] + 16 * wave * PITCH, 16, PITCH, 16 * wave, n0, split);
+    if (wave < MB) finish<COLS>(p, places + 16 * wave, sums[0] + 16 * wave * PITCH, 16, PITCH, 16 * wave, n0, split);
 }
 
 // The splits' partial sums and the epilogue, eight columns a thread.
@@ -549,8 +574,8 @@ __global__ __launch_bounds__(256) void join_kernel(const LinearParams p)
     const int64_t eights = part_half(p.N) / 8, u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (u >= eights * p.M) return;
     const int m = (int)(u / eights), n = 8 * (int)(u % eights);
-    const Place at(p, m);
-    if (!at.on) return;
+    const Place at = place_of(p, m);
+    if (!at.on()) return;
     const int64_t row = part_row(p.N, p.glu);
     const float* s = p.ws + m * row + n;
     Eight a{}, b{};
