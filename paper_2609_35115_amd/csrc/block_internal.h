@@ -59,12 +59,7 @@ struct LinearParams {
     int splits;
     float* ws;         // splits > 1: [split][M][N or 2 N] partial sums
 };
-// The shape that a call takes and its splits of K.
-struct LinearPlan {
-    int kind, splits;
-    int64_t ws_bytes;
-};
-LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16);
+struct LinearPlan;   // linear_plan.h
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t st);
 
 // Rows of heads, as dc_head_rows.

@@ -7,6 +7,7 @@
 
 #include "block_internal.h"
 #include "dc_flow.h"
+#include "linear_plan.h"
 
 using namespace dcb;
 

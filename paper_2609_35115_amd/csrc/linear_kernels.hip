@@ -5,6 +5,7 @@
 
 #include "block_internal.h"
 #include "dc_flow.h"
+#include "linear_plan.h"
 
 namespace dcb {
 
@@ -146,14 +147,10 @@ __device__ __forceinline__ void epilogue(const LinearParams& p, const Place& at,
     }
 }
 
-// Partial sums of a split: [split][M][columns], a row's columns padded to eight.
-__host__ __device__ inline int part_half(int N) { return (N + 7) / 8 * 8; }
-__host__ __device__ inline int64_t part_row(int N, int glu) { return (int64_t)part_half(N) * (glu ? 2 : 1); }
-
 // What a wave does with its `rows` rows of sums in LDS (`pitch` floats apart, with
 // glu the factors COLS / 2 floats behind; `places` are the rows', m0 on): the
-// epilogue, or a split's partial sums, eight columns a lane and whole rows side by
-// side.
+// epilogue, or a split's partial sums ([split][M][part_row]), eight columns a lane
+// and whole rows side by side.
 template <int COLS>
 __device__ __forceinline__ void finish(const LinearParams& p, const Place* places, const float* sums, int rows, int pitch, int m0, int n0, int split)
 {
@@ -495,8 +492,8 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
 // ------------------------------------------------------------- few rows
 //
 // Calls of up to 16 MB rows: what counts is the weight's way from memory.  A block's
-// four waves share the K of NT sixteen-column groups (with glu one and its
-// factors) and all rows; weights and rows go from memory straight to the
+// four waves share the K of sixteen columns (NT = 2, with glu: and their factors)
+// and all rows; weights and rows go from memory straight to the
 // operand registers, U groups of four chunks at a time, and the waves' sums meet
 // in LDS.
 template <bool BF16, int MB, int NT, bool WIDE>
@@ -507,7 +504,7 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
     __shared__ Place places[16 * MB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
-    const int BC = p.glu ? 16 : 16 * NT;
+    constexpr int BC = 16;   // (NT = 2: with glu, their factors)
     const int split = blockIdx.x % p.splits, n0 = blockIdx.x / p.splits * BC;
 
     const char *xrow[MB], *wrow[NT];
@@ -519,15 +516,16 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
     }
 #pragma unroll
     for (int j = 0; j < NT; j++) {
-        const int part = p.glu ? j : 0, col = n0 + (p.glu ? 0 : 16 * j) + l16;
-        wrow[j] = (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
+        wrow[j] = (const char*)p.w + ((int64_t)j * p.N + min(n0 + l16, p.N - 1)) * p.wstride * ES;
     }
     const int groups = (p.K + KG - 1) / KG, parts = 4 * p.splits, part = 4 * split + wave;
     const int g0 = (int)((int64_t)groups * part / parts), g1 = (int)((int64_t)groups * (part + 1) / parts);
 
-    auto chunk = [&](const char* r, int k) {
+    // (`whole`, uniform: no lane's chunk passes the row's end)
+    auto chunk = [&](const char* r, int k, bool whole) {
         if constexpr (WIDE) return k < p.K ? *(const u32x4*)(r + (int64_t)k * ES) : u32x4{0, 0, 0, 0};
-        else return k < p.K ? load_chunk<BF16>(r, k, p.K) : u32x4{0, 0, 0, 0};
+        if (whole) return (u32x4) * (const u32x4_any*)(r + (int64_t)k * ES);
+        return k < p.K ? load_chunk<BF16>(r, k, p.K) : u32x4{0, 0, 0, 0};
     };
     f32x4 acc[MB][NT];
 #pragma unroll
@@ -536,13 +534,14 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
         for (int j = 0; j < NT; j++) acc[i][j] = f32x4{0, 0, 0, 0};
     for (int q = g0; q < g1; q += U) {
         u32x4 w[U][NT], x[U][MB];
+        const bool whole = q + U <= g1 && (q + U) * KG <= p.K;
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int k = q + u < g1 ? (q + u) * KG + g * CE : p.K;   // (past this wave's part: zeros)
 #pragma unroll
-            for (int j = 0; j < NT; j++) w[u][j] = chunk(wrow[j], k);
+            for (int j = 0; j < NT; j++) w[u][j] = chunk(wrow[j], k, whole);
 #pragma unroll
-            for (int i = 0; i < MB; i++) x[u][i] = chunk(xrow[i], k);
+            for (int i = 0; i < MB; i++) x[u][i] = chunk(xrow[i], k, whole);
         }
 #pragma unroll
         for (int u = 0; u < U; u++)
@@ -592,57 +591,26 @@ __global__ __launch_bounds__(256) void join_kernel(const LinearParams p)
     epilogue(p, at, n, a, b, load_bias(p, n, 0), p.glu ? load_bias(p, n, 1) : Eight{});
 }
 
-// ------------------------------------------------------------------ choice
+// ------------------------------------------------------------------ launch
 
-// Rows and columns of a block.
-struct Shape {
-    int bm, bn;
-};
-enum { kFew, kTile64, kTile128, kTile256, kPlane64, kPlane128, kPlane256 };
-constexpr Shape kShapes[] = {{0, 0}, {64, 64}, {128, 128}, {256, 256}, {64, 64}, {128, 128}, {256, 128}};
-
-static int64_t tiles(int kind, int64_t M, int64_t cols)
+template <bool BF16> hipError_t launch_few(const LinearParams& p, int kind, int64_t blocks, hipStream_t st)
 {
-    const Shape s = kShapes[kind];
-    return ((M + s.bm - 1) / s.bm) * ((cols + s.bn - 1) / s.bn);
-}
-
-LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
-{
-    LinearPlan pl{kFew, 1, 0};
-    const int64_t cols = (int64_t)N * (glu ? 2 : 1);
-    const int KT = bf16 ? 64 : 32, steps = (K + KT - 1) / KT;
-    if (M <= 64) {
-        const int nt = glu || M > 32 ? 2 : 1;
-        const int64_t blocks = (cols + 16 * nt - 1) / (16 * nt);
-        while (blocks * pl.splits < 256 && steps >= 16 * pl.splits && pl.splits < 16) pl.splits *= 2;
-    } else {
-        const int small = bf16 ? kTile64 : kPlane64;
-        pl.kind = tiles(small + 2, M, cols) >= 192 ? small + 2 : tiles(small + 1, M, cols) >= 192 ? small + 1 : small;
-        const int64_t blocks = tiles(pl.kind, M, cols);
-        while (blocks * pl.splits < 192 && steps >= 8 * pl.splits && pl.splits < 8) pl.splits *= 2;
-    }
-    if (pl.splits > 1) pl.ws_bytes = pl.splits * M * part_row(N, glu) * 4;
-    return pl;
-}
-
-template <bool BF16> hipError_t launch_few(const LinearParams& p, hipStream_t st)
-{
-    const int nt = p.glu || p.M > 32 ? 2 : 1, bc = p.glu ? 16 : 16 * nt;
-    const int64_t blocks = (int64_t)((p.N + bc - 1) / bc) * p.splits;
 #define DCB_FEW(MB, NT) (p.wide ? launch_with(few_kernel<BF16, MB, NT, true>, blocks, 256, 0, st, p) : launch_with(few_kernel<BF16, MB, NT, false>, blocks, 256, 0, st, p))
-    if (nt == 1) return p.M <= 16 ? DCB_FEW(1, 1) : DCB_FEW(2, 1);
-    return p.M <= 16 ? DCB_FEW(1, 2) : p.M <= 32 ? DCB_FEW(2, 2) : DCB_FEW(4, 2);
+    if (p.glu) return kind == kFew16 ? DCB_FEW(1, 2) : DCB_FEW(2, 2);
+    return kind == kFew16 ? DCB_FEW(1, 1) : DCB_FEW(2, 1);
 #undef DCB_FEW
 }
 
-static hipError_t launch_tiles(const LinearParams& p, int kind, hipStream_t st)
+static hipError_t launch_kind(const LinearParams& p, int kind, hipStream_t st)
 {
     // (256 x 256 has no variant for rows that are not of whole chunks)
     if (kind == kTile256 && !p.wide) kind = kTile128;
-    const int bm = kShapes[kind].bm, bc = p.glu ? kShapes[kind].bn / 2 : kShapes[kind].bn;
-    const int64_t blocks = (int64_t)((p.M + bm - 1) / bm) * ((p.N + bc - 1) / bc) * p.splits;
+    const LinearCost& c = kLinearCost[p.bf16 ? 1 : 0][kind];
+    const int bc = linear_columns(kind, c.bn, p.glu);
+    const int64_t blocks = (int64_t)((p.M + c.bm - 1) / c.bm) * ((p.N + bc - 1) / bc) * p.splits;
     switch (kind) {
+    case kFew16:
+    case kFew32: return p.bf16 ? launch_few<true>(p, kind, blocks, st) : launch_few<false>(p, kind, blocks, st);
     case kTile64:
         return p.wide ? launch_with(tile_kernel<true, 64, 64, 2, 2, true, 4>, blocks, 256, 0, st, p)
                       : launch_with(tile_kernel<true, 64, 64, 2, 2, false, 2>, blocks, 256, 0, st, p);
@@ -659,7 +627,7 @@ static hipError_t launch_tiles(const LinearParams& p, int kind, hipStream_t st)
 
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t st)
 {
-    const hipError_t e = plan.kind != kFew ? launch_tiles(p, plan.kind, st) : p.bf16 ? launch_few<true>(p, st) : launch_few<false>(p, st);
+    const hipError_t e = launch_kind(p, plan.kind, st);
     if (e != hipSuccess || p.splits == 1) return e;
     return launch_with(join_kernel, ((int64_t)(part_half(p.N) / 8) * p.M + 255) / 256, 256, 0, st, p);
 }
