@@ -1,5 +1,6 @@
 // gfx950 kernel of a block's norms: the residual add with the norm after a
 // sublayer and its gate, and the modulated norm before the next one.
+#include <algorithm>
 #include <type_traits>
 
 #include "block_internal.h"
@@ -7,70 +8,98 @@
 
 namespace dcb {
 
+// A factor or addend of every element of a row: (gate or 1 + scale) times gain, and
+// bias times the same plus shift.
+enum { kPostFactor, kPostAddend, kPreFactor, kPreAddend };
+
 // r = x_scale x + gate post(h), y = pre(r) (1 + scale) + shift.
 //
-// A thread holds NV vectors of eight consecutive elements of a row (vector
-// threadIdx + i * threads), so that the row is read once and both norms work on
-// registers.  Gains, biases and modulations are folded into two factors and two
-// addends per element (gate gain, gate bias, gain (1 + scale), bias (1 + scale) +
-// shift) and kept from row to row while they stay the same.  With ONE a wave has
-// a row to itself and no barrier; else a block of up to eight waves has.  The mean is
-// subtracted before squares are summed (two sums a LayerNorm): no cancellation.
-template <bool RB, bool HB, int NV, bool ONE>
-__global__ __launch_bounds__(ONE ? 256 : 512) void norm_kernel(const NormParams p)
+// A row's elements lie in NV vectors of eight consecutive ones a thread (vector
+// t + i threads), so that the row is read once and both norms work on registers.
+// LANES 0: a block of up to eight waves has a row; else LANES lanes of a wave have
+// one (64 / LANES rows a wave, side by side), and there is no barrier.  Blocks or
+// waves walk several rows, the next one loaded while this one is worked on.  Gains,
+// biases and modulations are folded into a factor and an addend of each norm.  With
+// KEEP they wait in LDS, written and read by the same thread, until the entry
+// changes (where a modulation depends on it); else (a modulation for each token, or
+// more than LDS holds) they are read at their use.  The mean is subtracted before
+// squares are summed: no cancellation.
+//
+// What bounds it: HBM.  16,384 rows of 4,096 bf16 (537 MB): see DCB_NORM_FIGURES.
+template <bool RB, bool HB, int NV, int LANES, bool KEEP>
+__global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParams p)
 {
-    __shared__ float part[4][8];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int t = ONE ? lane : threadIdx.x, threads = ONE ? 64 : blockDim.x;
+    constexpr bool ONE = LANES != 0;
+    constexpr int ROWS = ONE ? 64 / (ONE ? LANES : 1) : 1;   // rows side by side
+    extern __shared__ __align__(16) float kept[];            // [array][NV][half][threads][4]
+    __shared__ float part[2][8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int t = ONE ? lane % (ONE ? LANES : 1) : threadIdx.x, threads = ONE ? LANES : blockDim.x;
     const int C = p.width, full = C >> 3, rest = C & 7;
     int turn = 0;
     auto total = [&](float v) {
-        v = wave_sum(v);
-        if constexpr (!ONE) {   // (four buffers in turn: a wave is at most one sum ahead of another's reads)
-            float* s = part[turn++ & 3];
+        if constexpr (ONE) {
+            v = dpp_add<0xB1>(v);                             // quad_perm 1 0 3 2
+            v = dpp_add<0x4E>(v);                             // quad_perm 2 3 0 1
+            if constexpr (LANES >= 8) v = dpp_add<0x141>(v);   // row_half_mirror: the other quad of eight lanes
+            if constexpr (LANES >= 16) v = dpp_add<0x140>(v);  // row_mirror: the other eight of sixteen
+            if constexpr (LANES >= 32) v = sum_xor16(v);
+            if constexpr (LANES >= 64) v = sum_xor32(v);
+        } else {   // (two buffers in turn: a wave is at most one sum ahead of another's reads)
+            v = wave_sum(v);
+            float* s = part[turn++ & 1];
             if (lane == 0) s[wave] = v;
             __syncthreads();
-            v = s[0];
-            for (int w = 1; w < waves; w++) v += s[w];
+            const f32x4 a = *(const f32x4*)s, b = *(const f32x4*)(s + 4);
+            v = a[0];
+#pragma unroll
+            for (int w = 1; w < 8; w++)
+                if (w < waves) v += w < 4 ? a[w] : b[w - 4];
         }
         return v;
     };
 
-    int row = (ONE ? blockIdx.x * 4 + wave : blockIdx.x) * p.per;
-    const int end = min(row + p.per, p.rows);
-    if (row >= end) return;
-    int e = row / p.call.n, i = row - e * p.call.n, len = p.call.len(e);
+    const int walk = ONE ? blockIdx.x * 4 + wave : blockIdx.x;
+    const int side = ONE ? lane / (ONE ? LANES : 1) : 0;
+    int row = walk * p.per * ROWS + side;
+    const int end = min((walk + 1) * p.per * ROWS, p.rows);
+    int e = min(row, p.rows - 1) / p.call.n, i = row - e * p.call.n, len = p.call.len(e);
+    bool on = row < end && i < len;
 
     // a row's elements as they are stored
     Raw8<RB> xr[NV];
     Raw8<HB> hr[NV];
-    auto load = [&](int e, int i) {
-        const int64_t xa = e * p.x.sb + i * p.x.st, ha = e * p.h.sb + i * p.h.st;
+    auto load = [&](int e, int i, bool on) {
+        const int64_t xa = e * p.x.sb + i * p.x.st, ha = p.h.p ? e * p.h.sb + i * p.h.st : 0;
 #pragma unroll
         for (int v = 0; v < NV; v++) {
             const int u = t + v * threads;
-            if (u < full) {
+            xr[v] = Raw8<RB>{};
+            hr[v] = Raw8<HB>{};
+            if (on & (u < full)) {
                 xr[v] = load_raw<RB>(p.x.p, xa + 8 * u);
                 if (p.h.p) hr[v] = load_raw<HB>(p.h.p, ha + 8 * u);
-            } else if (u == full && rest) {
-                xr[v] = load_raw_part<RB>(p.x.p, xa + 8 * u, rest);
-                if (p.h.p) hr[v] = load_raw_part<HB>(p.h.p, ha + 8 * u, rest);
-            } else {
-                xr[v] = Raw8<RB>{};
-                hr[v] = Raw8<HB>{};
+            }
+        }
+        if (rest) {   // (one lane's, apart from the others' loads)
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int u = t + v * threads;
+                if (on & (u == full)) {
+                    xr[v] = load_raw_part<RB>(p.x.p, xa + 8 * u, rest);
+                    if (p.h.p) hr[v] = load_raw_part<HB>(p.h.p, ha + 8 * u, rest);
+                }
             }
         }
     };
 
-    float A[NV][8], B[NV][8], G[NV][8], T[NV][8];
-    // a vector of modulations or gains, `none` where there are none
-    auto vec = [&](const Rows& m, int e, int i, int u, float none, float (&o)[8]) {
+    // elements 8 u .. 8 u + 7 of a modulation or gain, `none` where there is none
+    auto vec = [&](const void* m, int64_t at, int bf16, int u, float none, float (&o)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; j++) o[j] = none;
-        if (!m.p || 8 * u >= C) return;
-        const int64_t at = e * m.sb + i * m.st + 8 * u;
+        if (!m || u > full) return;
         if (u < full) {
-            const f32x4 a = load4(m.p, at, m.bf16), b = load4(m.p, at + 4, m.bf16);
+            const f32x4 a = load4(m, at + 8 * u, bf16), b = load4(m, at + 8 * u + 4, bf16);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 o[j] = a[j];
@@ -79,42 +108,68 @@ __global__ __launch_bounds__(ONE ? 256 : 512) void norm_kernel(const NormParams 
         } else {
 #pragma unroll
             for (int j = 0; j < 7; j++)
-                if (j < rest) o[j] = load1(m.p, at + j, m.bf16);
+                if (j < rest) o[j] = load1(m, at + 8 * u + j, bf16);
         }
     };
-    auto factors = [&](int e, int i) {
+    // the factor or addend `which` of vector u of a row
+    auto fold = [&](int which, int e, int i, int u, float (&o)[8]) {
+        float a[8];
+        const Rows& m = which <= kPostAddend ? p.gate : p.scale;
+        const NormSpec& s = which <= kPostAddend ? p.post : p.pre;
+        vec(m.p, e * m.sb + i * m.st, m.bf16, u, which <= kPostAddend ? 1.0f : 0.0f, a);
+        if (which > kPostAddend) {
 #pragma unroll
-        for (int v = 0; v < NV; v++) {
-            const int u = t + v * threads;
-            float a[8], b[8], c[8];
-            if (p.h.p) {
-                vec(p.gate, e, i, u, 1.0f, a);
-                vec(Rows{(void*)p.post.gain, 0, 0, 0}, 0, 0, u, 1.0f, b);
-                vec(Rows{(void*)p.post.bias, 0, 0, 0}, 0, 0, u, 0.0f, c);
+            for (int j = 0; j < 8; j++) a[j] += 1.0f;
+        }
+        if (which == kPostFactor || which == kPreFactor) {
+            vec(s.gain, 0, 0, u, 1.0f, o);
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    A[v][j] = a[j] * b[j];
-                    B[v][j] = a[j] * c[j];
-                }
+            for (int j = 0; j < 8; j++) o[j] *= a[j];
+        } else {
+            vec(s.bias, 0, 0, u, 0.0f, o);
+            float b[8];
+            vec(which == kPreAddend ? p.shift.p : nullptr, e * p.shift.sb + i * p.shift.st, p.shift.bf16, u, 0.0f, b);
+#pragma unroll
+            for (int j = 0; j < 8; j++) o[j] = fmaf(o[j], a[j], b[j]);
+        }
+    };
+    const bool has[4] = {p.h.p && (p.gate.p || p.post.gain), p.h.p && p.post.bias, p.y.p && (p.scale.p || p.pre.gain),
+                         p.y.p && (p.pre.bias || p.shift.p)};
+    auto place = [&](int which, int v) {
+        const int array = which > 0 ? has[0] + (which > 1 ? has[1] + (which > 2 ? has[2] : 0) : 0) : 0;
+        return kept + ((array * NV + v) * 2 * (int)blockDim.x + (int)threadIdx.x) * 4;
+    };
+    auto keep = [&](int e) {
+#pragma unroll
+        for (int which = 0; which < 4; which++) {
+            if (!has[which]) continue;
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                float o[8];
+                fold(which, e, 0, t + v * threads, o);
+                float* to = place(which, v);
+                *(f32x4*)to = f32x4{o[0], o[1], o[2], o[3]};
+                *(f32x4*)(to + 4 * blockDim.x) = f32x4{o[4], o[5], o[6], o[7]};
             }
-            if (p.y.p) {
-                vec(p.scale, e, i, u, 0.0f, a);
-                vec(Rows{(void*)p.pre.gain, 0, 0, 0}, 0, 0, u, 1.0f, b);
-                vec(Rows{(void*)p.pre.bias, 0, 0, 0}, 0, 0, u, 0.0f, c);
-                float s[8];
-                vec(p.shift, e, i, u, 0.0f, s);
+        }
+    };
+    auto get = [&](int which, int e, int i, int v, float (&o)[8]) {
+        if constexpr (KEEP) {
+            const float* from = place(which, v);
+            const f32x4 a = *(const f32x4*)from, b = *(const f32x4*)(from + 4 * blockDim.x);
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    G[v][j] = b[j] * (1.0f + a[j]);
-                    T[v][j] = c[j] * (1.0f + a[j]) + s[j];
-                }
+            for (int j = 0; j < 4; j++) {
+                o[j] = a[j];
+                o[4 + j] = b[j];
             }
+        } else {
+            fold(which, e, i, t + v * threads, o);
         }
     };
 
-    // x less its mean (LayerNorm) times 1 / sqrt(mean square + eps), in place
+    // the factor 1 / sqrt(mean square + eps) of x, with DC_NORM_LAYER of x less its mean, which is taken from x here
     const float inv_c = 1.0f / (float)C;
-    auto norm = [&](const NormSpec& s, float (&x)[NV][8]) {
+    auto root = [&](const NormSpec& s, float (&x)[NV][8]) {
         if (s.kind == DC_NORM_LAYER) {
             float sum = 0.0f;
 #pragma unroll
@@ -125,82 +180,109 @@ __global__ __launch_bounds__(ONE ? 256 : 512) void norm_kernel(const NormParams 
 #pragma unroll
             for (int v = 0; v < NV; v++)
 #pragma unroll
-                for (int j = 0; j < 8; j++) x[v][j] = 8 * (t + v * threads) + j < C ? x[v][j] - mean : 0.0f;
+                for (int j = 0; j < 8; j++) x[v][j] -= 8 * (t + v * threads) + j < C ? mean : 0.0f;
         }
         float ss = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; v++)
 #pragma unroll
             for (int j = 0; j < 8; j++) ss = fmaf(x[v][j], x[v][j], ss);
-        const float f = __builtin_amdgcn_rsqf(total(ss) * inv_c + s.eps);   // 1 ulp
-#pragma unroll
-        for (int v = 0; v < NV; v++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) x[v][j] *= f;
+        return __builtin_amdgcn_rsqf(total(ss) * inv_c + s.eps);   // 1 ulp
     };
-    auto store = [&](const Rows& o, int e, int i, auto bf16, const float (&x)[NV][8]) {
-        const int64_t at = e * o.sb + i * o.st;
+    auto store = [&](const Rows& o, int64_t at, int v, auto bf16, const float (&x)[8]) {
+        const int u = t + v * threads;
+        if (u < full) {
+            store8<decltype(bf16)::value>(o.p, at + 8 * u, x);
+        } else if (u == full && rest) {
 #pragma unroll
-        for (int v = 0; v < NV; v++) {
-            const int u = t + v * threads;
-            if (u < full) {
-                store8<decltype(bf16)::value>(o.p, at + 8 * u, x[v]);
-            } else if (u == full) {
-#pragma unroll
-                for (int j = 0; j < 7; j++)
-                    if (j < rest) store1(o.p, at + 8 * u + j, decltype(bf16)::value, x[v][j]);
-            }
+            for (int j = 0; j < 7; j++)
+                if (j < rest) store1(o.p, at + 8 * u + j, decltype(bf16)::value, x[j]);
         }
     };
 
-    const bool by_token = (p.gate.p && p.gate.st) || (p.scale.p && p.scale.st) || (p.shift.p && p.shift.st);
     const bool by_entry = (p.gate.p && p.gate.sb) || (p.scale.p && p.scale.sb) || (p.shift.p && p.shift.sb);
-    bool stale = true;
-    if (i < len) load(e, i);
-    while (true) {
+    int kept_of = -1;   // the entry whose factors are kept
+    load(e, i, on);
+    for (int it = 0; it < p.per; it++) {
         // the next row's place; rows behind an entry's last token are passed over
-        int nr = row + 1, ne = e, ni = i + 1, nlen = len;
+        const int nr = row + ROWS;
+        int ne = e, ni = i + ROWS, nlen = len;
         if (ni >= p.call.n) {
-            ne = e + 1;
-            ni = 0;
-            nlen = nr < end ? p.call.len(ne) : 0;
+            ne = min(nr, p.rows - 1) / p.call.n;
+            ni = nr - ne * p.call.n;
+            nlen = p.call.len(ne);
         }
-        if (i < len) {
-            float x[NV][8], h[NV][8];
+        const bool non = (nr < end) & (ni < nlen) & (it + 1 < p.per);
+
+        float x[NV][8], h[NV][8];
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            widen<RB>(xr[v], x[v]);
+            widen<HB>(hr[v], h[v]);
+        }
+        if (KEEP && on && (kept_of < 0 || (by_entry && kept_of != e))) {
+            keep(e);
+            kept_of = e;
+        }
+        if (ONE || non) load(ne, ni, non);
+        if (ONE || on) {   // (a block's row is on for all of its threads)
+            float f = 1.0f;
+            if (p.h.p && p.post.kind) f = root(p.post, h);
 #pragma unroll
             for (int v = 0; v < NV; v++) {
-                widen<RB>(xr[v], x[v]);
-                widen<HB>(hr[v], h[v]);
-            }
-            if (stale || by_token) factors(e, i);
-            stale = false;
-            if (nr < end && ni < nlen) load(ne, ni);
-            if (p.h.p && p.post.kind) norm(p.post, h);
 #pragma unroll
-            for (int v = 0; v < NV; v++)
+                for (int j = 0; j < 8; j++) x[v][j] *= p.x_scale;
+                if (p.h.p) {
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    x[v][j] *= p.x_scale;
-                    if (p.h.p) x[v][j] = 8 * (t + v * threads) + j < C ? x[v][j] + fmaf(h[v][j], A[v][j], B[v][j]) : 0.0f;
+                    for (int j = 0; j < 8; j++) h[v][j] *= f;
+                    float o[8];
+                    if (has[kPostFactor]) {
+                        get(kPostFactor, e, i, v, o);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) h[v][j] *= o[j];
+                    }
+                    if (has[kPostAddend]) {
+                        get(kPostAddend, e, i, v, o);   // (of elements past the row's last: zeros)
+#pragma unroll
+                        for (int j = 0; j < 8; j++) h[v][j] += o[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; j++) x[v][j] += h[v][j];
                 }
-            if (p.r.p) store(p.r, e, i, std::integral_constant<bool, RB>{}, x);
-            if (p.y.p) {
-                if (p.pre.kind) norm(p.pre, x);
-#pragma unroll
-                for (int v = 0; v < NV; v++)
-#pragma unroll
-                    for (int j = 0; j < 8; j++) x[v][j] = fmaf(x[v][j], G[v][j], T[v][j]);
-                store(p.y, e, i, std::integral_constant<bool, HB>{}, x);
             }
-        } else if (nr < end && ni < nlen) {
-            load(ne, ni);
+            if (p.r.p && on) {
+                const int64_t at = e * p.r.sb + i * p.r.st;
+#pragma unroll
+                for (int v = 0; v < NV; v++) store(p.r, at, v, std::integral_constant<bool, RB>{}, x[v]);
+            }
+            if (p.y.p) {
+                f = 1.0f;
+                if (p.pre.kind) f = root(p.pre, x);
+                const int64_t at = e * p.y.sb + i * p.y.st;
+#pragma unroll
+                for (int v = 0; v < NV; v++) {
+                    float o[8];
+#pragma unroll
+                    for (int j = 0; j < 8; j++) x[v][j] *= f;
+                    if (has[kPreFactor]) {
+                        get(kPreFactor, e, i, v, o);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) x[v][j] *= o[j];
+                    }
+                    if (has[kPreAddend]) {
+                        get(kPreAddend, e, i, v, o);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) x[v][j] += o[j];
+                    }
+                    if (on) store(p.y, at, v, std::integral_constant<bool, HB>{}, x[v]);
+                }
+            }
         }
-        if (nr >= end) break;
-        stale |= ne != e && by_entry;
         row = nr;
         e = ne;
         i = ni;
         len = nlen;
+        on = non;
     }
 }
 
@@ -208,15 +290,25 @@ template <bool RB, bool HB> hipError_t launch_norm_t(NormParams p, hipStream_t s
 {
     const int vecs = (p.width + 7) / 8;
     const bool one = vecs <= 128;
+    const int lanes = vecs <= 8 ? 8 : vecs <= 16 ? 16 : vecs <= 32 ? 32 : 64;
     const int nv = one ? (vecs <= 64 ? 1 : 2) : vecs <= 256 ? 1 : vecs <= 1024 ? 2 : 4;
     const int waves = one ? 4 : (vecs + 64 * nv - 1) / (64 * nv);
-    const int64_t want = 256 * 8;   // blocks that fill the card
-    const int64_t units = one ? want * 4 : want;
-    p.per = (int)((p.rows + units - 1) / units);
-    const int64_t walks = (p.rows + p.per - 1) / p.per, blocks = one ? (walks + 3) / 4 : walks;
-#define DCB_NORM(NV, ONE) launch_with(norm_kernel<RB, HB, NV, ONE>, blocks, 64 * waves, 0, st, p)
-    if (one) return nv == 1 ? DCB_NORM(1, true) : DCB_NORM(2, true);
-    return nv == 1 ? DCB_NORM(1, false) : nv == 2 ? DCB_NORM(2, false) : DCB_NORM(4, false);
+    const int arrays = (p.h.p && (p.gate.p || p.post.gain)) + (p.h.p && p.post.bias) + (p.y.p && (p.scale.p || p.pre.gain)) +
+                       (p.y.p && (p.pre.bias || p.shift.p));
+    const int lds = arrays * nv * 32 * 64 * waves;
+    const bool by_token = (p.gate.p && p.gate.st) || (p.scale.p && p.scale.st) || (p.shift.p && p.shift.st);
+    const bool keep = !by_token && lds <= 64 * 1024;
+    // rows of a walk: as few as give every CU eight blocks of walks
+    const int64_t sides = one ? 64 / lanes : 1, units = (p.rows + sides - 1) / sides;
+    const int64_t want = one ? 256 * 8 * 4 : 256 * 8;
+    p.per = (int)((units + want - 1) / want);
+    const int64_t walks = (units + p.per - 1) / p.per, blocks = one ? (walks + 3) / 4 : walks;
+#define DCB_NORM(NV, LANES)                                                                          \
+    (keep ? launch_with(norm_kernel<RB, HB, NV, LANES, true>, blocks, 64 * waves, lds, st, p)         \
+          : launch_with(norm_kernel<RB, HB, NV, LANES, false>, blocks, 64 * waves, 0, st, p))
+    if (!one) return nv == 1 ? DCB_NORM(1, 0) : nv == 2 ? DCB_NORM(2, 0) : DCB_NORM(4, 0);
+    if (nv == 2) return DCB_NORM(2, 64);
+    return lanes == 8 ? DCB_NORM(1, 8) : lanes == 16 ? DCB_NORM(1, 16) : lanes == 32 ? DCB_NORM(1, 32) : DCB_NORM(1, 64);
 #undef DCB_NORM
 }
 
