@@ -16,6 +16,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 // (global memory takes vectors at any element's alignment)
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+typedef uint32_t __attribute__((aligned(2))) u32_any;
 
 // Rows of tokens: token i of entry e at p + e sb + i st, in elements (p null: none).
 struct Rows {
@@ -167,17 +168,66 @@ template <bool BF16> __device__ __forceinline__ void widen(const Raw8<BF16>& r, 
         }
     }
 }
-// The first m (< 8) of eight elements, zeros behind them.
-template <bool BF16> __device__ __forceinline__ Raw8<BF16> load_raw_part(const void* p, int64_t at, int m)
+// The first m (1 to 7, uniform) of eight elements, zeros behind them: four, two and
+// one at a time, straight to where they belong.
+template <bool BF16, int M> __device__ __forceinline__ Raw8<BF16> load_raw_m(const void* p, int64_t at)
 {
+    constexpr int two = M & 4, one = M & 6;   // where the pair and the last one begin
     Raw8<BF16> r{};
-#pragma unroll
-    for (int j = 0; j < 7; j++) {
-        if (j >= m) break;
-        if constexpr (BF16) r.w[0][j >> 1] |= (uint32_t)((const uint16_t*)p)[at + j] << (16 * (j & 1));
-        else r.w[j >> 2][j & 3] = ((const uint32_t*)p)[at + j];
+    if constexpr (BF16) {
+        const uint16_t* s = (const uint16_t*)p + at;
+        if constexpr (M & 4) {
+            const u32x2 x = *(const u32x2_any*)s;
+            r.w[0][0] = x[0];
+            r.w[0][1] = x[1];
+        }
+        if constexpr (M & 2) r.w[0][two / 2] = *(const u32_any*)(s + two);
+        if constexpr (M & 1) r.w[0][one / 2] = s[one];
+    } else {
+        const uint32_t* s = (const uint32_t*)p + at;
+        if constexpr (M & 4) r.w[0] = *(const u32x4_any*)s;
+        if constexpr (M & 2) {
+            const u32x2 x = *(const u32x2_any*)(s + two);
+            r.w[two / 4][0] = x[0];
+            r.w[two / 4][1] = x[1];
+        }
+        if constexpr (M & 1) r.w[one / 4][one % 4] = s[one];
     }
     return r;
+}
+template <bool BF16> __device__ __forceinline__ Raw8<BF16> load_raw_part(const void* p, int64_t at, int m)
+{
+    switch (m) {
+    case 1: return load_raw_m<BF16, 1>(p, at);
+    case 2: return load_raw_m<BF16, 2>(p, at);
+    case 3: return load_raw_m<BF16, 3>(p, at);
+    case 4: return load_raw_m<BF16, 4>(p, at);
+    case 5: return load_raw_m<BF16, 5>(p, at);
+    case 6: return load_raw_m<BF16, 6>(p, at);
+    default: return load_raw_m<BF16, 7>(p, at);
+    }
+}
+template <bool BF16, int M> __device__ __forceinline__ void store_m(void* p, int64_t at, const float (&x)[8])
+{
+    constexpr int two = M & 4, one = M & 6;
+    if constexpr (M & 4) store4(p, at, BF16, f32x4{x[0], x[1], x[2], x[3]});
+    if constexpr (M & 2) {
+        if constexpr (BF16) *(u32_any*)((uint16_t*)p + at + two) = pack2(x[two], x[two + 1]);
+        else *(u32x2_any*)((float*)p + at + two) = u32x2{__float_as_uint(x[two]), __float_as_uint(x[two + 1])};
+    }
+    if constexpr (M & 1) store1(p, at + one, BF16, x[one]);
+}
+template <bool BF16> __device__ __forceinline__ void store_part(void* p, int64_t at, int m, const float (&x)[8])
+{
+    switch (m) {
+    case 1: return store_m<BF16, 1>(p, at, x);
+    case 2: return store_m<BF16, 2>(p, at, x);
+    case 3: return store_m<BF16, 3>(p, at, x);
+    case 4: return store_m<BF16, 4>(p, at, x);
+    case 5: return store_m<BF16, 5>(p, at, x);
+    case 6: return store_m<BF16, 6>(p, at, x);
+    default: return store_m<BF16, 7>(p, at, x);
+    }
 }
 template <bool BF16> __device__ __forceinline__ void store8(void* p, int64_t at, const float (&x)[8])
 {

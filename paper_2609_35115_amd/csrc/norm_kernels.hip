@@ -97,7 +97,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     auto vec = [&](const void* m, int64_t at, int bf16, int u, float none, float (&o)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; j++) o[j] = none;
-        if (!m || u > full) return;
+        if (!m || u > full || (u == full && !rest)) return;
         if (u < full) {
             const f32x4 a = load4(m, at + 8 * u, bf16), b = load4(m, at + 8 * u + 4, bf16);
 #pragma unroll
@@ -106,9 +106,8 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
                 o[4 + j] = b[j];
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 7; j++)
-                if (j < rest) o[j] = load1(m, at + 8 * u + j, bf16);
+            if (bf16) widen<true>(load_raw_part<true>(m, at + 8 * u, rest), o);
+            else widen<false>(load_raw_part<false>(m, at + 8 * u, rest), o);
         }
     };
     // the factor or addend `which` of vector u of a row
@@ -194,9 +193,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
         if (u < full) {
             store8<decltype(bf16)::value>(o.p, at + 8 * u, x);
         } else if (u == full && rest) {
-#pragma unroll
-            for (int j = 0; j < 7; j++)
-                if (j < rest) store1(o.p, at + 8 * u + j, decltype(bf16)::value, x[j]);
+            store_part<decltype(bf16)::value>(o.p, at + 8 * u, rest, x);
         }
     };
 
@@ -226,6 +223,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
         }
         if (ONE || non) load(ne, ni, non);
         if (ONE || on) {   // (a block's row is on for all of its threads)
+            const int mi = on ? i : 0;   // whose modulations are read: a lane group without a row may stand past the last token
             float f = 1.0f;
             if (p.h.p && p.post.kind) f = root(p.post, h);
 #pragma unroll
@@ -237,12 +235,12 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
                     for (int j = 0; j < 8; j++) h[v][j] *= f;
                     float o[8];
                     if (has[kPostFactor]) {
-                        get(kPostFactor, e, i, v, o);
+                        get(kPostFactor, e, mi, v, o);
 #pragma unroll
                         for (int j = 0; j < 8; j++) h[v][j] *= o[j];
                     }
                     if (has[kPostAddend]) {
-                        get(kPostAddend, e, i, v, o);   // (of elements past the row's last: zeros)
+                        get(kPostAddend, e, mi, v, o);   // (of elements past the row's last: zeros)
 #pragma unroll
                         for (int j = 0; j < 8; j++) h[v][j] += o[j];
                     }
@@ -265,12 +263,12 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
 #pragma unroll
                     for (int j = 0; j < 8; j++) x[v][j] *= f;
                     if (has[kPreFactor]) {
-                        get(kPreFactor, e, i, v, o);
+                        get(kPreFactor, e, mi, v, o);
 #pragma unroll
                         for (int j = 0; j < 8; j++) x[v][j] *= o[j];
                     }
                     if (has[kPreAddend]) {
-                        get(kPreAddend, e, i, v, o);
+                        get(kPreAddend, e, mi, v, o);
 #pragma unroll
                         for (int j = 0; j < 8; j++) x[v][j] += o[j];
                     }

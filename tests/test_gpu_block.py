@@ -175,6 +175,18 @@ def test_norm_many_rows_walk():
     check_norm(x, h, lens, gate=rand(g, 9, 1100), pre=Norm("layer"))
 
 
+def test_norm_modulations_of_tokens():
+    """A modulation for each token, where the last lanes or walks have no row."""
+    from paper_2609_35115_amd.block import Norm
+    g = gen(7)
+    for B, n, width in ((3, 7, 64), (1, 9, 130), (2, 4111, 24), (1, 8195, 520), (3, 701, 1500), (2, 2051, 4104)):
+        lens = torch.randint(0, n + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+        x, h = rand(g, B, n, width), rand(g, B, n, width, dtype=BF16)
+        gate, scale, shift = (rand(g, B, n, width) for _ in range(3))
+        for some in (None, lens):
+            check_norm(x, h, some, post=Norm("rms"), gate=gate, pre=Norm("layer"), scale=scale, shift=shift)
+
+
 def test_norm_special_values():
     from paper_2609_35115_amd.block import Norm, norm_residual
     x = torch.zeros(1, 4, 64, device="cuda")
