@@ -90,11 +90,7 @@ struct PagedParams {
     int splits;
     float* ws;
 };
-struct PagedPlan {
-    int rows, splits;                 // query rows of a block, blocks that share a row's keys
-    int64_t ws_bytes;
-};
-PagedPlan plan_paged(const Paged& c, int n, int group, int window, int sinks);
+struct PagedPlan;   // paged_plan.h
 hipError_t launch_append(const PagedParams& p, hipStream_t st);
 hipError_t launch_attend(const PagedParams& p, const PagedPlan& plan, hipStream_t st);
 

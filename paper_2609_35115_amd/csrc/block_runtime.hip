@@ -8,6 +8,7 @@
 #include "block_internal.h"
 #include "dc_flow.h"
 #include "linear_plan.h"
+#include "paged_plan.h"
 
 using namespace dcb;
 
@@ -134,6 +135,11 @@ Paged paged(const dc_paged* c)
                  units(c->v_stride_page), units(c->v_stride_t), units(c->v_stride_h),
                  c->batch, c->heads, c->head_dim, c->dtype == DC_BF16,
                  __builtin_ctz((unsigned)c->page_size), c->pages, c->page_size * c->table_pages};
+}
+
+PagedPlan plan(const dc_paged* c, int32_t n, int32_t group, int32_t window, int32_t sinks)
+{
+    return plan_paged(c->head_dim, c->dtype == DC_BF16, (int64_t)c->batch * c->heads, n, group, c->page_size * c->table_pages, window, sinks);
 }
 
 dc_status check_span(const dc_span* s, const dc_paged* c)
@@ -284,7 +290,7 @@ int64_t dc_paged_workspace(const dc_paged* c, int32_t q_heads, int32_t n, int32_
 {
     if (check_paged(c) != DC_OK || q_heads < 1 || q_heads % c->heads != 0 || n < 1 || window < 0 || sinks < 0) return 0;
     if (check_size(q_heads, c->batch, n) != DC_OK) return 0;
-    return plan_paged(paged(c), n, q_heads / c->heads, window, sinks).ws_bytes;
+    return plan(c, n, q_heads / c->heads, window, sinks).ws_bytes;
 }
 
 dc_status dc_paged_attend(const dc_paged* c, const dc_span* span, const dc_head_rows* q, const dc_head_rows* out,
@@ -314,12 +320,12 @@ dc_status dc_paged_attend(const dc_paged* c, const dc_span* span, const dc_head_
     p.sinks = window ? sinks : 0;
     p.causal = causal ? 1 : 0;
     p.scale_log2 = scale_log2;
-    const PagedPlan plan = plan_paged(p.c, p.n, p.group, window, sinks);
-    CHECK(plan.ws_bytes == 0 || (workspace && workspace_bytes >= plan.ws_bytes && (uintptr_t)workspace % 16 == 0), DC_EINVAL,
+    const PagedPlan pl = plan(c, p.n, p.group, window, sinks);
+    CHECK(pl.ws_bytes == 0 || (workspace && workspace_bytes >= pl.ws_bytes && (uintptr_t)workspace % 16 == 0), DC_EINVAL,
           "workspace is NULL, too small or not 16-byte aligned");
-    p.splits = plan.splits;
+    p.splits = pl.splits;
     p.ws = (float*)workspace;
-    return done(launch_attend(p, plan, (hipStream_t)hip_stream), "dc_paged_attend");
+    return done(launch_attend(p, pl, (hipStream_t)hip_stream), "dc_paged_attend");
 }
 
 }  // extern "C"

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "block_internal.h"
+#include "paged_plan.h"
 
 namespace dcb {
 
@@ -232,7 +233,7 @@ __device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int
 // straight from memory to registers, one tile ahead (the pages two ahead), with its
 // own base and sums; the waves meet in LDS at the end.  Values go
 // through LDS, for transposed reads.
-template <bool BF16, int D> constexpr int few_blocks() { return D == 64 ? 4 : BF16 ? 3 : 2; }   // on a CU
+template <bool BF16, int D> constexpr int few_blocks() { return D == 64 ? 4 : BF16 ? 3 : 2; }   // on a CU, by registers
 template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, D>())) void attend_few(const PagedParams p)
 {
     constexpr int ES = BF16 ? 2 : 4, CE = 16 / ES, NB = BF16 ? 2 : 1, KT = 16 * NB;   // sixteens and keys of a tile
@@ -802,20 +803,7 @@ template <int D, int NG> __global__ __launch_bounds__(256) void join_kernel(cons
     if (on) store_result(p, e, h, row, d, inverse(l, m), o);
 }
 
-// ------------------------------------------------------------------ choice
-
-PagedPlan plan_paged(const Paged& c, int n, int group, int window, int sinks)
-{
-    const int64_t regions = (int64_t)c.batch * c.heads, rows = (int64_t)n * group;
-    const int64_t keys = window ? std::min((int64_t)c.limit, (int64_t)sinks + window + n) : c.limit;
-    PagedPlan pl{rows <= 16 ? 16 : c.bf16 && rows > 64 ? 128 : 64, 1, 0};
-    const int64_t blocks = regions * ((rows + pl.rows - 1) / pl.rows);
-    const int fit = c.D == 64 ? 4 : c.bf16 ? 3 : 2;   // blocks of 16 rows on a CU
-    if (pl.rows == 16) pl.splits = (int)std::max((int64_t)1, std::min(std::min(256 * fit / blocks, keys / 256), (int64_t)64));
-    else pl.splits = (int)std::max((int64_t)1, std::min(std::min(512 / blocks, keys / 512), (int64_t)16));
-    if (pl.splits > 1) pl.ws_bytes = regions * rows * pl.splits * (c.D + 2) * 4;
-    return pl;
-}
+// ------------------------------------------------------------------ launch
 
 template <bool BF16, int D> hipError_t launch_attend_d(const PagedParams& p, const PagedPlan& plan, hipStream_t st)
 {
