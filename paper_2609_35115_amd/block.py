@@ -59,6 +59,16 @@ def _type(x, name: str) -> int:
     return dt
 
 
+def _overlap(sb: int, st: int, batch: int, n: int, width: int) -> bool:
+    """Whether rows of `width` elements at e sb + i st may share elements."""
+    if n == 0:
+        return False
+    if batch == 1 or n == 1:
+        return (sb if n == 1 else st) < width and batch * n > 1
+    a, b = ((st, n), (sb, batch)) if st <= sb else ((sb, batch), (st, n))
+    return a[0] < width or b[0] < a[0] * a[1]
+
+
 def _rows(at: int, x, name: str, device, batch: int, n: int, width: int, out=False):
     """Fills row set `at` with x [batch][n][width]; its first element's address."""
     if x.dim() != 3 or x.shape[0] != batch or x.shape[1] != n or x.shape[2] != width:
@@ -68,7 +78,7 @@ def _rows(at: int, x, name: str, device, batch: int, n: int, width: int, out=Fal
     sb, st, sc = x.stride()
     if sc != 1 and width > 1:
         _refuse(f"{name}: a row's elements must be consecutive")
-    if out and ((sb == 0 and batch > 1) or (st == 0 and n > 1)):
+    if out and _overlap(sb, st, batch, n, width):
         _refuse(f"{name}: rows that overlap each other's")
     p = x.data_ptr()
     _pack_rows(_frame.rows_, 32 * at, p, sb, st, _type(x, name))

@@ -268,9 +268,13 @@ def test_linear_whole_numbers(K, N, dtype):
         check_linear(x, whole(g, 2 * N, K, dtype=dtype), whole(g, 2 * N, most=1), act="none_glu", gate=whole(g, N), lens=lens, exact=True, out_dtype=F32)
 
 
+TILES = [(1, 3100, 72, 3900), (2, 1560, 200, 3841), (1, 3100, 75, 3900), (1, 700, 64, 2000), (1, 200, 4096, 130), (1, 70, 1030, 70),
+         (1, 8, 4096, 16), (3, 12, 2050, 100), (1, 50, 8192, 48), (1, 30, 8192, 40), (1, 9000, 64, 1200), (3, 200, 4096, 1000), (1, 129, 4100, 300),
+         (1, 4100, 1001, 777)]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-@pytest.mark.parametrize("B,n,K,N", [(1, 3100, 72, 3900), (2, 1560, 200, 3841), (1, 3100, 75, 3900), (1, 700, 64, 2000), (1, 200, 4096, 130), (1, 70, 1030, 70),
-                                     (1, 8, 4096, 16), (3, 12, 2050, 100), (1, 50, 8192, 48)])
+@pytest.mark.parametrize("B,n,K,N", TILES)
 def test_linear_tiles_and_splits(B, n, K, N, dtype):
     """Each tile of rows, rows not of whole chunks, and K split over blocks."""
     g = gen(n)

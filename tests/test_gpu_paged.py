@@ -187,8 +187,11 @@ def test_attend(dtype, D, group):
         check(c, q, pos, lens, window=10_000, sinks=100, scale=-0.1)
 
 
+LONG = [(1, 5000, 1), (1, 3001, 8), (4, 4100, 4), (5, 3000, 8), (70, 2600, 2), (600, 1500, 1), (40, 3000, 8), (24, 2500, 1)]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-@pytest.mark.parametrize("n,past,group", [(1, 5000, 1), (1, 3001, 8), (4, 4100, 4), (5, 3000, 8), (70, 2600, 2), (600, 1500, 1)])
+@pytest.mark.parametrize("n,past,group", LONG)
 def test_attend_long_and_split(dtype, n, past, group):
     g = gen(n)
     for D in (64, 128):
@@ -199,6 +202,27 @@ def test_attend_long_and_split(dtype, n, past, group):
         check(c, q, ints(past, past // 3))
         check(c, q, ints(past, past // 3), window=1700, sinks=33, causal=False)
         check(c, q, ints(past, past // 3), window=300, sinks=33)
+
+
+WIDE = [(700, 70), (2600, 100)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("group", [1, 3, 4])
+def test_attend_wide(dtype, D, group):
+    """Calls of many blocks of rows, in pages smaller and larger than a tile."""
+    g = gen(D * group)
+    for n, past in WIDE:
+        for ps in (4, 128):
+            c = Cache(g, 3, 2, D, dtype, ps, -(-(past + n) // ps), heads_first=ps == 4)
+            lens = lengths(n, n - 1, n // 3)
+            c.fill([past + n, past + n - 1, past + n // 3])
+            q, pos = c.rand(n, 2 * group), ints(past, past, past)
+            say(f"attend {dtype} {D} group {group}: {n} over {past}, pages of {ps}")
+            check(c, q, pos, lens)
+            check(c, q, pos, lens, window=200, sinks=9)
+            check(c, q, pos, lens, window=50, sinks=100, causal=False)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
