@@ -8,6 +8,10 @@
 
 namespace dcb {
 
+// Beside what the second launch of a split call takes the device: what it and its
+// workspace take the host of a call outside a graph is about 3.5 us, of which this counts a part.
+constexpr double kSecondLaunch = 1.5;
+
 enum LinearKind { kFew16, kFew32, kTile64, kTile128, kTile256, kPlane64, kPlane128, kPlane256, kLinearKinds };
 
 // A kernel's block, and what it costs: microseconds fitted to calls of 1 to 20,000
@@ -86,7 +90,7 @@ inline LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
             const double wide = kind <= kFew32 && glu ? 2.0 : 1.0;   // (a block of few rows has the factors besides)
             double us = c.base + (double)steps / s * (c.own * rounds + c.step * k * wide) + c.round * rounds + c.block * k +
                         c.out * (double)M * N * (bf16 ? 2e-6 : 4e-6);
-            if (s > 1) us += c.join + c.part * (double)(M * part_row(N, glu) * s) * 4e-6;
+            if (s > 1) us += c.join + kSecondLaunch + c.part * (double)(M * part_row(N, glu) * s) * 4e-6;
             if (any && us >= least) continue;
             any = true;
             least = us;

@@ -35,6 +35,8 @@ struct PagedCost {
     int fit;
     double base, own, tile, round, block, join, part, split;
 };
+// Beside `join`: a part of what a second launch and a workspace take the host, 3.5 us.
+constexpr double kSecondJoin = 1.5;
 constexpr int kPagedRows[3] = {16, 64, 128};
 constexpr PagedCost kPagedCost[3][2][2] = {   // [rows][128 wide][bf16]
     {{{2, 2.92, 0.808, 0.819, 0.0, 0.499, 2.94, 0.322, 0.0}, {1, 3.59, 1.047, 0.0, 0.511, 0.0, 2.99, 0.0, 0.017}},
@@ -67,7 +69,7 @@ inline PagedPlan plan_paged(int D, int bf16, int64_t regions, int n, int group, 
             if (kind == 0) per = (double)(int64_t)(per / 4 + 0.999);   // (the waves' turns)
             const double k = (double)((blocks * s + 255) / 256), rounds = (double)(int64_t)((k + c.fit - 1) / c.fit);
             double us = c.base + per * (c.own * rounds + c.tile * k) + c.round * rounds + c.block * k;
-            if (s > 1) us += c.join + c.part * (double)(regions * rows * s) * (D + 2) * 4e-6 + c.split * s;
+            if (s > 1) us += c.join + kSecondJoin + c.part * (double)(regions * rows * s) * (D + 2) * 4e-6 + c.split * s;
             if (any && us >= least) continue;
             any = true;
             least = us;

@@ -7,8 +7,8 @@ from __future__ import annotations
 
 from ctypes import byref
 
-from .block import _check, _launch
-from .carry4 import _INT32, _dtype, _frame, _out, _refuse, _rows, _span, _t
+from .block import _check, _launch, _t
+from .carry4 import _INT32, _dtype, _frame, _out, _refuse, _rows, _span
 from .carry4 import _pack_rows as _packs
 from .flow import DcHeadRows, DcPaged, DcSpan, flib
 
