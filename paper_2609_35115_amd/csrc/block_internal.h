@@ -15,6 +15,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 // (global memory takes vectors at any element's alignment)
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef u32x4 __attribute__((aligned(4))) u32x4_dwords;
 typedef u32x2 __attribute__((aligned(2))) u32x2_any;
 typedef uint32_t __attribute__((aligned(2))) u32_any;
 
@@ -203,26 +204,27 @@ template <bool BF16> __device__ __forceinline__ Raw8<BF16> load_raw_part(const v
     default: return load_raw_m<BF16, 7>(p, at);
     }
 }
-template <bool BF16, int M> __device__ __forceinline__ void store_m(void* p, int64_t at, const float (&x)[8])
+// Stores m (1 to 7, uniform) of eight elements: the first ones, or (LAST) the last ones.
+template <bool BF16, int M, bool LAST> __device__ __forceinline__ void store_m(void* p, int64_t at, const float (&x)[8])
 {
-    constexpr int two = M & 4, one = M & 6;
-    if constexpr (M & 4) store4(p, at, BF16, f32x4{x[0], x[1], x[2], x[3]});
+    constexpr int two = M & 4, one = M & 6, from = LAST ? 8 - M : 0;
+    if constexpr (M & 4) store4(p, at, BF16, f32x4{x[from], x[from + 1], x[from + 2], x[from + 3]});
     if constexpr (M & 2) {
-        if constexpr (BF16) *(u32_any*)((uint16_t*)p + at + two) = pack2(x[two], x[two + 1]);
-        else *(u32x2_any*)((float*)p + at + two) = u32x2{__float_as_uint(x[two]), __float_as_uint(x[two + 1])};
+        if constexpr (BF16) *(u32_any*)((uint16_t*)p + at + two) = pack2(x[from + two], x[from + two + 1]);
+        else *(u32x2_any*)((float*)p + at + two) = u32x2{__float_as_uint(x[from + two]), __float_as_uint(x[from + two + 1])};
     }
-    if constexpr (M & 1) store1(p, at + one, BF16, x[one]);
+    if constexpr (M & 1) store1(p, at + one, BF16, x[from + one]);
 }
-template <bool BF16> __device__ __forceinline__ void store_part(void* p, int64_t at, int m, const float (&x)[8])
+template <bool BF16, bool LAST> __device__ __forceinline__ void store_part(void* p, int64_t at, int m, const float (&x)[8])
 {
     switch (m) {
-    case 1: return store_m<BF16, 1>(p, at, x);
-    case 2: return store_m<BF16, 2>(p, at, x);
-    case 3: return store_m<BF16, 3>(p, at, x);
-    case 4: return store_m<BF16, 4>(p, at, x);
-    case 5: return store_m<BF16, 5>(p, at, x);
-    case 6: return store_m<BF16, 6>(p, at, x);
-    default: return store_m<BF16, 7>(p, at, x);
+    case 1: return store_m<BF16, 1, LAST>(p, at, x);
+    case 2: return store_m<BF16, 2, LAST>(p, at, x);
+    case 3: return store_m<BF16, 3, LAST>(p, at, x);
+    case 4: return store_m<BF16, 4, LAST>(p, at, x);
+    case 5: return store_m<BF16, 5, LAST>(p, at, x);
+    case 6: return store_m<BF16, 6, LAST>(p, at, x);
+    default: return store_m<BF16, 7, LAST>(p, at, x);
     }
 }
 template <bool BF16> __device__ __forceinline__ void store8(void* p, int64_t at, const float (&x)[8])

@@ -12,7 +12,7 @@ namespace dcb {
 // workspace take the host of a call outside a graph is about 3.5 us, of which this counts a part.
 constexpr double kSecondLaunch = 1.5;
 
-enum LinearKind { kFew16, kFew32, kTile64, kTile128, kTile256, kPlane64, kPlane128, kPlane256, kLinearKinds };
+enum LinearKind { kFew16, kFew32, kTile64, kTile128, kTile256, kPlane64, kPlane128, kPlane256, kRing128, kLinearKinds };
 
 // A kernel's block, and what it costs: microseconds fitted to calls of 1 to 20,000
 // rows, n_in and n_out from 16 to 8,192, in one to eight splits each (110 sizes, 900
@@ -47,6 +47,7 @@ constexpr LinearCost kLinearCost[2][kLinearKinds] = {
         {64, 64, 3, 3.11, 0.415, 0.255, 0.0, 0.71, 3.59, 0.229, 0.076},
         {128, 128, 2, 3.20, 0.0, 1.132, 0.0, 1.92, 3.23, 0.413, 0.247},
         {256, 128, 1, 3.67, 1.860, 0.0, 0.0, 3.45, 2.71, 0.393, 0.199},
+        {},
     },
     {   // bf16
         {16, 16, 4, 2.65, 0.0, 0.206, 0.0, 0.028, 2.85, 1.59, 0.0},
@@ -55,6 +56,7 @@ constexpr LinearCost kLinearCost[2][kLinearKinds] = {
         {128, 128, 2, 4.30, 0.339, 0.322, 2.16, 0.0, 1.93, 0.339, 0.177},
         {256, 256, 4, 0.0, 0.0, 1.296, 4.91, 4.49, 1.79, 0.336, 0.176},
         {}, {}, {},
+        {128, 128, 1, 3.10, 0.494, 0.0, 1.535, 0.0, 2.88, 0.385, 0.354},
     },
 };
 
@@ -81,7 +83,7 @@ inline LinearPlan plan_linear(int64_t M, int N, int K, int glu, int bf16)
     for (int kind = first; kind < kLinearKinds; kind++) {
         const LinearCost& c = kLinearCost[bf16 ? 1 : 0][kind];
         if (c.bm == 0 || (M <= 16 && kind != kFew16)) continue;
-        if (kind == kTile256 && K % 8 != 0) continue;   // (rows of whole chunks only)
+        if ((kind == kTile256 || kind == kRing128) && K % 8 != 0) continue;   // (rows of whole chunks only)
         const int64_t bc = linear_columns(kind, c.bn, glu), tiles = (M + c.bm - 1) / c.bm * ((N + bc - 1) / bc);
         const int64_t unit = kind <= kFew32 ? 256 : 128, steps = (row + unit - 1) / unit;
         for (int s : {1, 2, 3, 4, 6, 8}) {

@@ -25,8 +25,13 @@ enum { kPostFactor, kPostAddend, kPreFactor, kPreAddend };
 // more than LDS holds) they are read at their use.  The mean is subtracted before
 // squares are summed: no cancellation.
 //
-// What bounds it: HBM.  16,384 rows of 4,096 bf16 (537 MB): see DCB_NORM_FIGURES.
-template <bool RB, bool HB, int NV, int LANES, bool KEEP>
+// What bounds it: HBM, at the rate of a copy (5.1 TB/s) where rows are long and many:
+// 16,384 rows of 4,096 bf16 (537 MB) 104 us, 5.2 TB/s; fp32 with a bf16 sublayer (805 MB)
+// 154 us; rows of 1,024 (134 MB) 29 us, 4.7.  Rows that are not of whole vectors pay for
+// their last one's stores (30,005 of 2,576 130 us, of 2,572 152), rows of two
+// bytes' alignment for their loads (of 2,571 160).  Few rows: the launch, the loads'
+// latency and each sum's (4 of 1,024 4.4 us in a graph).
+template <bool RB, bool HB, int NV, int LANES, bool KEEP, bool REST>
 __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParams p)
 {
     constexpr bool ONE = LANES != 0;
@@ -35,7 +40,14 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     __shared__ float part[2][8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int t = ONE ? lane % (ONE ? LANES : 1) : threadIdx.x, threads = ONE ? LANES : blockDim.x;
-    const int C = p.width, full = C >> 3, rest = C & 7;
+    // A last vector that the row does not fill is the row's last eight elements instead, loaded like the others
+    // (30,005 x 2,572 bf16: 165 us with loads of its own, 152).  `again` of them are the vector's before it as well:
+    // what this thread reads there is not used, and may be the result already where that is in x's place.  Rows of
+    // less than eight elements (`tiny`) are loaded in parts.
+    const int C = p.width, vecs = (C + 7) >> 3, rest = REST ? C & 7 : 0;
+    const bool tiny = REST && C < 8;
+    auto first = [&](int u) { return REST && !tiny ? min(8 * u, C - 8) : 8 * u; };
+    auto again = [&](int u) { return REST && !tiny && u == vecs - 1 ? 8 - rest : 0; };
     int turn = 0;
     auto total = [&](float v) {
         if constexpr (ONE) {
@@ -76,38 +88,32 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
             const int u = t + v * threads;
             xr[v] = Raw8<RB>{};
             hr[v] = Raw8<HB>{};
-            if (on & (u < full)) {
-                xr[v] = load_raw<RB>(p.x.p, xa + 8 * u);
-                if (p.h.p) hr[v] = load_raw<HB>(p.h.p, ha + 8 * u);
-            }
-        }
-        if (rest) {   // (one lane's, apart from the others' loads)
-#pragma unroll
-            for (int v = 0; v < NV; v++) {
-                const int u = t + v * threads;
-                if (on & (u == full)) {
-                    xr[v] = load_raw_part<RB>(p.x.p, xa + 8 * u, rest);
-                    if (p.h.p) hr[v] = load_raw_part<HB>(p.h.p, ha + 8 * u, rest);
-                }
+            if (!on | (u >= vecs)) continue;
+            if (!tiny) {
+                xr[v] = load_raw<RB>(p.x.p, xa + first(u));
+                if (p.h.p) hr[v] = load_raw<HB>(p.h.p, ha + first(u));
+            } else {
+                xr[v] = load_raw_part<RB>(p.x.p, xa, rest);
+                if (p.h.p) hr[v] = load_raw_part<HB>(p.h.p, ha, rest);
             }
         }
     };
 
-    // elements 8 u .. 8 u + 7 of a modulation or gain, `none` where there is none
+    // a modulation or gain of vector u's elements, `none` where there is none
     auto vec = [&](const void* m, int64_t at, int bf16, int u, float none, float (&o)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; j++) o[j] = none;
-        if (!m || u > full || (u == full && !rest)) return;
-        if (u < full) {
-            const f32x4 a = load4(m, at + 8 * u, bf16), b = load4(m, at + 8 * u + 4, bf16);
+        if (!m || u >= vecs) return;
+        if (!tiny) {
+            const f32x4 a = load4(m, at + first(u), bf16), b = load4(m, at + first(u) + 4, bf16);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 o[j] = a[j];
                 o[4 + j] = b[j];
             }
         } else {
-            if (bf16) widen<true>(load_raw_part<true>(m, at + 8 * u, rest), o);
-            else widen<false>(load_raw_part<false>(m, at + 8 * u, rest), o);
+            if (bf16) widen<true>(load_raw_part<true>(m, at, rest), o);
+            else widen<false>(load_raw_part<false>(m, at, rest), o);
         }
     };
     // the factor or addend `which` of vector u of a row
@@ -169,31 +175,38 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     // the factor 1 / sqrt(mean square + eps) of x, with DC_NORM_LAYER of x less its mean, which is taken from x here
     const float inv_c = 1.0f / (float)C;
     auto root = [&](const NormSpec& s, float (&x)[NV][8]) {
-        if (s.kind == DC_NORM_LAYER) {
+        // the sum of f(x) over this thread's elements
+        auto over = [&](auto f) {
             float sum = 0.0f;
 #pragma unroll
+            for (int v = 0; v < NV; v++) {
+                if constexpr (REST) {
+                    const int skip = again(t + v * threads);
+#pragma unroll
+                    for (int j = 0; j < 8; j++) sum = f(sum, j < skip ? 0.0f : x[v][j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; j++) sum = f(sum, x[v][j]);
+                }
+            }
+            return sum;
+        };
+        if (s.kind == DC_NORM_LAYER) {
+            const float mean = total(over([](float sum, float x) { return sum + x; })) * inv_c;
+#pragma unroll
             for (int v = 0; v < NV; v++)
 #pragma unroll
-                for (int j = 0; j < 8; j++) sum += x[v][j];
-            const float mean = total(sum) * inv_c;
-#pragma unroll
-            for (int v = 0; v < NV; v++)
-#pragma unroll
-                for (int j = 0; j < 8; j++) x[v][j] -= 8 * (t + v * threads) + j < C ? mean : 0.0f;
+                for (int j = 0; j < 8; j++) x[v][j] -= (t + v * threads < vecs) & (!tiny | (j < rest)) ? mean : 0.0f;
         }
-        float ss = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; v++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) ss = fmaf(x[v][j], x[v][j], ss);
-        return __builtin_amdgcn_rsqf(total(ss) * inv_c + s.eps);   // 1 ulp
+        return __builtin_amdgcn_rsqf(total(over([](float sum, float x) { return fmaf(x, x, sum); })) * inv_c + s.eps);   // 1 ulp
     };
     auto store = [&](const Rows& o, int64_t at, int v, auto bf16, const float (&x)[8]) {
         const int u = t + v * threads;
-        if (u < full) {
+        if (u < (REST ? C >> 3 : vecs)) {
             store8<decltype(bf16)::value>(o.p, at + 8 * u, x);
-        } else if (u == full && rest) {
-            store_part<decltype(bf16)::value>(o.p, at + 8 * u, rest, x);
+        } else if (REST && u < vecs) {
+            if (tiny) store_part<decltype(bf16)::value, false>(o.p, at, rest, x);
+            else store_part<decltype(bf16)::value, true>(o.p, at + 8 * u, rest, x);
         }
     };
 
@@ -240,7 +253,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
                         for (int j = 0; j < 8; j++) h[v][j] *= o[j];
                     }
                     if (has[kPostAddend]) {
-                        get(kPostAddend, e, mi, v, o);   // (of elements past the row's last: zeros)
+                        get(kPostAddend, e, mi, v, o);   // (of elements past a tiny row's last: zeros)
 #pragma unroll
                         for (int j = 0; j < 8; j++) h[v][j] += o[j];
                     }
@@ -284,7 +297,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     }
 }
 
-template <bool RB, bool HB> hipError_t launch_norm_t(NormParams p, hipStream_t st)
+template <bool RB, bool HB, bool REST> hipError_t launch_norm_t(NormParams p, hipStream_t st)
 {
     const int vecs = (p.width + 7) / 8;
     const bool one = vecs <= 128;
@@ -304,8 +317,8 @@ template <bool RB, bool HB> hipError_t launch_norm_t(NormParams p, hipStream_t s
     p.per = (int)((units + want - 1) / want);
     const int64_t walks = (units + p.per - 1) / p.per, blocks = one ? (walks + 3) / 4 : walks;
 #define DCB_NORM(NV, LANES)                                                                          \
-    (keep ? launch_with(norm_kernel<RB, HB, NV, LANES, true>, blocks, 64 * waves, lds, st, p)         \
-          : launch_with(norm_kernel<RB, HB, NV, LANES, false>, blocks, 64 * waves, 0, st, p))
+    (keep ? launch_with(norm_kernel<RB, HB, NV, LANES, true, REST>, blocks, 64 * waves, lds, st, p)   \
+          : launch_with(norm_kernel<RB, HB, NV, LANES, false, REST>, blocks, 64 * waves, 0, st, p))
     if (!one) return nv == 1 ? DCB_NORM(1, 0) : nv == 2 ? DCB_NORM(2, 0) : DCB_NORM(4, 0);
     if (nv == 2) return DCB_NORM(2, 64);
     return lanes == 8 ? DCB_NORM(1, 8) : lanes == 16 ? DCB_NORM(1, 16) : lanes == 32 ? DCB_NORM(1, 32) : DCB_NORM(1, 64);
@@ -316,8 +329,10 @@ hipError_t launch_norm(NormParams p, hipStream_t st)
 {
     p.rows = p.call.batch * p.call.n;
     const bool hb = p.y.p ? p.y.bf16 : p.h.p ? p.h.bf16 : p.x.bf16;
-    if (p.x.bf16) return hb ? launch_norm_t<true, true>(p, st) : launch_norm_t<true, false>(p, st);
-    return hb ? launch_norm_t<false, true>(p, st) : launch_norm_t<false, false>(p, st);
+#define DCB_NORM(RB, HB) (p.width % 8 ? launch_norm_t<RB, HB, true>(p, st) : launch_norm_t<RB, HB, false>(p, st))
+    if (p.x.bf16) return hb ? DCB_NORM(true, true) : DCB_NORM(true, false);
+    return hb ? DCB_NORM(false, true) : DCB_NORM(false, false);
+#undef DCB_NORM
 }
 
 }  // namespace dcb

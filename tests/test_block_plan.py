@@ -25,7 +25,7 @@ extern "C" void paged(int D, int bf16, int64_t regions, int n, int group, int li
     out[0] = p.rows, out[1] = p.splits, out[2] = p.ws_bytes;
 }
 """
-FEW16, FEW32, TILE64, TILE128, TILE256, PLANE64, PLANE128, PLANE256 = range(8)
+FEW16, FEW32, TILE64, TILE128, TILE256, PLANE64, PLANE128, PLANE256, RING128 = range(9)
 
 
 @pytest.fixture(scope="module")
@@ -88,7 +88,7 @@ def test_workspaces_are_the_plans(plans):
 
 def test_every_linear_kernel_is_run_by_the_gpu_tests(plans):
     from tests import test_gpu_block as g
-    for dtype, kinds in (("bf16", {FEW16, FEW32, TILE64, TILE128, TILE256}), ("f32", {FEW16, FEW32, PLANE64, PLANE128, PLANE256})):
+    for dtype, kinds in (("bf16", {FEW16, FEW32, TILE64, TILE128, TILE256, RING128}), ("f32", {FEW16, FEW32, PLANE64, PLANE128, PLANE256})):
         calls = [(b * n, K, N, glu) for b, n in g.ROWS for K, N in g.SIZES for glu in (0, 1)] + [(b * n, K, N, glu) for b, n, K, N in g.TILES for glu in (0, 1)]
         got = {(k, s > 1) for k, s, _ in (linear(plans, *c[:3], dtype, c[3]) for c in calls)}
         assert {k for k, _ in got} == kinds and {(k, True) for k in kinds if k not in (TILE256, PLANE256)} <= got | {(TILE128, True)}, got

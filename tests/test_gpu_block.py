@@ -270,7 +270,7 @@ def test_linear_whole_numbers(K, N, dtype):
 
 TILES = [(1, 3100, 72, 3900), (2, 1560, 200, 3841), (1, 3100, 75, 3900), (1, 700, 64, 2000), (1, 200, 4096, 130), (1, 70, 1030, 70),
          (1, 8, 4096, 16), (3, 12, 2050, 100), (1, 50, 8192, 48), (1, 30, 8192, 40), (1, 9000, 64, 1200), (3, 200, 4096, 1000), (1, 129, 4100, 300),
-         (1, 4100, 1001, 777)]
+         (1, 4100, 1001, 777), (1, 500, 1096, 2000), (1, 7, 4097, 130), (2, 15, 1003, 40)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
