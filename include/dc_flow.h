@@ -365,9 +365,10 @@ typedef struct dc_norm {
  * r enters the second line before it is rounded.  h NULL: r = x_scale x (post
  * and gate NULL).  post NULL: h itself; gate NULL: ones.  r_out NULL: r is not
  * stored; y_out NULL (with pre, scale and shift): only r.  pre NULL: r itself.
- * scale and shift NULL: zeros.  Widths of 1 to 16384.  r_out may be x or h,
- * y_out h or x (the same rows, types of one size); otherwise rows may not
- * overlap.  Sums in fp32, one rounding of each result. */
+ * scale and shift NULL: zeros.  Widths of 1 to 16384.  r_out has x's type and
+ * y_out h's (either where h is NULL).  r_out may be x or h, y_out h or x (the
+ * same rows, types of one size); otherwise rows may not overlap.  Sums in fp32,
+ * one rounding of each result. */
 dc_status dc_norm_residual(const dc_call* call, int32_t width, const dc_rows* x, float x_scale, const dc_rows* h,
                            const dc_norm* post, const dc_rows* gate, const dc_rows* r_out, const dc_norm* pre,
                            const dc_rows* scale, const dc_rows* shift, const dc_rows* y_out, void* hip_stream);
@@ -394,7 +395,10 @@ typedef struct dc_linear_layer {
  * device bytes, 16-byte aligned (NULL where that is 0), not shared with a call
  * that may run at the same time.  The order of the sums is fixed by the call's
  * sizes (batch, n, n_in, n_out), types and alignment: the same call gives the
- * same bits, whatever the other rows hold. */
+ * same bits, whatever the other rows hold.  DC_F32 calls of more than 32 rows
+ * multiply in three bf16 parts of each value (off by less than 2^-21 of a
+ * product's magnitude, 2^-24 on average; of values below 2^-110 the last bits are
+ * lost): their sums with an infinity in them are NaN. */
 int64_t dc_linear_workspace(const dc_linear_layer* layer, int32_t batch, int32_t n);
 dc_status dc_linear(const dc_call* call, const dc_linear_layer* layer, const dc_rows* x, const dc_rows* gate,
                     const dc_rows* residual, float residual_scale, const dc_rows* out, void* workspace,
@@ -405,7 +409,9 @@ dc_status dc_linear(const dc_call* call, const dc_linear_layer* layer, const dc_
  * (a prompt's pages can stand in the tables of several entries).  A page number
  * outside the pool is a hole: its tokens are not stored, and no query sees
  * them.  Positions from table_pages * page_size on are none either.  The table
- * is read on the device. */
+ * is read on the device.  A call's kernel, splits and workspace go by the
+ * positions that the table has room for: a table much longer than its entries
+ * is better passed as its first pages only. */
 #define DC_PAGED_ABI_VERSION 1
 typedef struct dc_paged {
     int32_t abi_version;      /* DC_PAGED_ABI_VERSION                                           */
@@ -419,7 +425,7 @@ typedef struct dc_paged {
     int64_t table_stride;     /* elements from entry to entry                                   */
     void* k;                  /* device: row t of page g and head h at g stride_page +          */
     void* v;                  /*   t stride_t + h stride_h, in elements; rows aligned to 16     */
-    int64_t k_stride_page, k_stride_t, k_stride_h;   /*   bytes                                 */
+    int64_t k_stride_page, k_stride_t, k_stride_h;   /*   bytes; strides >= 0, below 2^36 bytes */
     int64_t v_stride_page, v_stride_t, v_stride_h;
 } dc_paged;
 

@@ -167,12 +167,11 @@ def norm_residual(x, h=None, *, post=None, gate=None, x_scale: float = 1.0, pre=
     identity); gate, scale, shift: None, [width], [batch][width] or
     [batch][n][width].  Each tensor float32 or bfloat16; r has x's type, y has
     h's.  h None: r = x_scale x, and only y is computed (in x's type, or in
-    out's).  y is None where pre,
-    scale and shift are.  lens int32 [batch] or None: rows behind an entry's
-    lens are left as they are (zeros where out is None).  out: the two results'
-    tensors, either of which may be None (that result is not stored); they may
-    be x and h (r in x, y in h) and share no memory with another argument
-    otherwise."""
+    out's).  y is None where pre, scale and shift are.  Widths to 16384.  lens
+    int32 [batch] or None: rows behind an entry's lens are left as they are
+    (zeros where out is None).  out: the two results' tensors, either of which
+    may be None (that result is not stored); they may be x and h (r in x, y in h)
+    and share no memory with another argument otherwise."""
     torch = _t()
     shape = _shape(x, "x")
     B, n, W = shape
@@ -226,9 +225,10 @@ def linear(x, weight, bias=None, act: str = "none", gate=None, residual=None, re
     float32, one value a row of the weight.  gate: None, [n_out],
     [batch][n_out] or [batch][n][n_out]; residual [batch][n][n_out]; both
     float32 or bfloat16.  lens int32 [batch] or None: rows behind an entry's
-    lens are left as they are (zeros where out is None).  out (x's type, or
-    out_dtype) may be residual itself, and shares no memory with another
-    argument otherwise."""
+    lens are left as they are (zeros where out is None).  out (of either type;
+    where it is None, a new one of x's type or out_dtype) may be residual itself,
+    and shares no memory with another argument otherwise.  In float32 with more
+    than 32 rows a sum with an infinity in it is NaN."""
     torch = _t()
     shape = _shape(x, "x")
     B, n, K = shape

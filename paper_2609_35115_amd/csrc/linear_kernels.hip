@@ -270,6 +270,13 @@ template <int N> __device__ __forceinline__ void dma_wait_but() { asm volatile("
 // XORed with the row's low bits, so that the sixteen rows of an operand read lie in
 // different banks.  With WIDE the loads go from memory to LDS directly, else (rows
 // or K not of whole chunks) through registers.
+//
+// What bounds it, in bf16: large products, the matrix cores and the loads' way from L2
+// to LDS together (256 x 256: 8,192^3 819 us, 1,340 TFLOP/s; 4,096^3 106 us, without the
+// loads 86, without the products 105); smaller tiles, that way alone (64 x 64 tiles of
+// 4,096^3 ask for 19 TB/s, and take as long without the products); one block a CU, the
+// loads' latency, so that four waves and two steps took 64 us for 512 x 4,096 -> 8,192,
+// eight and four 44 (28 without the loads).
 template <bool BF16, int BM, int BN, int WM, int WN, bool WIDE, int ST>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParams p)
 {
@@ -394,9 +401,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
 // fp32 on the bf16 matrix cores, which are sixteen times as fast: every value is
 // the sum of three bf16 planes of eight of its bits each (cut off one after the
 // other, exactly; below 2^-110 the last bits are lost), and six of the nine products
-// of planes are added, the smallest first.  What is left out is below 2^-23 of a
-// product's magnitude.  An infinity comes out as NaN.  The planes are made on the way
+// of planes are added, the smallest first.  What is left out is below 2^-21 of a
+// product's magnitude (a second plane is below 2^-7 of its value, a third below 2^-15,
+// and two products of both are left out), 2^-24 on average.  An infinity comes out
+// as NaN.  The planes are made on the way
 // to LDS: K steps of 32 values through registers and two buffers.
+//
+// What bounds it: the products, and in smaller tiles the planes (5.5 operations a value:
+// 64 x 64 tiles spend as long on them).  4,096^3 585 us, 235 TFLOP/s of fp32 (by
+// fp32's own products 969); 4,011 x 1,001 -> 777 46 us.
 template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM * WN, 2) void plane_kernel(const LinearParams p)
 {
     constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, KT = 32;
@@ -496,6 +509,10 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
 // and all rows; weights and rows go from memory straight to the
 // operand registers, U groups of four chunks at a time, and the waves' sums meet
 // in LDS.
+//
+// What bounds it: HBM where the weight is large (4 x 4,096 -> 8,192 bf16 15.4 us, 4.4 TB/s;
+// fp32 33.7, 4.0; 16 rows 20, since every block reads all of them), else the launch
+// and a load's latency for every U groups (4 x 512 -> 1,536 in a graph 3.2 us).
 template <bool BF16, int MB, int NT, bool WIDE>
 __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 {

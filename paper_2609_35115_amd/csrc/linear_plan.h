@@ -24,13 +24,15 @@ enum LinearKind { kFew16, kFew32, kTile64, kTile128, kTile256, kPlane64, kPlane1
 // of partial sums.  By the fit's choice calls of more than 32 rows took 1.01 times
 // their best choice on average, and 1.16 at most; by rules on the number of blocks
 // (at least 192 of the largest tile) 1.07 and 1.83.  Us of one call by choice
-// (* the fit's), in 64 x 64, 128 x 128 and 256 x 256 tiles, bf16, /splits:
-//     128 x 4,096 -> 8,192    *25.0     30.4/4    34.4/8
-//     512 x 4,096 -> 8,192     66.0    *55.8/2    54.8/4
-//   1,024 x 1,024 -> 1,024     *8.1     16.6      26.3/2
-//  14,336 x   512 -> 2,048     75.6     49.4     *43.7
-//  14,336 x 2,048 ->   512     58.9    *40.1      54.4/2
-//   4,096 x 4,096 -> 4,096    226.6    139.2    *113.0
+// (* the fit's), in 64 x 64, 128 x 128, 128 x 128 through the longer ring (one block
+// a CU) and 256 x 256 tiles, bf16, /splits:
+//     128 x 4,096 -> 8,192    *25.0     30.0/4    26.4/4    37.9/4
+//     512 x 4,096 -> 8,192     66.1     56.2/2   *43.9      55.6/4
+//   1,024 x 1,024 -> 1,024     *8.1     16.6      13.2      26.2/2
+//   2,048 x 2,048 -> 2,048     29.7     27.9     *23.0      42.7/2
+//  14,336 x   512 -> 2,048     74.7     51.2      62.5     *45.1
+//  14,336 x 2,048 ->   512     59.3    *41.1      46.5      54.7/2
+//   4,096 x 4,096 -> 4,096    228.4    140.0     161.5    *113.6
 // and few rows' kernel against 64 x 64 tiles
 //      16 x 4,096 -> 8,192    *20.0     20.4/4
 //      32 x 4,096 -> 8,192     28.4    *21.6/4

@@ -35,7 +35,8 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t page, uint32_t sp, uint3
 
 // ------------------------------------------------------------------- store
 //
-// A thread copies 16 bytes of a key and of its value.  What bounds it: HBM.
+// A thread copies 16 bytes of a key and of its value.  What bounds it: HBM (16,384
+// tokens of eight bf16 heads of 128, 134 MB: 28 us, 4.8 TB/s), or the launch.
 template <int ES> __global__ __launch_bounds__(256) void append_kernel(const PagedParams p)
 {
     constexpr int CE = 16 / ES;
@@ -233,6 +234,11 @@ __device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int
 // straight from memory to registers, one tile ahead (the pages two ahead), with its
 // own base and sums; the waves meet in LDS at the end.  Values go
 // through LDS, for transposed reads.
+//
+// What bounds it: HBM (one token of eight entries over 65,000 keys of eight bf16
+// heads of 128, 2.1 GB: 384 us, 5.5 TB/s; over 30,000 in fp32 357 us, 5.5), with few
+// keys the launch and a tile's latency (13 fp32 tokens of three entries over 281 keys
+// 10 us), a second launch where keys are split.
 template <bool BF16, int D> constexpr int few_blocks() { return D == 64 ? 4 : BF16 ? 3 : 2; }   // on a CU, by registers
 template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, D>())) void attend_few(const PagedParams p)
 {
@@ -452,6 +458,11 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, 
 // chunks are stored with their index XORed with bits of the row, so that the rows
 // of an operand read lie in different banks.  In bf16 the probabilities' sum is one
 // more row of the second product.
+//
+// What bounds it: the products, the exponentials and the maxima between them, about
+// equal (4,096 tokens of two entries over 6,000 others, 16 heads of 128 and four key
+// heads: 536 us, 1,010 TFLOP/s; 64-wide heads 810); in fp32 its own products
+// (1,024 tokens over 2,000 others 383 us, 110 TFLOP/s of 157).
 template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void attend_many(const PagedParams p)
 {
     constexpr int ES = BF16 ? 2 : 4, NB = BF16 ? 4 : 2, KT = 16 * NB, KS = D * ES / 64, DB = D / 16, RB = 64 * QG;
@@ -748,7 +759,7 @@ template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void at
 
 // Joins the splits of a row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
 // NG groups of D / 4 threads share a row's splits, each with its own running
-// maximum, and meet in LDS.
+// maximum, and meet in LDS.  Its parts come from L2 as a rule: the launch bounds it (3 us).
 template <int D, int NG> __global__ __launch_bounds__(256) void join_kernel(const PagedParams p)
 {
     constexpr int CH = D / 4, ROWS = 256 / (CH * NG);   // rows of a block

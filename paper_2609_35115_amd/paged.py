@@ -35,7 +35,9 @@ class PagedCarry:
     position p of entry b lies in page table[b][p // page_size].  A page number
     outside the pool is a hole: nothing is stored there or seen.  The tensors
     are the caller's and are used in place, the table's values as they are when
-    a call runs; positions and lengths stay with the caller too."""
+    a call runs; positions and lengths stay with the caller too.  attend shares
+    out its work by the positions that the table has room for: of a table much
+    longer than its entries, pass table[:, :pages] of those in use."""
 
     def __init__(self, k_pages, v_pages, table):
         torch = _t()

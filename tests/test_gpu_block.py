@@ -6,7 +6,8 @@ A norm's sums add at most 32 values in a lane, six times across lanes and eight
 times across waves, so a mean or a mean square is off by at most 46 U of the
 sum of magnitudes, and K = 64 U covers it with the factors' few roundings.  A
 product of n_in terms is off by at most (n_in + 16) U of the terms' magnitudes
-in any order of the sum; where every term is a small whole number, sums are
+in any order of the sum (the 16 hold what fp32's three parts of a value leave
+out, less than 8 U, and the sum of their products); where every term is a small whole number, sums are
 exact, and results equal the reference's rounding bit for bit."""
 from __future__ import annotations
 
@@ -173,6 +174,21 @@ def test_norm_many_rows_walk():
     x, h = rand(g, 9, 1100, 1100), rand(g, 9, 1100, 1100, dtype=BF16)
     lens = torch.tensor([0, 1100, 3, 0, 0, 700, 1, 1099, 0], device="cuda", dtype=torch.int32)
     check_norm(x, h, lens, gate=rand(g, 9, 1100), pre=Norm("layer"))
+
+
+@pytest.mark.parametrize("width", [9, 63, 513, 1027, 1539, 2571, 4097, 16383])
+def test_norm_results_in_their_inputs_places(width):
+    """Rows whose last vector repeats elements of the one before it, which another wave may have written."""
+    from paper_2609_35115_amd.block import Norm, norm_residual
+    g = gen(width)
+    for dt in (BF16, F32):
+        x, h = rand(g, 3, 1500 if width < 9000 else 200, width, dtype=dt), rand(g, 3, 1500 if width < 9000 else 200, width, dtype=dt)
+        for k in (dict(), dict(pre=Norm("layer")), dict(post=Norm("rms"), pre=Norm("rms"))):
+            want = norm_residual(x, h, x_scale=0.5, out=(torch.empty_like(x), torch.empty_like(h)), **k)
+            for out in (lambda a, b: (a, b), lambda a, b: (b, a)):
+                a, b = x.clone(), h.clone()
+                got = norm_residual(a, b, x_scale=0.5, out=out(a, b), **k)
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_norm_modulations_of_tokens():
