@@ -269,7 +269,8 @@ template <int N> __device__ __forceinline__ void dma_wait_but() { asm volatile("
 // their way while one is multiplied; a row's eight chunks are stored with their index
 // XORed with the row's low bits, so that the sixteen rows of an operand read lie in
 // different banks.  With WIDE the loads go from memory to LDS directly, else (rows
-// or K not of whole chunks) through registers.
+// or K not of whole chunks) through registers, by eight waves (14,336 x 514 -> 2,047 65 us,
+// four 74; 3,000 x 3,001 -> 3,000 120 and 127).
 //
 // What bounds it, in bf16: large products, the matrix cores and the loads' way from L2
 // to LDS together (256 x 256: 8,192^3 819 us, 1,340 TFLOP/s; 4,096^3 106 us, without the
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
     constexpr int KT = kChunks * CE, ROWS = BM + BN, LOADS = ROWS * kChunks / T;
     constexpr int BUF = ROWS * kChunks * 16;
     constexpr int OUT = WM * WN * out_bytes<MI, NI>(), LDS = ST * BUF > OUT ? ST * BUF : OUT;
-    static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0 && (WIDE || ST == 2));
+    static_assert(ROWS * kChunks % T == 0 && T / kChunks % 8 == 0 && (WIDE || ST == 2) && NI % 2 == 0);   // (pairs: glu)
     __shared__ __align__(16) unsigned char smem[LDS];
     __shared__ int some;
     __shared__ Place places[BM];
@@ -544,17 +545,23 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
         if constexpr (WIDE) return k < p.K ? *(const u32x4*)(r + (int64_t)k * ES) : u32x4{0, 0, 0, 0};
         if (whole) {
             const char* a = r + (int64_t)k * ES;
-            if (!BF16 || dwords) return (u32x4) * (const u32x4_any*)a;
-            // Loads at two bytes past a dword go at a third of the rate.  Instead the dwords that hold the
-            // chunk (four, or five with two bytes before it and two behind), shifted: 4 x 4,097 -> 8,192
-            // 35.5 us, 27.7 (4,098: 14.5)
-            const uint32_t off = (uintptr_t)a & 2;
-            const u32x4_dwords d = *(const u32x4_dwords*)(a - off);
-            const uint32_t d4 = *(const uint32_t*)(a + (off ? 14 : 12)), sh = 8 * off;
-            return u32x4{__builtin_amdgcn_alignbit(d[1], d[0], sh), __builtin_amdgcn_alignbit(d[2], d[1], sh),
-                         __builtin_amdgcn_alignbit(d[3], d[2], sh), __builtin_amdgcn_alignbit(d4, d[3], sh)};
+            if (BF16 && !dwords) a -= (uintptr_t)a & 2;   // (see shift)
+            return (u32x4) * (const u32x4_any*)a;
         }
         return k < p.K ? load_chunk<BF16>(r, k, p.K) : u32x4{0, 0, 0, 0};
+    };
+    // Loads at two bytes past a dword go at a third of the rate.  Instead the dwords from two bytes before are loaded
+    // and shifted with the first one of the row's next chunk: the next lane group's, or (of the last group) the next
+    // of the U's, or `end`, the dword at the last chunk's last element.
+    auto last = [&](const char* r, int k) { return *(const uint32_t*)(r + 2 * (int64_t)k - ((uintptr_t)r & 2 ? 0 : 2)); };
+    auto shift = [&](const char* r, u32x4 (&c)[U], uint32_t end) {
+        const uint32_t sh = 8 * ((uintptr_t)r & 2);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const uint32_t next = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((lane + 16) & 63), (int)(g ? c[u][0] : u + 1 < U ? c[u + 1][0] : end));
+#pragma unroll
+            for (int t = 0; t < 4; t++) c[u][t] = __builtin_amdgcn_alignbit(t < 3 ? c[u][t + 1] : next, c[u][t], sh);
+        }
     };
     f32x4 acc[MB][NT];
 #pragma unroll
@@ -562,22 +569,35 @@ __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 #pragma unroll
         for (int j = 0; j < NT; j++) acc[i][j] = f32x4{0, 0, 0, 0};
     for (int q = g0; q < g1; q += U) {
-        u32x4 w[U][NT], x[U][MB];
+        u32x4 w[NT][U], x[MB][U];
         const bool whole = q + U <= g1 && (q + U) * KG <= p.K;
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int k = q + u < g1 ? (q + u) * KG + g * CE : p.K;   // (past this wave's part: zeros)
 #pragma unroll
-            for (int j = 0; j < NT; j++) w[u][j] = chunk(wrow[j], k, whole);
+            for (int j = 0; j < NT; j++) w[j][u] = chunk(wrow[j], k, whole);
 #pragma unroll
-            for (int i = 0; i < MB; i++) x[u][i] = chunk(xrow[i], k, whole);
+            for (int i = 0; i < MB; i++) x[i][u] = chunk(xrow[i], k, whole);
+        }
+        if constexpr (BF16 && !WIDE) {
+            if (whole && !dwords) {   // (uniform)
+                uint32_t we[NT], xe[MB];
+#pragma unroll
+                for (int j = 0; j < NT; j++) we[j] = last(wrow[j], (q + U) * KG - 1);
+#pragma unroll
+                for (int i = 0; i < MB; i++) xe[i] = last(xrow[i], (q + U) * KG - 1);
+#pragma unroll
+                for (int j = 0; j < NT; j++) shift(wrow[j], w[j], we[j]);
+#pragma unroll
+                for (int i = 0; i < MB; i++) shift(xrow[i], x[i], xe[i]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
             for (int i = 0; i < MB; i++)
 #pragma unroll
-                for (int j = 0; j < NT; j++) acc[i][j] = mma<BF16>(w[u][j], x[u][i], acc[i][j]);
+                for (int j = 0; j < NT; j++) acc[i][j] = mma<BF16>(w[j][u], x[i][u], acc[i][j]);
     }
     constexpr int COLS = 16 * NT, PITCH = COLS + 4;
 #pragma unroll
@@ -642,10 +662,10 @@ static hipError_t launch_kind(const LinearParams& p, int kind, hipStream_t st)
     case kFew32: return p.bf16 ? launch_few<true>(p, kind, blocks, st) : launch_few<false>(p, kind, blocks, st);
     case kTile64:
         return p.wide ? launch_with(tile_kernel<true, 64, 64, 2, 2, true, 4>, blocks, 256, 0, st, p)
-                      : launch_with(tile_kernel<true, 64, 64, 2, 2, false, 2>, blocks, 256, 0, st, p);
+                      : launch_with(tile_kernel<true, 64, 64, 4, 2, false, 2>, blocks, 512, 0, st, p);
     case kTile128:
         return p.wide ? launch_with(tile_kernel<true, 128, 128, 2, 2, true, 2>, blocks, 256, 0, st, p)
-                      : launch_with(tile_kernel<true, 128, 128, 2, 2, false, 2>, blocks, 256, 0, st, p);
+                      : launch_with(tile_kernel<true, 128, 128, 2, 4, false, 2>, blocks, 512, 0, st, p);
     case kRing128: return launch_with(tile_kernel<true, 128, 128, 2, 4, true, 4>, blocks, 512, 0, st, p);
     case kTile256: return launch_with(tile_kernel<true, 256, 256, 2, 4, true, 2>, blocks, 512, 0, st, p);
     case kPlane64: return launch_with(plane_kernel<64, 64, 2, 2>, blocks, 256, 0, st, p);

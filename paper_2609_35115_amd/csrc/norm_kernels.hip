@@ -27,10 +27,9 @@ enum { kPostFactor, kPostAddend, kPreFactor, kPreAddend };
 //
 // What bounds it: HBM, at the rate of a copy (5.1 TB/s) where rows are long and many:
 // 16,384 rows of 4,096 bf16 (537 MB) 104 us, 5.2 TB/s; fp32 with a bf16 sublayer (805 MB)
-// 154 us; rows of 1,024 (134 MB) 29 us, 4.7.  Rows that are not of whole vectors pay for
-// their last one's stores (30,005 of 2,576 130 us, of 2,572 152), rows of two
-// bytes' alignment for their loads (of 2,571 160).  Few rows: the launch, the loads'
-// latency and each sum's (4 of 1,024 4.4 us in a graph).
+// 154 us; rows of 1,024 (134 MB) 29 us, 4.7.  Rows not aligned to 16 bytes pay for
+// lines that two loads share (30,005 of 2,576 130 us, of 2,572 144, of 2,571 150).
+// Few rows: the launch, the loads' latency and each sum's (4 of 1,024 4.4 us in a graph).
 template <bool RB, bool HB, int NV, int LANES, bool KEEP, bool REST>
 __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParams p)
 {
@@ -41,7 +40,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int t = ONE ? lane % (ONE ? LANES : 1) : threadIdx.x, threads = ONE ? LANES : blockDim.x;
     // A last vector that the row does not fill is the row's last eight elements instead, loaded like the others
-    // (30,005 x 2,572 bf16: 165 us with loads of its own, 152).  `again` of them are the vector's before it as well:
+    // (30,005 x 2,572 bf16: 165 us with loads and stores of its own, 144).  `again` of them are the vector's before it as well:
     // what this thread reads there is not used, and may be the result already where that is in x's place.  Rows of
     // less than eight elements (`tiny`) are loaded in parts.
     const int C = p.width, vecs = (C + 7) >> 3, rest = REST ? C & 7 : 0;
@@ -200,10 +199,13 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
         }
         return __builtin_amdgcn_rsqf(total(over([](float sum, float x) { return fmaf(x, x, sum); })) * inv_c + s.eps);   // 1 ulp
     };
+    // Elements that two threads have are stored by both, the same bits, but not where another thread may have yet
+    // to read what was there.
     auto store = [&](const Rows& o, int64_t at, int v, auto bf16, const float (&x)[8]) {
         const int u = t + v * threads;
-        if (u < (REST ? C >> 3 : vecs)) {
-            store8<decltype(bf16)::value>(o.p, at + 8 * u, x);
+        const bool twice = REST && !tiny && o.p != p.x.p && o.p != p.h.p;
+        if (u < (!REST || twice ? vecs : C >> 3)) {
+            store8<decltype(bf16)::value>(o.p, at + first(u), x);
         } else if (REST && u < vecs) {
             if (tiny) store_part<decltype(bf16)::value, false>(o.p, at, rest, x);
             else store_part<decltype(bf16)::value, true>(o.p, at + 8 * u, rest, x);
