@@ -409,8 +409,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
 // to LDS: K steps of 32 values through registers and two buffers.
 //
 // What bounds it: the products, and in smaller tiles the planes (5.5 operations a value:
-// 64 x 64 tiles spend as long on them).  4,096^3 585 us, 235 TFLOP/s of fp32 (by
-// fp32's own products 969); 4,011 x 1,001 -> 777 46 us.
+// 64 x 64 tiles spend as long on them).  4,096^3 568 us, 242 TFLOP/s of fp32 (by
+// fp32's own products 969); 4,011 x 1,001 -> 777 45 us.
 template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM * WN, 2) void plane_kernel(const LinearParams p)
 {
     constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, KT = 32;
@@ -437,12 +437,13 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
     auto fetch = [&](int s, u32x4 (&to)[LOADS]) {
         load_chunks<false>(row, s * KT + 4 * (tid % kChunks), p.K, (s + 1) * KT <= p.K, to);
     };
-    // (chunks of eight values, their index XORed with bits of the row: the sixteen rows of a read lie in different banks)
+    // (chunks of eight values, their index XORed with bits of the row: the eight rows that are read at once lie in
+    // different banks)
     auto keep = [&](const u32x4 (&from)[LOADS], int buf) {
 #pragma unroll
         for (int c = 0; c < LOADS; c++) {
             const int r = tid / kChunks + c * (T / kChunks);
-            unsigned char* to = smem + buf * BUF + r * 64 + ((tid % kChunks / 2) ^ ((r >> 2) & 3)) * 16 + tid % 2 * 8;
+            unsigned char* to = smem + buf * BUF + r * 64 + ((tid % kChunks / 2) ^ ((r >> 1) & 3)) * 16 + tid % 2 * 8;
             uint32_t y[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) y[j] = from[c][j];
@@ -460,7 +461,7 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
     for (int i = 0; i < MI; i++)
 #pragma unroll
         for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0, 0, 0, 0};
-    const int ch = l16 * 64 + (g ^ ((l16 >> 2) & 3)) * 16;
+    const int ch = l16 * 64 + (g ^ ((l16 >> 1) & 3)) * 16;
     const unsigned char *xl = smem + wm * (BM / WM) * 64 + ch, *wl = smem + (BM + wn * (BN / WN)) * 64 + ch;
 
     // Of the two waves on a SIMD one makes the next step's planes before its products,
