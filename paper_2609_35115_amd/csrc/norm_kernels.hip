@@ -313,9 +313,11 @@ template <bool RB, bool HB, bool REST> hipError_t launch_norm_t(NormParams p, hi
     const bool keep = !by_token && lds <= 64 * 1024;
     // rows of a walk: as few as give every CU 32 walks of a wave, or blocks of 64 waves
     // (21,001 of 30,005 rows of 2,571, walks that end at their entry's last token: 145 us with eight blocks, 133;
-    // 16,384 of 4,096 111 and 105; more walks read factors more often)
-    const int64_t sides = one ? 64 / lanes : 1, units = (p.rows + sides - 1) / sides;
-    const int64_t want = one ? 256 * 32 : 256 * 64 / waves;
+    // 16,384 of 4,096 111 and 105; more walks read factors more often); of rows that blocks of 16 waves a CU walk in
+    // two to some turns, so many, so that walks load ahead (bf16, us, with 64 and 16 waves: 4,000 rows of 4,096 33.7 and
+    // 29.0, of 2,048 17.9 and 16.7, 1,500 of 4,096 15.8 and 14.8; of 8,192, blocks of eight waves, 52.7 and 56.1)
+    const int64_t sides = one ? 64 / lanes : 1, units = (p.rows + sides - 1) / sides, few = 256 * 16 / waves;
+    const int64_t want = one ? 256 * 32 : waves <= 4 && 3 * units >= 4 * few && units <= 256 * 16 ? few : 256 * 64 / waves;
     p.per = (int)((units + want - 1) / want);
     const int64_t walks = (units + p.per - 1) / p.per, blocks = one ? (walks + 3) / 4 : walks;
 #define DCB_NORM(NV, LANES)                                                                          \

@@ -187,7 +187,7 @@ def test_attend(dtype, D, group):
         check(c, q, pos, lens, window=10_000, sinks=100, scale=-0.1)
 
 
-LONG = [(1, 5000, 1), (1, 3001, 8), (4, 4100, 4), (5, 3000, 8), (70, 2600, 2), (600, 1500, 1), (40, 3000, 8), (24, 2500, 1)]
+LONG = [(1, 5000, 1), (1, 3001, 8), (4, 4100, 4), (5, 3000, 8), (70, 2600, 2), (600, 1500, 1), (40, 3000, 8), (24, 2500, 1), (1, 2000, 40), (2, 700, 23)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
