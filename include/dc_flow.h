@@ -395,8 +395,8 @@ typedef struct dc_linear_layer {
  * device bytes, 16-byte aligned (NULL where that is 0), not shared with a call
  * that may run at the same time.  The order of the sums is fixed by the call's
  * sizes (batch, n, n_in, n_out), types and alignment: the same call gives the
- * same bits, whatever the other rows hold.  DC_F32 calls of more than 32 rows
- * multiply in three bf16 parts of each value (off by less than 2^-21 of a
+ * same bits, whatever the other rows hold.  DC_F32 calls of more than 16 rows
+ * may multiply in three bf16 parts of each value (off by less than 2^-21 of a
  * product's magnitude, 2^-24 on average; of values below 2^-110 the last bits are
  * lost): their sums with an infinity in them are NaN. */
 int64_t dc_linear_workspace(const dc_linear_layer* layer, int32_t batch, int32_t n);

@@ -228,7 +228,7 @@ def linear(x, weight, bias=None, act: str = "none", gate=None, residual=None, re
     lens are left as they are (zeros where out is None).  out (of either type;
     where it is None, a new one of x's type or out_dtype) may be residual itself,
     and shares no memory with another argument otherwise.  In float32 with more
-    than 32 rows a sum with an infinity in it is NaN."""
+    than 16 rows a sum with an infinity in it may be NaN."""
     torch = _t()
     shape = _shape(x, "x")
     B, n, K = shape
