@@ -445,7 +445,9 @@ dc_status dc_paged_append(const dc_paged* c, const dc_span* span, const dc_head_
  * query does not see does not reach its result, whatever it holds.  The span's
  * sinks are not read.  out's rows may be q's.  workspace and the sums' order:
  * as for dc_carry4_attend, of dc_paged_workspace() bytes.  With DC_BF16 the
- * probabilities are rounded to bf16 for the product with the values. */
+ * product with the values takes a probability in two bf16 parts (off by 2^-15 of
+ * it at most) in calls that run in blocks of 16 rows, as most calls of few rows
+ * do; in the others it is rounded to bf16. */
 int64_t dc_paged_workspace(const dc_paged* c, int32_t q_heads, int32_t n, int32_t window, int32_t sinks);
 dc_status dc_paged_attend(const dc_paged* c, const dc_span* span, const dc_head_rows* q, const dc_head_rows* out,
                           int32_t window, int32_t sinks, int32_t causal, float scale, void* workspace,

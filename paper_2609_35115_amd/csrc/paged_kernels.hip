@@ -73,9 +73,13 @@ hipError_t launch_append(const PagedParams& p, hipStream_t st)
 //
 // S^T = K Q^T and O^T += V^T P^T, so that a lane (r, g) = (lane % 16, lane / 16)
 // holds of query r the scores of keys 4 g .. 4 g + 3 of every sixteen, and of its
-// result the dimensions 16 b + 4 g .. + 3.  bf16: a probability is rounded to bf16
-// for the product with the values, half a step of the result's own type.  fp32:
-// four 16x16x4 products of a 16-byte chunk's elements, in fp32 throughout.
+// result the dimensions 16 b + 4 g .. + 3.  bf16: the product with the values takes a
+// probability in two bf16 parts in blocks of 16 rows (the loads bound them: one token
+// over 65,000 keys of 8 entries 386 us, with one part 384), and rounded to bf16, half a
+// step of the result's own type, in blocks of more (the products bound them: 4,096
+// tokens of 2 entries over 6,000 others 533 us, with two parts 711).  Errors are 1.00
+// and 1.41 times those of the result's own rounding.  fp32: four 16x16x4 products of a
+// 16-byte chunk's elements, in fp32 throughout.
 struct RowSpan {
     int hi, lo, sinks;   // a row sees the positions below hi, of those the ones from lo on and the first `sinks`
     RowSpan() = default;
@@ -228,6 +232,26 @@ __device__ __forceinline__ void store_part(const PagedParams& p, int64_t eh, int
         p.ws[parts * p.c.D + 2 * part] = m;
         p.ws[parts * p.c.D + 2 * part + 1] = l;
     }
+}
+
+// Eight probabilities as the sum of two bf16 parts.  The high one is cut from (1 - 2^-8)
+// of a probability, so that the low one, the exact difference, is not 0 either, and an
+// infinite value stays an infinity in both products.  It is below 2^-6 of the
+// probability, and rounded by 2^-15 of it at most.
+struct Parts {
+    u32x4 high, low;
+};
+__device__ __forceinline__ Parts two_parts(f32x4 a, f32x4 b)
+{
+    Parts p;
+    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const uint32_t u = __float_as_uint(x[2 * k] * 0.99609375f), v = __float_as_uint(x[2 * k + 1] * 0.99609375f);
+        p.high[k] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+        p.low[k] = pack2(x[2 * k] - __uint_as_float(u & 0xffff0000u), x[2 * k + 1] - __uint_as_float(v & 0xffff0000u));
+    }
+    return p;
 }
 
 // Up to 16 rows a block.  Each of its four waves takes a tile of keys in turn,
@@ -402,11 +426,13 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, 
             }
         }
         if constexpr (BF16) {
-            const u32x4 pf = {pack2(s[0][0][0], s[0][0][1]), pack2(s[0][0][2], s[0][0][3]), pack2(s[0][1][0], s[0][1][1]), pack2(s[0][1][2], s[0][1][3])};
+            const Parts pf = two_parts(s[0][0], s[0][1]);
 #pragma unroll
             for (int b = 0; b < DB; b++) {
                 const unsigned char* a = vt + (4 * g + (r >> 2)) * VROW + 32 * b + 8 * (r & 3);
-                o[0][b] = mma<true>(read_tr(a, a + 16 * VROW), pf, o[0][b]);
+                const u32x4 v = read_tr(a, a + 16 * VROW);
+                o[0][b] = mma<true>(v, pf.low, o[0][b]);
+                o[0][b] = mma<true>(v, pf.high, o[0][b]);
             }
         } else {
 #pragma unroll
