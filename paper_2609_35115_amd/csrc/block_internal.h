@@ -45,6 +45,7 @@ struct NormParams {
     int width;
     float x_scale;
     int rows, per;     // set at the launch: rows in all, rows of a block's (or wave's) walk
+    int apart;         // set at the launch: results_apart (norm_plan.h)
 };
 hipError_t launch_norm(NormParams p, hipStream_t st);
 

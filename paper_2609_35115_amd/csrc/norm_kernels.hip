@@ -5,6 +5,7 @@
 
 #include "block_internal.h"
 #include "dc_flow.h"
+#include "norm_plan.h"
 
 namespace dcb {
 
@@ -41,8 +42,9 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     const int t = ONE ? lane % (ONE ? LANES : 1) : threadIdx.x, threads = ONE ? LANES : blockDim.x;
     // A last vector that the row does not fill is the row's last eight elements instead, loaded like the others
     // (30,005 x 2,572 bf16: 165 us with loads and stores of its own, 144).  `again` of them are the vector's before it as well:
-    // what this thread reads there is not used, and may be the result already where that is in x's place.  Rows of
-    // less than eight elements (`tiny`) are loaded in parts.
+    // no sum has them twice, and they are stored twice only where both results lie apart from x and h.  Else what this
+    // thread reads there may be a result that another thread has stored, and enters nothing.  Rows of less than eight
+    // elements (`tiny`) are loaded in parts.
     const int C = p.width, vecs = (C + 7) >> 3, rest = REST ? C & 7 : 0;
     const bool tiny = REST && C < 8;
     auto first = [&](int u) { return REST && !tiny ? min(8 * u, C - 8) : 8 * u; };
@@ -199,11 +201,10 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
         }
         return __builtin_amdgcn_rsqf(total(over([](float sum, float x) { return fmaf(x, x, sum); })) * inv_c + s.eps);   // 1 ulp
     };
-    // Elements that two threads have are stored by both, the same bits, but not where another thread may have yet
-    // to read what was there.
+    // Elements that two threads have are stored by both, the same bits, where both have read the inputs.
+    const bool twice = REST && !tiny && p.apart;
     auto store = [&](const Rows& o, int64_t at, int v, auto bf16, const float (&x)[8]) {
         const int u = t + v * threads;
-        const bool twice = REST && !tiny && o.p != p.x.p && o.p != p.h.p;
         if (u < (!REST || twice ? vecs : C >> 3)) {
             store8<decltype(bf16)::value>(o.p, at + first(u), x);
         } else if (REST && u < vecs) {
@@ -332,6 +333,7 @@ template <bool RB, bool HB, bool REST> hipError_t launch_norm_t(NormParams p, hi
 hipError_t launch_norm(NormParams p, hipStream_t st)
 {
     p.rows = p.call.batch * p.call.n;
+    p.apart = results_apart(p.x.p, p.h.p, p.r.p, p.y.p);
     const bool hb = p.y.p ? p.y.bf16 : p.h.p ? p.h.bf16 : p.x.bf16;
 #define DCB_NORM(RB, HB) (p.width % 8 ? launch_norm_t<RB, HB, true>(p, st) : launch_norm_t<RB, HB, false>(p, st))
     if (p.x.bf16) return hb ? DCB_NORM(true, true) : DCB_NORM(true, false);
