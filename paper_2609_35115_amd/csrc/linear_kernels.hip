@@ -273,8 +273,9 @@ template <int N> __device__ __forceinline__ void dma_wait_but() { asm volatile("
 // four 74; 3,000 x 3,001 -> 3,000 120 and 127).
 //
 // What bounds it, in bf16: large products, the matrix cores and the loads' way from L2
-// to LDS together (256 x 256: 8,192^3 819 us, 1,340 TFLOP/s; 4,096^3 106 us, without the
-// loads 86, without the products 105); smaller tiles, that way alone (64 x 64 tiles of
+// to LDS together (256 x 256: 8,192^3 812 and 866 us on two cards, 1,350 and 1,270
+// TFLOP/s; 4,096^3 106 and 114, of which 0.81 are left without the loads and 0.99
+// without the products); smaller tiles, that way alone (64 x 64 tiles of
 // 4,096^3 ask for 19 TB/s, and take as long without the products); one block a CU, the
 // loads' latency, so that four waves and two steps took 64 us for 512 x 4,096 -> 8,192,
 // eight and four 44 (28 without the loads).
@@ -409,8 +410,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
 // to LDS: K steps of 32 values through registers and two buffers.
 //
 // What bounds it: the products, and in smaller tiles the planes (5.5 operations a value:
-// 64 x 64 tiles spend as long on them).  4,096^3 568 us, 242 TFLOP/s of fp32 (by
-// fp32's own products 969); 4,011 x 1,001 -> 777 45 us.
+// 64 x 64 tiles spend as long on them).  4,096^3 563 and 597 us on two cards,
+// 244 and 230 TFLOP/s of fp32 (by fp32's own products 1.7 times as long); 4,011 x 1,001
+// -> 777 45 and 47.
 template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM * WN, 2) void plane_kernel(const LinearParams p)
 {
     constexpr int T = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, KT = 32;
@@ -512,9 +514,11 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
 // operand registers, U groups of four chunks at a time, and the waves' sums meet
 // in LDS.
 //
-// What bounds it: HBM where the weight is large (4 x 4,096 -> 8,192 bf16 15.4 us, 4.4 TB/s;
-// fp32 33.7, 4.0; 16 rows 20, since every block reads all of them), else the launch
-// and a load's latency for every U groups (4 x 512 -> 1,536 in a graph 3.2 us).
+// What bounds it: HBM where the weight is large (4 x 4,096 -> 8,192, weights past the caches,
+// in a graph: bf16 15.3 us, 4.4 TB/s; gated halves, twice the weight, 28.4, 4.7; fp32
+// 33.7, 4.0; 16 rows 19.6, gated 32.5, since every block reads all of them; the same
+// weight again, from the memory-side cache, 13.8, 24.2, 25.1, 17.5 and 25.6), else the
+// launch and a load's latency for every U groups (4 x 512 -> 1,536 in a graph 3.6 us).
 template <bool BF16, int MB, int NT, bool WIDE>
 __global__ __launch_bounds__(256) void few_kernel(const LinearParams p)
 {

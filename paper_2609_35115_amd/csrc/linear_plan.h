@@ -17,11 +17,12 @@ enum LinearKind { kFew16, kFew32, kTile64, kTile128, kTile256, kPlane64, kPlane1
 // A kernel's block, and what it costs: microseconds fitted to calls of 1 to 20,000
 // rows, n_in and n_out from 16 to 8,192, in one to eight splits each (110 sizes, 900
 // calls in a graph over buffers past the caches; most within a tenth, all within 0.6
-// to 1.3).  A CU that has k of the blocks, `fit` of them at once, takes
+// to 1.3).  A CU that has k of the blocks takes
 //   base + steps (own ceil(k / fit) + step k) + round ceil(k / fit) + block k,
-// a step being 128 bytes of a row (few rows: 256, the four waves' together), `out`
-// for a megabyte of the result, and with splits `join` and `part` for a megabyte
-// of partial sums.  By the fit's choice calls of more than 32 rows took 1.01 times
+// `fit` being fitted as the others are, not counted (one 256 x 256 block fills a CU's
+// LDS, and calls of up to four a CU fit best as one round), a step 128 bytes of a row
+// (few rows: 256, the four waves' together), `out` for a megabyte of the result, and
+// with splits `join` and `part` for a megabyte of partial sums.  By the fit's choice calls of more than 32 rows took 1.01 times
 // their best choice on average, and 1.16 at most; by rules on the number of blocks
 // (at least 192 of the largest tile) 1.07 and 1.83.  Us of one call by choice
 // (* the fit's), in 64 x 64, 128 x 128, 128 x 128 through the longer ring (one block

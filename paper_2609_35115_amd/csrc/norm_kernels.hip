@@ -27,10 +27,14 @@ enum { kPostFactor, kPostAddend, kPreFactor, kPreAddend };
 // squares are summed: no cancellation.
 //
 // What bounds it: HBM, at the rate of a copy (5.1 TB/s) where rows are long and many:
-// 16,384 rows of 4,096 bf16 (537 MB) 104 us, 5.2 TB/s; fp32 with a bf16 sublayer (805 MB)
-// 154 us; rows of 1,024 (134 MB) 29 us, 4.7.  Rows not aligned to 16 bytes pay for
-// lines that two loads share (30,005 of 2,576 130 us, of 2,572 144, of 2,571 150).
-// Few rows: the launch, the loads' latency and each sum's (4 of 1,024 4.4 us in a graph).
+// 16,384 rows of 4,096 bf16 (537 MB) 100 us, 5.4 TB/s; fp32 with a bf16 sublayer (805 MB)
+// 154 us; rows of 1,024 (134 MB, past the caches) 30 us, 4.5.  Rows not aligned to 16
+// bytes pay for lines that two loads share (30,005 of 2,576 124 us, of 2,572 128, of
+// 2,571 132; with a modulation for each entry 156).  Modulations for each token are read
+// as rows are (8,192 of 4,096 with three: bf16, 470 MB, 115 us; fp32, 671 MB, 131);
+// factors that LDS does not hold, again for every row (8,192 bf16 of 8,192 with all four
+// arrays 161 us, 3.3 TB/s; 2,000 fp32 of 16,384 161).  Few rows: the launch, the loads'
+// latency and each sum's (4 of 1,024 4.7 us in a graph).
 template <bool RB, bool HB, int NV, int LANES, bool KEEP, bool REST>
 __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParams p)
 {
@@ -41,7 +45,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512) void norm_kernel(const NormParam
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int t = ONE ? lane % (ONE ? LANES : 1) : threadIdx.x, threads = ONE ? LANES : blockDim.x;
     // A last vector that the row does not fill is the row's last eight elements instead, loaded like the others
-    // (30,005 x 2,572 bf16: 165 us with loads and stores of its own, 144).  `again` of them are the vector's before it as well:
+    // (30,005 x 2,572 bf16: with loads and stores of its own 1.15 times as long).  `again` of them are the vector's before it as well:
     // no sum has them twice, and they are stored twice only where both results lie apart from x and h.  Else what this
     // thread reads there may be a result that another thread has stored, and enters nothing.  Rows of less than eight
     // elements (`tiny`) are loaded in parts.

@@ -36,7 +36,7 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t page, uint32_t sp, uint3
 // ------------------------------------------------------------------- store
 //
 // A thread copies 16 bytes of a key and of its value.  What bounds it: HBM (16,384
-// tokens of eight bf16 heads of 128, 134 MB: 28 us, 4.8 TB/s), or the launch.
+// tokens of eight bf16 heads of 128, 134 MB, past the caches: 28.6 us, 4.7 TB/s), or the launch.
 template <int ES> __global__ __launch_bounds__(256) void append_kernel(const PagedParams p)
 {
     constexpr int CE = 16 / ES;
@@ -74,11 +74,11 @@ hipError_t launch_append(const PagedParams& p, hipStream_t st)
 // S^T = K Q^T and O^T += V^T P^T, so that a lane (r, g) = (lane % 16, lane / 16)
 // holds of query r the scores of keys 4 g .. 4 g + 3 of every sixteen, and of its
 // result the dimensions 16 b + 4 g .. + 3.  bf16: the product with the values takes a
-// probability in two bf16 parts in blocks of 16 rows (the loads bound them: one token
-// over 65,000 keys of 8 entries 386 us, with one part 384), and rounded to bf16, half a
-// step of the result's own type, in blocks of more (the products bound them: 4,096
-// tokens of 2 entries over 6,000 others 533 us, with two parts 711).  Errors are 1.00
-// and 1.41 times those of the result's own rounding.  fp32: four 16x16x4 products of a
+// probability in two bf16 parts in blocks of 16 rows (the loads bound them: of one token
+// over 65,000 keys of 8 entries 386 us, one part 384), and rounded to bf16, half a step
+// of the result's own type, in blocks of more (the products bound them: of 4,096 tokens
+// of 2 entries over 6,000 others 533 us, two parts 711; all normally distributed).
+// Errors are 1.00 and 1.41 times those of the result's own rounding.  fp32: four 16x16x4 products of a
 // 16-byte chunk's elements, in fp32 throughout.
 struct RowSpan {
     int hi, lo, sinks;   // a row sees the positions below hi, of those the ones from lo on and the first `sinks`
@@ -260,7 +260,7 @@ __device__ __forceinline__ Parts two_parts(f32x4 a, f32x4 b)
 // through LDS, for transposed reads.
 //
 // What bounds it: HBM (one token of eight entries over 65,000 keys of eight bf16
-// heads of 128, 2.1 GB: 384 us, 5.5 TB/s; over 30,000 in fp32 357 us, 5.5), with few
+// heads of 128, 2.1 GB: 391 us, 5.5 TB/s; over 30,000 in fp32 358 us, 5.5), with few
 // keys the launch and a tile's latency (13 fp32 tokens of three entries over 281 keys
 // 10 us), a second launch where keys are split.
 template <bool BF16, int D> constexpr int few_blocks() { return D == 64 ? 4 : BF16 ? 3 : 2; }   // on a CU, by registers
@@ -487,8 +487,10 @@ template <bool BF16, int D> __global__ __launch_bounds__(256, (few_blocks<BF16, 
 //
 // What bounds it: the products, the exponentials and the maxima between them, about
 // equal (4,096 tokens of two entries over 6,000 others, 16 heads of 128 and four key
-// heads: 536 us, 1,010 TFLOP/s; 64-wide heads 810); in fp32 its own products
-// (1,024 tokens over 2,000 others 383 us, 110 TFLOP/s of 157).
+// heads: 527 and 557 us on two cards, 1,025 and 970 TFLOP/s; 8,192 tokens of 16 heads of
+// 64 169 and 176, 815 and 780, with twice the exponentials a product and the sums' row a
+// fifth of the second product); in fp32 its own products (two entries of 1,024 tokens
+// over 2,000 others 384 us, 110 TFLOP/s of 157).
 template <bool BF16, int D, int QG> __global__ __launch_bounds__(256, 2) void attend_many(const PagedParams p)
 {
     constexpr int ES = BF16 ? 2 : 4, NB = BF16 ? 4 : 2, KT = 16 * NB, KS = D * ES / 64, DB = D / 16, RB = 64 * QG;

@@ -16,10 +16,12 @@ struct PagedPlan {
 // What a kernel costs: microseconds fitted to calls of 1 to 2,000 tokens over 30 to
 // 60,000 others, 1 to 128 entries of 1 to 16 key heads and 1 to 8 query heads each,
 // unsplit and in up to 64 splits (270 calls, 3,300 choices, in a graph; all but a few
-// within a fifth).  A CU that has k of the blocks, `fit` of them at once, takes
+// within a fifth).  A CU that has k of the blocks takes
 //   base + tiles (own ceil(k / fit) + tile k) + round ceil(k / fit) + block k
-// of its blocks' tiles (16 rows: of one wave's, a quarter), and with splits `join`,
-// `part` for a megabyte of partial results and `split` for each.  By the fit's choice
+// of its blocks' tiles (16 rows: of one wave's, a quarter), `fit` being fitted as the
+// others are, not the blocks that a CU holds at once (three of 128 bf16 rows of 64,
+// fitted as six), and with splits `join`, `part` for a megabyte of partial results and `split`
+// for each.  By the fit's choice
 // calls took 1.02 times their best choice on average; by rules (16 rows for up to 16,
 // splits to fill the card) 1.15, and 4 at most.  Us of one call by choice (* the
 // fit's), in blocks of 16, 64 and 128 rows, /splits:
