@@ -398,7 +398,7 @@ typedef struct dc_linear_layer {
  * same bits, whatever the other rows hold.  DC_F32 calls of more than 16 rows
  * may multiply in three bf16 parts of each value (off by less than 2^-21 of a
  * product's magnitude, 2^-24 on average; of values below 2^-110 the last bits are
- * lost): their sums with an infinity in them are NaN. */
+ * lost); sums with an infinity in them are as fp32's own. */
 int64_t dc_linear_workspace(const dc_linear_layer* layer, int32_t batch, int32_t n);
 dc_status dc_linear(const dc_call* call, const dc_linear_layer* layer, const dc_rows* x, const dc_rows* gate,
                     const dc_rows* residual, float residual_scale, const dc_rows* out, void* workspace,

@@ -227,8 +227,7 @@ def linear(x, weight, bias=None, act: str = "none", gate=None, residual=None, re
     float32 or bfloat16.  lens int32 [batch] or None: rows behind an entry's
     lens are left as they are (zeros where out is None).  out (of either type;
     where it is None, a new one of x's type or out_dtype) may be residual itself,
-    and shares no memory with another argument otherwise.  In float32 with more
-    than 16 rows a sum with an infinity in it may be NaN."""
+    and shares no memory with another argument otherwise."""
     torch = _t()
     shape = _shape(x, "x")
     B, n, K = shape

@@ -207,6 +207,21 @@ template <int BM, int BN> struct TileAt {
     }
 };
 
+// The weight's row that is row r of a block's BN, columns past N from its last row.
+template <int BN, int WN, int ES> __device__ __forceinline__ const char* weight_row(const LinearParams& p, int n0, int r)
+{
+    constexpr int NI = BN / WN / 16;
+    int col, part = 0;
+    if (p.glu) {   // a wave's first half of 16-column groups, and the same columns' factors
+        const int w = r / (BN / WN), f = r / 16 % NI;
+        part = f >= NI / 2;
+        col = n0 + w * (BN / WN / 2) + (f - part * (NI / 2)) * 16 + r % 16;
+    } else {
+        col = n0 + r;
+    }
+    return (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
+}
+
 // The operands' rows that a thread loads: its chunk of rows tid / 8 + c T / 8, first
 // the BM rows of x, then those of the weight.  Rows that the call does not have are
 // read from the weight instead and columns past N from its last row: their results
@@ -215,7 +230,6 @@ template <int BM, int BN> struct TileAt {
 template <int BM, int BN, int WN, int T, int ES, int LOADS>
 __device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt<BM, BN>& at, Place (&places)[BM], const char* (&row)[LOADS])
 {
-    constexpr int NI = BN / WN / 16;
     for (int m = threadIdx.x; m < BM; m += T) places[m] = place_of(p, at.m0 + m);
     __syncthreads();
     bool any = false;
@@ -227,15 +241,7 @@ __device__ __forceinline__ bool operand_rows(const LinearParams& p, const TileAt
             any |= x.on();
             row[c] = x.on() ? (const char*)p.x.p + (x.e * p.x.sb + x.i * p.x.st) * ES : (const char*)p.w;
         } else {
-            int r = rr - BM, col, part = 0;
-            if (p.glu) {   // a wave's first half of 16-column groups, and the same columns' factors
-                const int w = r / (BN / WN), f = r / 16 % NI;
-                part = f >= NI / 2;
-                col = at.n0 + w * (BN / WN / 2) + (f - part * (NI / 2)) * 16 + r % 16;
-            } else {
-                col = at.n0 + r;
-            }
-            row[c] = (const char*)p.w + ((int64_t)part * p.N + min(col, p.N - 1)) * p.wstride * ES;
+            row[c] = weight_row<BN, WN, ES>(p, at.n0, rr - BM);
         }
     }
     return any;
@@ -405,9 +411,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(const LinearParam
 // other, exactly; below 2^-110 the last bits are lost), and six of the nine products
 // of planes are added, the smallest first.  What is left out is below 2^-21 of a
 // product's magnitude (a second plane is below 2^-7 of its value, a third below 2^-15,
-// and two products of both are left out), 2^-24 on average.  An infinity comes out
-// as NaN.  The planes are made on the way
-// to LDS: K steps of 32 values through registers and two buffers.
+// and two products of both are left out), 2^-24 on average.  An infinity has planes
+// that are NaN: sums that come out as NaN are computed again by fp32's own products
+// (only those, so that a row's bits do not depend on other rows).  The planes are made
+// on the way to LDS: K steps of 32 values through registers and two buffers.
 //
 // What bounds it: the products, and in smaller tiles the planes (5.5 operations a value:
 // 64 x 64 tiles spend as long on them).  4,096^3 563 and 597 us on two cards,
@@ -499,6 +506,30 @@ template <int BM, int BN, int WM, int WN> __global__ __launch_bounds__(64 * WM *
             }
             if (!ahead) next();
             __syncthreads();
+        }
+    }
+    float nan = 0.0f;   // 0 times a sum: NaN for one that is no number
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) nan = fmaf(0.0f, acc[i][j][k], nan);
+    if (__builtin_expect(__any(nan != nan), 0)) {
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const Place x = places[wm * (BM / WM) + 16 * i + l16];
+            const char* xr = x.on() ? (const char*)p.x.p + (x.e * p.x.sb + x.i * p.x.st) * 4 : (const char*)p.w;
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const char* wr = weight_row<BN, WN, 4>(p, at.n0, wn * (BN / WN) + 16 * j + l16);
+                f32x4 own = {0, 0, 0, 0};
+#pragma unroll 1
+                for (int k = s0 * KT; k < min(s1 * KT, p.K); k += 16)
+                    own = mma<false>(load_chunk<false>(wr, k + 4 * g, p.K), load_chunk<false>(xr, k + 4 * g, p.K), own);
+#pragma unroll
+                for (int k = 0; k < 4; k++) acc[i][j][k] = acc[i][j][k] != acc[i][j][k] ? own[k] : acc[i][j][k];
+            }
         }
     }
     __syncthreads();
